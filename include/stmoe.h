@@ -31,6 +31,8 @@
  *     [sync].
  *   - Limits: 1 <= E <= 256 (8-bit expert indices in the tables),
  *     1 <= K <= min(E, 16), 1 <= B <= 16, H and I multiples of 8, H <= 16384.
+ *     moe_route_balance and moe_expert_ffn_mx take batches of T tokens
+ *     beyond B.
  *   - Data types: STMOE_BF16 (weights and activations bfloat16, fp32
  *     accumulation) or STMOE_F32.  Outputs of the FFN are fp32.
  */
@@ -53,7 +55,10 @@ enum {
     STMOE_ESTATE = -5      /* call out of order (e.g. predict before profile) */
 };
 
-typedef enum { STMOE_F32 = 0, STMOE_BF16 = 1 } stmoe_dtype;
+/* STMOE_MXFP4 names microscaled 4-bit experts (packed by moe_mx_pack_expert):
+ * moe_blob_bytes and moe_model_desc take it (there with bf16 hidden states and
+ * routers); matrices, hidden states and logits are STMOE_F32 or STMOE_BF16. */
+typedef enum { STMOE_F32 = 0, STMOE_BF16 = 1, STMOE_MXFP4 = 2 } stmoe_dtype;
 
 /* Message of the last failed call on this thread ("" if none). */
 const char* stmoe_last_error(void);
@@ -171,9 +176,57 @@ int stmoe_import(stmoe_predictor* p, const uint8_t* cct_idx, const uint8_t* cct_
 int stmoe_stats(stmoe_predictor* p, int64_t* out);
 
 /* ------------------------------------------------------------------------
+ * The router over a batch of T tokens, for training: from logits, the top-K
+ * selection and gate weights as moe_route_topk gives them, the number of
+ * selections per expert, and two losses,
+ *   balance = E * sum_e counts[e] / (n K) * prob_sum[e] / n
+ *   z       = sum_t lse_t^2 / n
+ * with prob_sum[e] = sum_t softmax(logits[t])[e] and lse_t the logarithm of
+ * sum_e exp(logits[t][e]), over the n tokens that count: those whose mask is
+ * not zero and that have a logit above minus infinity.  A logit of minus
+ * infinity is no candidate and has probability 0; the type's lowest value is
+ * a number like others.  A NaN ranks below every number and makes its row's
+ * weights and the losses NaN.
+ *
+ *   logits   device [T] rows of E values, row stride ld elements, dtype
+ *   mask     device [T] uint8, or NULL: every token counts
+ *   topk_idx device out [T][K] int32; -1 (and weight 0) where a row has fewer
+ *            than K candidates, and throughout a row that does not count
+ *   topk_w   device out [T][K] fp32
+ *   counts   device out [E] int32
+ *   n_tokens device out [1] int32: n
+ *   prob_sum device out [E] fp32, or NULL
+ *   loss     device out [2] fp32: balance, z (both 0 if n is 0)
+ *   ws       device workspace of moe_route_balance_workspace_bytes(T, E)
+ *            bytes, 256-byte aligned; calls sharing it must be ordered on one
+ *            stream
+ *   0 <= T <= 2^26; T = 0 writes zero counts and losses.  Sums run in a fixed
+ *   order: the same inputs give the same bits.
+ * ---------------------------------------------------------------------- */
+size_t moe_route_balance_workspace_bytes(int64_t T, int E);
+int moe_route_balance(const void* logits, int64_t T, int64_t ld, int E, int K, int dtype, int renorm,
+                      const uint8_t* mask, int32_t* topk_idx, float* topk_w, int32_t* counts,
+                      int32_t* n_tokens, float* prob_sum, float* loss, void* ws, size_t ws_bytes,
+                      void* stream);
+/* Its gradient: d_logits from the gradients of the gate weights and of the
+ * two losses, with the selection and the counts as constants.  logits,
+ * topk_idx, counts and n_tokens as moe_route_balance took and gave them (the
+ * counts and n_tokens may be summed over ranks); rows whose first topk_idx is
+ * negative get zeros.
+ *   d_w      device [T][K] fp32, or NULL (zeros)
+ *   d_loss   device [2] fp32
+ *   d_logits device out [T] rows of E values, row stride ld_d, dtype; may be
+ *            logits itself when ld_d = ld */
+int moe_route_balance_backward(const void* logits, int64_t T, int64_t ld, int E, int K, int dtype,
+                               int renorm, const int32_t* topk_idx, const int32_t* counts,
+                               const int32_t* n_tokens, const float* d_w, const float* d_loss,
+                               void* d_logits, int64_t ld_d, void* stream);
+
+/* ------------------------------------------------------------------------
  * Expert packing.  A packed expert ("blob") is one contiguous buffer:
  * W_gate [I][H], then W_up [I][H], then W_down [H][I], each row-major in
  * the storage dtype; 3*H*I elements.  One blob moves with one copy.
+ * (STMOE_MXFP4 blobs are laid out by moe_mx_pack_expert, below.)
  * ---------------------------------------------------------------------- */
 size_t moe_blob_bytes(int H, int I, int dtype);
 /* [sync, host] blob_out: host, moe_blob_bytes(H, I, dtype) bytes. */
@@ -229,6 +282,62 @@ int moe_expert_ffn(const void* x, const int32_t* topk_idx, const float* topk_w, 
 int moe_expert_ffn_noalloc(const void* x, const int32_t* topk_idx, const float* topk_w, int B, int K,
                            int H, int I, int E, int dtype, const void* const* expert_ptrs,
                            const void* const* shared_ptrs, int n_shared, float* y, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Microscaled 4-bit floats (MXFP4).  32 consecutive columns of a row share
+ * the scale 2^(s - 127), s the scale byte; an element is a 4-bit code (bit 3
+ * the sign, bits 0..2 the magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6), its value the
+ * code's times the scale.  A matrix [rows][cols] is held row-major as
+ *   codes  [rows][ceil(cols / 2)] bytes, column 2j in the low half of byte j
+ *          (the last high half of an odd row is 0)
+ *   scales [rows][ceil(cols / 32)] bytes
+ * Quantising takes as scale the power of two at or below the block's largest
+ * magnitude, divided by 4 (at least 2^-127), and rounds every value / scale to
+ * the nearest magnitude, ties to the even code, at most 6.  A block that holds
+ * an infinity or a NaN gets the scale byte 255 and codes 0: its values read
+ * back as NaN.  Every value read back is exact in both dtypes.
+ *   x, y   device, dtype, row stride ld elements (>= cols)
+ *   rows   0 <= rows <= 2^31 (0: nothing is done); 1 <= cols <= 2^30
+ * ---------------------------------------------------------------------- */
+int moe_mx_quantize(const void* x, int64_t rows, int cols, int64_t ld, int dtype, uint8_t* codes,
+                    uint8_t* scales, void* stream);
+int moe_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols, void* y,
+                      int64_t ld, int dtype, void* stream);
+
+/* Pack one expert for moe_expert_ffn_mx: W_gate [I][H], W_up [I][H] and W_down
+ * [H][I] as codes and scales (device) into blob_out (device, 16-byte aligned,
+ * moe_blob_bytes(H, I, STMOE_MXFP4) bytes).  The blob can be copied anywhere
+ * (a pinned host pool, cache slots).  H a multiple of 8 up to 16384, I one up
+ * to 65536. */
+int moe_mx_pack_expert(const uint8_t* gate_codes, const uint8_t* gate_scales, const uint8_t* up_codes,
+                       const uint8_t* up_scales, const uint8_t* down_codes, const uint8_t* down_scales,
+                       int H, int I, void* blob_out, void* stream);
+
+/* The expert FFN over MXFP4 blobs, for 0 to 65536 tokens in one call (decode
+ * steps and prompts): the formula of moe_expert_ffn with the blobs' values.
+ *   x            device [T][H] dtype, 16-byte aligned
+ *   topk_idx     device [T][K] int32, topk_w device [T][K] fp32; an entry
+ *                outside [0, E) is ignored, and an expert repeated within a
+ *                row counts once, with its first entry's weight; a row without
+ *                any entry (and shared expert) gives zeros
+ *   expert_ptrs  device array [E] of device blob pointers (16-byte aligned
+ *                blobs); only selected experts' entries are read
+ *   shared_ptrs  device array [n_shared] of device blob pointers, or NULL
+ *   y            device out [T][H] ydtype, 16-byte aligned
+ *   ws           device workspace of moe_expert_ffn_mx_workspace_bytes(...)
+ *                bytes, 256-byte aligned, no initial contents required; calls
+ *                sharing it must be ordered on one stream
+ * dtype and ydtype: STMOE_BF16 or STMOE_F32 each.  Sums are fp32.  fp32 x, and
+ * the activations when y is fp32, enter the products as two bf16 pieces (16
+ * significant bits); with bf16 y the activations are rounded to bf16.  The
+ * same inputs give the same bits, and a token's result does not depend on the
+ * others'. */
+size_t moe_expert_ffn_mx_workspace_bytes(int T, int K, int E, int H, int I, int n_shared, int dtype,
+                                         int ydtype);
+int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const float* topk_w, int T, int K, int H,
+                      int I, int E, int dtype, int ydtype, const void* const* expert_ptrs,
+                      const void* const* shared_ptrs, int n_shared, void* y, void* ws, size_t ws_bytes,
+                      void* stream);
 
 /* ------------------------------------------------------------------------
  * Expert cache policy (host only, no HIP calls): per-layer partition of C
@@ -390,7 +499,8 @@ int expert_cache_stats(const expert_cache* c, stmoe_cache_stats* out);
 enum { MOE_MODE_ON_DEMAND = 0, MOE_MODE_STMOE = 1, MOE_MODE_HT_ONLY = 2, MOE_MODE_CCT_ONLY = 3 };
 
 typedef struct {
-    int L, E, K, B, H, I, n_shared, dtype, renorm;
+    int L, E, K, B, H, I, n_shared, dtype, renorm;   /* dtype STMOE_MXFP4: 4-bit experts (shared ones
+                                      too), bf16 hidden states and routers */
     const void* const* router_w;   /* host [L] device pointers to W_g [E][H] */
     const void* const* shared_w;   /* host [L*n_shared] device blob pointers, or NULL */
     const void* const* resident_w; /* host [L*E] device blob pointers when every routed

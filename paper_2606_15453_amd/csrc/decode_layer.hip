@@ -24,6 +24,9 @@ int ffn_launch(const void* x, const int32_t* idx, const float* w, int B, int K, 
                float* y, void* ws, hipStream_t s, unsigned long long* n_experts, hipEvent_t ev_mid,
                const float* logits, int renorm, const void* ebase, size_t estride, int ready, const void* router,
                int host);
+int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int K, int H, int I, int E, int dtype,
+                  int ydtype, const void* const* eptr, const void* const* sptr, int n_shared, void* y, void* ws,
+                  hipStream_t s, unsigned long long* n_experts, hipEvent_t ev_mid);
 bool ffn_takes_router(int B, int K, int H, int I, int E, int n_shared, int dtype);
 int ffn_route_place(int B, int K, int H, int I, int E, int n_shared, int dtype);
 int ffn_route_plan(const float* z, int renorm, int32_t* idx, float* w, int B, int K, int H, int I, int E, int dtype,
@@ -69,7 +72,8 @@ __global__ void next_token_kernel(int64_t* tok) { *tok += 1; }
 using namespace stmoe;
 
 struct moe_ctx {
-    int L, E, K, B, H, I, n_shared, dtype, renorm;
+    int L, E, K, B, H, I, n_shared, dtype, renorm;   // dtype of the hidden states and routers
+    bool mx = false;                       // the experts are MXFP4 blobs
     size_t esz;
     std::vector<const void*> router;       // [L]
     // resident blobs at a fixed stride within every layer (one allocation,
@@ -184,9 +188,12 @@ struct CtxLayout {
 CtxLayout ctx_layout(const moe_model_desc* d) {
     CtxLayout y{};
     const size_t LBK = size_t(d->L) * d->B * d->K, LBH = size_t(d->L) * d->B * d->H;
-    const size_t esz = d->dtype == STMOE_BF16 ? 2 : 4;
+    const size_t esz = d->dtype == STMOE_F32 ? 4 : 2;
     y.route_ws_bytes = moe_route_workspace_bytes(d->B, d->E);
-    y.ffn_ws_bytes = moe_expert_ffn_workspace_bytes(d->B, d->K, d->E, d->H, d->I, d->n_shared, d->dtype);
+    y.ffn_ws_bytes =
+        d->dtype == STMOE_MXFP4
+            ? moe_expert_ffn_mx_workspace_bytes(d->B, d->K, d->E, d->H, d->I, d->n_shared, STMOE_BF16, STMOE_F32)
+            : moe_expert_ffn_workspace_bytes(d->B, d->K, d->E, d->H, d->I, d->n_shared, d->dtype);
     y.seq_bytes = update_predict_seq_bytes(d->L);
     size_t off = 0;
     auto take = [&](size_t n) { const size_t at = off; off = (off + n + 255) / 256 * 256; return at; };
@@ -215,7 +222,8 @@ int check_desc(const moe_model_desc* d) {
     STMOE_CHECK(d->I >= 8 && d->I % 8 == 0, "bad I");
     STMOE_CHECK(d->n_shared >= 0 && d->n_shared <= 8, "bad n_shared");
     STMOE_CHECK(d->n_shared == 0 || d->shared_w, "shared_w is required when n_shared > 0");
-    STMOE_CHECK(d->dtype == STMOE_BF16 || d->dtype == STMOE_F32, "bad dtype");
+    STMOE_CHECK(d->dtype == STMOE_BF16 || d->dtype == STMOE_F32 || d->dtype == STMOE_MXFP4, "bad dtype");
+    STMOE_CHECK(d->dtype != STMOE_MXFP4 || moe_blob_bytes(d->H, d->I, STMOE_MXFP4), "bad I for MXFP4 experts");
     return STMOE_OK;
 }
 
@@ -306,8 +314,10 @@ extern "C" int moe_ctx_create(const moe_model_desc* d, stmoe_predictor* pred, ex
     }
     auto* c = new moe_ctx();
     c->L = d->L; c->E = d->E; c->K = d->K; c->B = d->B; c->H = d->H; c->I = d->I;
-    c->n_shared = d->n_shared; c->dtype = d->dtype; c->renorm = d->renorm;
-    c->esz = d->dtype == STMOE_BF16 ? 2 : 4;
+    c->n_shared = d->n_shared; c->renorm = d->renorm;
+    c->mx = d->dtype == STMOE_MXFP4;
+    c->dtype = c->mx ? STMOE_BF16 : d->dtype;
+    c->esz = c->dtype == STMOE_BF16 ? 2 : 4;
     c->router.assign(d->router_w, d->router_w + d->L);
     c->pred = pred;
     c->cache = cache;
@@ -450,7 +460,7 @@ int decode_layer(moe_ctx* c, int token, int layer, const void* x, float* y, int 
         STMOE_HIP(hipStreamWaitEvent(c->s, c->ev_side, 0));
         c->side_pending = false;
     }
-    const int place = c->cache ? kRouteTail : ffn_route_place(B, K, c->H, c->I, E, c->n_shared, c->dtype);
+    const int place = c->cache || c->mx ? kRouteTail : ffn_route_place(B, K, c->H, c->I, E, c->n_shared, c->dtype);
     const bool plan = place == kRouteTailPlan, route_in_ffn = place == kRouteInFfn;
     const void* ebase = c->rbase.empty() ? nullptr : c->rbase[size_t(layer)];
     const void* const* sptr = c->n_shared ? c->shared + size_t(layer) * c->n_shared : nullptr;
@@ -558,7 +568,11 @@ int decode_layer(moe_ctx* c, int token, int layer, const void* x, float* y, int 
         if (!e1) { set_error("moe_decode_layer: hipEventCreate failed"); return STMOE_EHIP; }
         tl.mid = int(c->ev_used - 1);
     }
-    if (int rc = ffn_launch(x, idx_l, w_l, B, K, c->H, c->I, E, c->dtype, c->tables + size_t(layer) * E,
+    if (c->mx) {
+        if (int rc = mx_ffn_launch(x, idx_l, w_l, B, K, c->H, c->I, E, c->dtype, STMOE_F32, c->tables + size_t(layer) * E,
+                                   sptr, c->n_shared, y, c->ffn_ws, c->s, timed ? c->n_experts : nullptr, e1))
+            return rc;
+    } else if (int rc = ffn_launch(x, idx_l, w_l, B, K, c->H, c->I, E, c->dtype, c->tables + size_t(layer) * E,
                             sptr, c->n_shared,
                             y, c->ffn_ws, c->s, timed ? c->n_experts : nullptr, e1,
                             route_in_ffn && !router_in_ffn ? zbuf : nullptr, c->renorm, ebase, c->rstride, plan,

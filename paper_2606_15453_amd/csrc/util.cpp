@@ -2,7 +2,7 @@
 #include <cstring>
 #include <string>
 
-#include "common.h"
+#include "mx_format.h"
 
 namespace stmoe {
 namespace {
@@ -37,7 +37,9 @@ extern "C" int stmoe_host_free(void* p) {
 }
 
 extern "C" size_t moe_blob_bytes(int H, int I, int dtype) {
-    if (H < 1 || I < 1 || (dtype != STMOE_BF16 && dtype != STMOE_F32)) return 0;
+    if (H < 1 || I < 1) return 0;
+    if (dtype == STMOE_MXFP4) return H % 8 || I % 8 || H > kMaxH || I > mx::kMaxI ? 0 : mx::blob(H, I).total;
+    if (dtype != STMOE_BF16 && dtype != STMOE_F32) return 0;
     return size_t(3) * H * I * (dtype == STMOE_BF16 ? 2 : 4);
 }
 

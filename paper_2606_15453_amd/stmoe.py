@@ -39,7 +39,7 @@ if len(_hip_runtimes()) > 1:
     raise ImportError(f"more than one HIP runtime mapped: {_hip_runtimes()}")
 
 OK, EINVAL, EHIP, ENOMEM, ECAPACITY, ESTATE = 0, -1, -2, -3, -4, -5
-F32, BF16 = 0, 1
+F32, BF16, MXFP4 = 0, 1, 2
 USE_CCT, USE_HT, USE_BOTH = 1, 2, 3
 MODE_ON_DEMAND, MODE_STMOE, MODE_HT_ONLY, MODE_CCT_ONLY = 0, 1, 2, 3
 
@@ -94,6 +94,14 @@ _SIGS = {
     "moe_pack_expert": (i32, [vp, vp, vp, i32, i32, i32, vp]),
     "moe_expert_ffn_workspace_bytes": (sz, [i32, i32, i32, i32, i32, i32, i32]),
     "moe_expert_ffn": (i32, [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp, sz, vp]),
+    "moe_route_balance_workspace_bytes": (sz, [i64, i32]),
+    "moe_route_balance": (i32, [vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+    "moe_route_balance_backward": (i32, [vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp]),
+    "moe_mx_quantize": (i32, [vp, i64, i32, i64, i32, vp, vp, vp]),
+    "moe_mx_dequantize": (i32, [vp, vp, i64, i32, vp, i64, i32, vp]),
+    "moe_mx_pack_expert": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]),
+    "moe_expert_ffn_mx_workspace_bytes": (sz, [i32, i32, i32, i32, i32, i32, i32, i32]),
+    "moe_expert_ffn_mx": (i32, [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp, sz, vp]),
     "moe_expert_ffn_noalloc": (i32, [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp]),
     "expert_cache_warm_sets": (i32, [vp, i32, i32, i32, i32, i32, i32, vp]),
     "expert_cache_use_counts": (i32, [vp, i32, i32, i32, i32, i32, vp]),
@@ -240,6 +248,79 @@ def route_topk(x, w_gate, K, idx, w, ws, renorm=False, logits=None, stream=None,
           _p(logits), _p(ws), ws.numel() * ws.element_size(), _s(stream))
 
 
+# ---------------------------------------------------------------- checks of tensor arguments
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _dt(name, t):
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return d
+
+
+def _dense(name, t, shape, dtypes):
+    """t: a contiguous CUDA tensor of this shape and one of these dtypes, on the current device."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor, not {list(t.shape)}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}")
+
+
+def _rows(name, t):
+    """(rows, columns, row stride) of a matrix whose rows are contiguous and do not overlap."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    r, c = t.shape
+    ld = t.stride(0) if r > 1 else max(c, 1)
+    if ld < c:
+        raise ValueError(f"the rows of {name} overlap")
+    return r, c, ld
+
+
+# ------------------------------------------------------------- router of a batch
+def route_balance_workspace_bytes(T, E):
+    return _lib.moe_route_balance_workspace_bytes(T, E)
+
+
+def route_balance(logits, K, idx, w, counts, n_tokens, loss, ws, renorm=False, mask=None, prob_sum=None,
+                  stream=None):
+    """Top-K, per-expert counts, balance and z loss of a batch of logits [T][E] (rows may be strided)."""
+    T, E, ld = _rows("logits", logits)
+    _dense("idx", idx, (T, K), (torch.int32,))
+    _dense("w", w, (T, K), (torch.float32,))
+    _dense("counts", counts, (E,), (torch.int32,))
+    _dense("n_tokens", n_tokens, (1,), (torch.int32,))
+    _dense("loss", loss, (2,), (torch.float32,))
+    if prob_sum is not None:
+        _dense("prob_sum", prob_sum, (E,), (torch.float32,))
+    if mask is not None:
+        _dense("mask", mask, (T,), (torch.uint8, torch.bool))
+    _call("moe_route_balance", _p(logits), T, ld, E, K, _dt("logits", logits), int(renorm), _p(mask), _p(idx),
+          _p(w), _p(counts), _p(n_tokens), _p(prob_sum), _p(loss), _p(ws), ws.numel() * ws.element_size(), _s(stream))
+
+
+def route_balance_backward(logits, idx, counts, n_tokens, d_loss, d_logits, d_w=None, renorm=False, stream=None):
+    """d_logits of route_balance, from the gradients of the gate weights and of the two losses."""
+    T, E, ld = _rows("logits", logits)
+    K = idx.shape[1]
+    _dense("idx", idx, (T, K), (torch.int32,))
+    _dense("counts", counts, (E,), (torch.int32,))
+    _dense("n_tokens", n_tokens, (1,), (torch.int32,))
+    _dense("d_loss", d_loss, (2,), (torch.float32,))
+    if d_w is not None:
+        _dense("d_w", d_w, (T, K), (torch.float32,))
+    Td, Ed, ld_d = _rows("d_logits", d_logits)
+    if (Td, Ed) != (T, E) or d_logits.dtype != logits.dtype:
+        raise ValueError("d_logits must have the shape and dtype of logits")
+    _call("moe_route_balance_backward", _p(logits), T, ld, E, K, _dt("logits", logits), int(renorm), _p(idx),
+          _p(counts), _p(n_tokens), _p(d_w), _p(d_loss), _p(d_logits), ld_d, _s(stream))
+
+
 # ------------------------------------------------------------- predictor
 def predictor_workspace_bytes(L, E, K, B):
     return _lib.stmoe_workspace_bytes(L, E, K, B)
@@ -332,6 +413,52 @@ def expert_ffn_noalloc(x, idx, w, H, I, E, dtype, expert_ptrs, y, shared_ptrs=No
     B, K = idx.shape
     _call("moe_expert_ffn_noalloc", _p(x), _p(idx), _p(w), B, K, H, I, E, dtype, _p(expert_ptrs),
           _p(shared_ptrs), n_shared, _p(y), _s(stream))
+
+
+# ------------------------------------------------------------- microscaled 4-bit floats
+def mx_quantize(x, codes, scales, stream=None):
+    """x [rows][cols] (rows may be strided) to codes [rows][ceil(cols/2)] and scales [rows][ceil(cols/32)], uint8."""
+    r, c, ld = _rows("x", x)
+    _dense("codes", codes, (r, (c + 1) // 2), (torch.uint8,))
+    _dense("scales", scales, (r, (c + 31) // 32), (torch.uint8,))
+    _call("moe_mx_quantize", _p(x), r, c, ld, _dt("x", x), _p(codes), _p(scales), _s(stream))
+
+
+def mx_dequantize(codes, scales, y, stream=None):
+    """The values of codes and scales into y [rows][cols] (rows may be strided)."""
+    r, c, ld = _rows("y", y)
+    _dense("codes", codes, (r, (c + 1) // 2), (torch.uint8,))
+    _dense("scales", scales, (r, (c + 31) // 32), (torch.uint8,))
+    _call("moe_mx_dequantize", _p(codes), _p(scales), r, c, _p(y), ld, _dt("y", y), _s(stream))
+
+
+def mx_pack_expert(gate, up, down, H, I, blob, stream=None):
+    """Pack an expert for expert_ffn_mx: gate, up [I][H] and down [H][I], each (codes, scales), into blob (device)."""
+    for name, (codes, scales), r, c in (("gate", gate, I, H), ("up", up, I, H), ("down", down, H, I)):
+        _dense(f"{name} codes", codes, (r, c // 2), (torch.uint8,))
+        _dense(f"{name} scales", scales, (r, (c + 31) // 32), (torch.uint8,))
+    _dense("blob", blob, (blob_bytes(H, I, MXFP4),), (torch.uint8,))
+    _call("moe_mx_pack_expert", _p(gate[0]), _p(gate[1]), _p(up[0]), _p(up[1]), _p(down[0]), _p(down[1]), H, I,
+          _p(blob), _s(stream))
+
+
+def ffn_mx_workspace_bytes(T, K, E, H, I, n_shared=0, dtype=torch.bfloat16, y_dtype=torch.float32):
+    """Workspace bytes for expert_ffn_mx (256-byte aligned); 0 for an invalid shape."""
+    return _lib.moe_expert_ffn_mx_workspace_bytes(T, K, E, H, I, n_shared, _DTYPES[dtype], _DTYPES[y_dtype])
+
+
+def expert_ffn_mx(x, idx, w, H, I, E, expert_ptrs, y, ws, shared_ptrs=None, n_shared=0, stream=None):
+    """The expert FFN of tokens x [T][H] over MXFP4 blobs (mx_pack_expert)."""
+    T, K = idx.shape
+    _dense("x", x, (T, H), tuple(_DTYPES))
+    _dense("idx", idx, (T, K), (torch.int32,))
+    _dense("w", w, (T, K), (torch.float32,))
+    _dense("y", y, (T, H), tuple(_DTYPES))
+    _dense("expert_ptrs", expert_ptrs, (E,), (torch.int64,))
+    if n_shared:
+        _dense("shared_ptrs", shared_ptrs, (n_shared,), (torch.int64,))
+    _call("moe_expert_ffn_mx", _p(x), _p(idx), _p(w), T, K, H, I, E, _dt("x", x), _dt("y", y), _p(expert_ptrs),
+          _p(shared_ptrs), n_shared, _p(y), _p(ws), ws.numel() * ws.element_size(), _s(stream))
 
 
 # ------------------------------------------------------------- cache policy
