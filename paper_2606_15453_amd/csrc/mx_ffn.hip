@@ -37,8 +37,20 @@ struct MxArgs {
     int32_t* ntiles;
     uint16_t* act;                  // [position][piece][I] bf16 pieces
     float* part;                    // [entry][H]
+    // decode steps (T <= 16)
+    struct DecodeSlot* slots;       // by ascending expert, the shared ones last
+    int32_t* nslots;
+    int32_t* arrived;               // [row block of H] workgroups of the down launch that are done
+    float* split;                   // [row block][split][256] their sums
     unsigned long long* n_experts;  // counts distinct routed experts (timed decode layers), or null
 };
+
+// A distinct expert of a decode step and, per token, the entry that selects it.
+struct DecodeSlot {
+    int32_t g;
+    uint8_t k[kMaxB];               // kNone: the token does not select it
+};
+constexpr int kNone = 255;
 
 // Column operand: eight consecutive values of a row as bf16 pieces.
 template <bool F32>
@@ -62,32 +74,46 @@ __device__ __forceinline__ void split(float v, __bf16& hi, __bf16& lo) {
     lo = __builtin_isfinite(h) ? __bf16(v - h) : __bf16(0.f);
 }
 
+// Eight consecutive values as loaded.
+template <bool F32>
+struct Raw {
+    uint4 q[F32 ? 2 : 1];
+};
+
+template <bool F32>
+__device__ __forceinline__ Raw<F32> load_raw(const void* x, size_t at, bool in) {
+    Raw<F32> r;
+    const uint4* s = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(x) + at * (F32 ? 4 : 2));
+#pragma unroll
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) r.q[i] = in ? s[i] : make_uint4(0u, 0u, 0u, 0u);
+    return r;
+}
+
+__device__ __forceinline__ Pieces<false> pieces(const Raw<false>& r) {
+    union {
+        uint4 q;
+        bf16x8 v;
+    } u;
+    u.q = r.q[0];
+    return Pieces<false>{{u.v}};
+}
+
+__device__ __forceinline__ Pieces<true> pieces(const Raw<true>& r) {
+    Pieces<true> o;
+    const uint32_t w[8] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w, r.q[1].x, r.q[1].y, r.q[1].z, r.q[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        __bf16 h, l;
+        split(__uint_as_float(w[i]), h, l);
+        o.p[0][i] = h;
+        o.p[1][i] = l;
+    }
+    return o;
+}
+
 template <bool F32>
 __device__ __forceinline__ Pieces<F32> load8(const void* x, size_t at, bool in) {
-    Pieces<F32> r;
-    if constexpr (!F32) {
-        union {
-            uint4 q;
-            bf16x8 v;
-        } u;
-        u.q = in ? *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(x) + at) : make_uint4(0, 0, 0, 0);
-        r.p[0] = u.v;
-    } else {
-        float v[8];
-        const float* s = reinterpret_cast<const float*>(x) + at;
-        const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float4 a = in ? *reinterpret_cast<const float4*>(s) : z, b = in ? *reinterpret_cast<const float4*>(s + 4) : z;
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            __bf16 h, l;
-            split(v[i], h, l);
-            r.p[0][i] = h;
-            r.p[1][i] = l;
-        }
-    }
-    return r;
+    return pieces(load_raw<F32>(x, at, in));
 }
 
 // The expert of an entry, or -1 where it names none or repeats an earlier
@@ -269,26 +295,315 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a) {
     }
 }
 
-struct MxLayout {
-    int tm, max_tiles;
-    size_t order, tiles, ntiles, act, part, total;
+// ---------------------------------------------------------------- decode steps
+//
+// Up to 16 tokens are the columns of one matrix instruction whatever they
+// select, so each selected expert is read once, and the down projection is one
+// product over the selected experts' concatenated rows: the gate weight goes
+// into the activation, a wave adds a slot's product to a token that selects
+// the slot, and nothing is gathered.  Both launches are bound by the weights'
+// bytes; they split the contraction over the waves of a workgroup (and, down,
+// over workgroups) so that every CU has enough of them in flight.
+
+constexpr int kUnitTiles = 2;       // tiles a wave takes at a time: 2 KiB of codes and 128 scales
+constexpr int kDownWaves = 8;
+
+struct Unit {
+    uint4 c[kUnitTiles];
+    uint32_t s;                     // the tiles' scale bytes
 };
+
+// Unit u of a row block whose codes and scales begin at c and s.  A missing
+// last tile repeats the one before it (its columns' operands are zero).
+__device__ __forceinline__ Unit load_unit(const char* c, const char* s, int u, int KT, int lane) {
+    Unit r;
+    const int t = u * kUnitTiles, t1 = t + 1 < KT ? t + 1 : t;
+    r.c[0] = *reinterpret_cast<const uint4*>(c + size_t(t) * kTileBytes + lane * 16);
+    r.c[1] = *reinterpret_cast<const uint4*>(c + size_t(t1) * kTileBytes + lane * 16);
+    const uint32_t v = *reinterpret_cast<const uint16_t*>(s + size_t(t / kGroupTiles) * kGroupBytes + lane * 4 + t % kGroupTiles);
+    r.s = t1 == t ? v & 0xffu : v;
+    return r;
+}
+
+__device__ __forceinline__ uint32_t word(const uint4& q, int s) { return s == 0 ? q.x : s == 1 ? q.y : s == 2 ? q.z : q.w; }
+
+template <bool XF, bool YF>
+__global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
+    __shared__ uint32_t present[kMaxE / 32];
+    __shared__ int entry[kMaxB * kMaxK];
+    __shared__ float red[kWaves][2][4][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int slot = blockIdx.x / nrb, rb = blockIdx.x % nrb;
+    // the slot's expert: the slot-th of those present, then the shared ones
+    if (tid < kMaxE / 32) present[tid] = 0u;
+    int mine = tid < a.T * a.K ? a.idx[tid] : -1;
+    if (mine >= a.E) mine = -1;
+    entry[tid] = mine;
+    __syncthreads();
+    if (mine >= 0) atomicOr(&present[mine >> 5], 1u << (mine & 31));
+    __syncthreads();
+    int total = 0, g = -1;
+    for (int i = 0; i < kMaxE / 32; ++i) {
+        uint32_t m = __builtin_amdgcn_readfirstlane(present[i]);
+        const int c = __builtin_popcount(m);
+        if (slot >= total && slot < total + c) {
+            for (int j = slot - total; j > 0; --j) m &= m - 1u;
+            g = 32 * i + __builtin_ctz(m);
+        }
+        total += c;
+    }
+    if (blockIdx.x == 0) {
+        if (tid == 0) {
+            *a.nslots = total + a.ns;
+            if (a.n_experts) *a.n_experts += (unsigned long long)(total);
+        }
+        for (int i = tid; i < row_blocks(a.H); i += kThreads) a.arrived[i] = 0;
+    }
+    if (g < 0) {
+        if (slot - total >= a.ns) return;
+        g = a.E + slot - total;
+    }
+    const char* blobp = expert_blob(a, g);
+    const Blob L = blob(a.H, a.I);
+    const int KT = col_tiles(a.H), KG = col_groups(a.H), KU = (KT + kUnitTiles - 1) / kUnitTiles;
+    const char* gc = blobp + L.gate + size_t(rb) * KT * kTileBytes;
+    const char* uc = blobp + L.up + size_t(rb) * KT * kTileBytes;
+    const char* gs = blobp + L.gate_s + size_t(rb) * KG * kGroupBytes;
+    const char* us = blobp + L.up_s + size_t(rb) * KG * kGroupBytes;
+    Unit ng{}, nu{};
+    if (wave < KU) {
+        ng = load_unit(gc, gs, wave, KT, lane);
+        nu = load_unit(uc, us, wave, KT, lane);
+    }
+    // lane: token c; its first entry that selects the expert
+    const int c = lane & 15, q = lane >> 4;
+    int k = kNone;
+    if (c < a.T) {
+        if (g >= a.E) k = a.K + g - a.E;
+        else
+            for (int j = a.K - 1; j >= 0; --j)
+                if (entry[c * a.K + j] == g) k = j;
+    }
+    const bool live = k != kNone;
+    if (rb == 0 && tid < kMaxB) {
+        if (tid == 0) a.slots[slot].g = g;
+        a.slots[slot].k[tid] = uint8_t(k);
+    }
+    const size_t xrow = live ? size_t(c) * a.H : 0;
+    f32x4 ag = {0.f, 0.f, 0.f, 0.f}, au = {0.f, 0.f, 0.f, 0.f};
+    for (int u = wave; u < KU; u += kWaves) {
+        const Unit cg = ng, cu = nu;
+        // the unit's columns before the next weights: loads return in order,
+        // and the wait for the columns then leaves the weights in flight
+        Raw<XF> xr[kUnitTiles][4];
+#pragma unroll
+        for (int j = 0; j < kUnitTiles; ++j)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int at = (u * kUnitTiles + j) * kTileCols + q * kBlock + s * 8;
+                xr[j][s] = load_raw<XF>(a.x, xrow + at, live && at < a.H);
+            }
+        if (u + kWaves < KU) {
+            ng = load_unit(gc, gs, u + kWaves, KT, lane);
+            nu = load_unit(uc, us, u + kWaves, KT, lane);
+        }
+#pragma unroll
+        for (int j = 0; j < kUnitTiles; ++j) {
+            const float sg = scale_of(cg.s >> (8 * j) & 0xffu), su = scale_of(cu.s >> (8 * j) & 0xffu);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const Pieces<XF> xv = pieces(xr[j][s]);
+                const bf16x8 gv = decode8(word(cg.c[j], s), sg), uv = decode8(word(cu.c[j], s), su);
+#pragma unroll
+                for (int p = 0; p < Pieces<XF>::N; ++p) {
+                    ag = __builtin_amdgcn_mfma_f32_16x16x32_bf16(gv, xv.p[p], ag, 0, 0, 0);
+                    au = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uv, xv.p[p], au, 0, 0, 0);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        red[wave][0][r][lane] = ag[r];
+        red[wave][1][r][lane] = au[r];
+    }
+    __syncthreads();
+    // wave r: rows 4 q + r of the block
+    float gsum = 0.f, usum = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+        gsum += red[v][0][wave][lane];
+        usum += red[v][1][wave][lane];
+    }
+    const int row = rb * kTileRows + 4 * q + wave;
+    if (!live || row >= a.I) return;
+    const float w = k < a.K ? a.w[c * a.K + k] : 1.f;
+    const float h = gsum / (1.f + expf(-gsum)) * usum * w;
+    constexpr int NP = Pieces<YF>::N;
+    __bf16* o = reinterpret_cast<__bf16*>(a.act) + size_t(c * a.ks + k) * NP * a.I + row;
+    if constexpr (YF) {
+        __bf16 hi, lo;
+        split(h, hi, lo);
+        o[0] = hi;
+        o[a.I] = lo;
+    } else {
+        o[0] = __bf16(h);
+    }
+}
+
+// PC: up to eight tokens with two pieces each: the pieces are columns too.
+template <bool YF, bool PC>
+__global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int splits) {
+    constexpr int NP = Pieces<YF>::N, MP = PC ? 1 : NP;     // pieces; instructions per operand
+    __shared__ const char* base[kMaxE + kMaxShared];
+    __shared__ uint8_t sk[kMaxE + kMaxShared][kMaxB];
+    __shared__ float red[kDownWaves][4][64];
+    __shared__ int last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int rb = blockIdx.x / splits, sp = blockIdx.x % splits;
+    const int S = *a.nslots;
+    for (int s = tid; s < S; s += 64 * kDownWaves) {
+        const DecodeSlot d = a.slots[s];
+        base[s] = expert_blob(a, d.g);
+#pragma unroll
+        for (int t = 0; t < kMaxB; ++t) sk[s][t] = d.k[t];
+    }
+    __syncthreads();
+    const Blob L = blob(a.H, a.I);
+    const int KT = col_tiles(a.I), KG = col_groups(a.I), KU = (KT + kUnitTiles - 1) / kUnitTiles;
+    const size_t co = L.down + size_t(rb) * KT * kTileBytes, so = L.down_s + size_t(rb) * KG * kGroupBytes;
+    const int c = lane & 15, q = lane >> 4;
+    const int t = PC ? c >> 1 : c, pc = PC ? c & 1 : 0;
+    const int units = S * KU, step = splits * kDownWaves;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    Unit nx{};
+    int u = sp * kDownWaves + wave;
+    if (u < units) {
+        const int s = u / KU;
+        nx = load_unit(base[s] + co, base[s] + so, u - s * KU, KT, lane);
+    }
+    for (; u < units; u += step) {
+        const Unit cur = nx;
+        const int slot = u / KU, t0 = (u - slot * KU) * kUnitTiles;
+        const int k = sk[slot][t];
+        const bool live = k != kNone;
+        const size_t arow = live ? (size_t(t * a.ks + k) * NP + pc) * a.I : 0;
+        Raw<false> h[kUnitTiles][4][MP];
+#pragma unroll
+        for (int j = 0; j < kUnitTiles; ++j)
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int p = 0; p < MP; ++p) {
+                    const int at = (t0 + j) * kTileCols + q * kBlock + s * 8;
+                    h[j][s][p] = load_raw<false>(a.act, arow + size_t(p) * a.I + at, live && at < a.I);
+                }
+        if (u + step < units) {
+            const int s = (u + step) / KU;
+            nx = load_unit(base[s] + co, base[s] + so, u + step - s * KU, KT, lane);
+        }
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kUnitTiles; ++j) {
+            const float sd = scale_of(cur.s >> (8 * j) & 0xffu);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const bf16x8 dv = decode8(word(cur.c[j], s), sd);
+#pragma unroll
+                for (int p = 0; p < MP; ++p)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dv, pieces(h[j][s][p]).p[0], acc, 0, 0, 0);
+            }
+        }
+        // only to the tokens that select the slot: a NaN among its weights stays theirs
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] += live ? acc[r] : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) red[wave][r][lane] = sum[r];
+    __syncthreads();
+    const int r = wave & 3;
+    float v = 0.f;
+#pragma unroll
+    for (int x = 0; x < kDownWaves; ++x) v += red[x][r][lane];
+    if (splits > 1) {
+        // the row block's last workgroup adds the others' sums, in their order;
+        // stores and loads at device scope, the count after the stores are done
+        float* mine = a.split + (size_t(rb) * splits + sp) * 256;
+        if (wave < 4) __hip_atomic_store(&mine[r * 64 + lane], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0)
+            last = __hip_atomic_fetch_add(&a.arrived[rb], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
+        __syncthreads();
+        if (!last || wave >= 4) return;
+        v = 0.f;
+        for (int x = 0; x < splits; ++x)
+            v += __hip_atomic_load(&a.split[(size_t(rb) * splits + x) * 256 + r * 64 + lane], __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (wave >= 4) return;
+    if constexpr (PC) v += __shfl_xor(v, 1, 64);
+    const int row = rb * kTileRows + 4 * q + r;
+    if (t >= a.T || pc || row >= a.H) return;
+    if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = v;
+    else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(v);
+}
+
+struct MxLayout {
+    int tm, max_tiles, slots, splits;
+    size_t order, tiles, ntiles, act, part, plan, nslots, arrived, split, total;
+};
+
+// Workgroups of the down launch per row block: 512 in all.
+int down_splits(int H) {
+    const int rb = row_blocks(H);
+    return rb >= 512 ? 1 : (512 + rb - 1) / rb < 16 ? (512 + rb - 1) / rb : 16;
+}
 
 MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int ydtype) {
     MxLayout y{};
     const size_t n = size_t(T) * (K + ns);
-    y.tm = 16;
-    const size_t most = (n + y.tm - 1) / y.tm + E + ns;
-    y.max_tiles = int(most < n ? most : n);
     size_t off = 0;
     auto take = [&](size_t b) { const size_t at = off; off = (off + b + 255) / 256 * 256; return at; };
-    y.order = take(n * sizeof(int32_t));
-    y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
-    y.ntiles = take(sizeof(int32_t));
     y.act = take(n * (ydtype == STMOE_F32 ? 2 : 1) * I * sizeof(uint16_t));
-    y.part = take(n * H * sizeof(float));
+    if (T <= kMaxB) {
+        y.slots = (E < T * K ? E : T * K) + ns;
+        y.splits = down_splits(H);
+        y.plan = take(size_t(y.slots) * sizeof(DecodeSlot));
+        y.nslots = take(sizeof(int32_t));
+        y.arrived = take(size_t(row_blocks(H)) * sizeof(int32_t));
+        y.split = take(size_t(row_blocks(H)) * y.splits * 256 * sizeof(float));
+    } else {
+        y.tm = 16;
+        const size_t most = (n + y.tm - 1) / y.tm + E + ns;
+        y.max_tiles = int(most < n ? most : n);
+        y.order = take(n * sizeof(int32_t));
+        y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
+        y.ntiles = take(sizeof(int32_t));
+        y.part = take(n * H * sizeof(float));
+    }
     y.total = off;
     return y;
+}
+
+template <bool XF, bool YF>
+int launch_decode(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t ev_mid) {
+    const int rb = row_blocks(a.I);
+    hipLaunchKernelGGL((mx_up_decode<XF, YF>), dim3(unsigned(rb * L.slots)), dim3(kThreads), 0, s, a, rb);
+    STMOE_LAUNCHED();
+    if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
+    const dim3 grid(unsigned(row_blocks(a.H) * L.splits)), block(64 * kDownWaves);
+    if constexpr (YF) {
+        if (a.T <= kMaxB / 2) {
+            hipLaunchKernelGGL((mx_down_decode<YF, true>), grid, block, 0, s, a, L.splits);
+            STMOE_LAUNCHED();
+            return STMOE_OK;
+        }
+    }
+    hipLaunchKernelGGL((mx_down_decode<YF, false>), grid, block, 0, s, a, L.splits);
+    STMOE_LAUNCHED();
+    return STMOE_OK;
 }
 
 template <bool XF, bool YF>
@@ -334,10 +649,19 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
     a.tiles = reinterpret_cast<int4*>(base + L.tiles);
     a.ntiles = reinterpret_cast<int32_t*>(base + L.ntiles);
     a.act = reinterpret_cast<uint16_t*>(base + L.act);
+    a.slots = reinterpret_cast<DecodeSlot*>(base + L.plan);
+    a.nslots = reinterpret_cast<int32_t*>(base + L.nslots);
+    a.arrived = reinterpret_cast<int32_t*>(base + L.arrived);
+    a.split = reinterpret_cast<float*>(base + L.split);
     a.part = reinterpret_cast<float*>(base + L.part);
     a.n_experts = n_experts;
-    if (dtype == STMOE_F32) return ydtype == STMOE_F32 ? launch_direct<true, true>(a, L, s, ev_mid) : launch_direct<true, false>(a, L, s, ev_mid);
-    return ydtype == STMOE_F32 ? launch_direct<false, true>(a, L, s, ev_mid) : launch_direct<false, false>(a, L, s, ev_mid);
+    const bool xf = dtype == STMOE_F32, yf = ydtype == STMOE_F32;
+    if (T <= kMaxB) {
+        if (xf) return yf ? launch_decode<true, true>(a, L, s, ev_mid) : launch_decode<true, false>(a, L, s, ev_mid);
+        return yf ? launch_decode<false, true>(a, L, s, ev_mid) : launch_decode<false, false>(a, L, s, ev_mid);
+    }
+    if (xf) return yf ? launch_direct<true, true>(a, L, s, ev_mid) : launch_direct<true, false>(a, L, s, ev_mid);
+    return yf ? launch_direct<false, true>(a, L, s, ev_mid) : launch_direct<false, false>(a, L, s, ev_mid);
 }
 
 }  // namespace stmoe
