@@ -32,10 +32,11 @@ struct MxArgs {
     int T, K, H, I, E, ns, ks;      // ks = K + ns: entries per token
     int tm;                         // tokens per tile
     // workspace
-    int32_t* order;                 // [T * ks] entries (t * ks + k) by expert
-    int4* tiles;                    // (expert, first position, tokens, -)
+    int32_t* order;                 // [expert][T] its entries (t * ks + k)
+    int32_t* cnt;                   // [expert] how many
+    int4* tiles;                    // (expert, first place in its order, tokens, -)
     int32_t* ntiles;
-    uint16_t* act;                  // [position][piece][I] bf16 pieces
+    uint16_t* act;                  // [entry][piece][I] bf16 pieces
     float* part;                    // [entry][H]
     // decode steps (T <= 16)
     struct DecodeSlot* slots;       // by ascending expert, the shared ones last
@@ -111,11 +112,6 @@ __device__ __forceinline__ Pieces<true> pieces(const Raw<true>& r) {
     return o;
 }
 
-template <bool F32>
-__device__ __forceinline__ Pieces<F32> load8(const void* x, size_t at, bool in) {
-    return pieces(load_raw<F32>(x, at, in));
-}
-
 // The expert of an entry, or -1 where it names none or repeats an earlier
 // entry of its token (the first one counts).
 __device__ __forceinline__ int entry_expert(const MxArgs& a, int t, int k) {
@@ -128,39 +124,97 @@ __device__ __forceinline__ int entry_expert(const MxArgs& a, int t, int k) {
     return e;
 }
 
-// Entries by expert and the tiles of at most tm tokens: one workgroup.  The
-// order within an expert is that of the atomics; a token's results do not
-// depend on its place.
-__global__ __launch_bounds__(kPlanThreads) void mx_plan_kernel(MxArgs a) {
-    __shared__ int cnt[kMaxGroups], base[kMaxGroups], tile[kMaxGroups];
-    const int G = a.E + a.ns, n = a.T * a.ks;
-    for (int g = threadIdx.x; g < G; g += kPlanThreads) cnt[g] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-        const int e = entry_expert(a, i / a.ks, i % a.ks);
-        if (e >= 0) atomicAdd(&cnt[e], 1);
+// Entries of one expert per workgroup, any order (a token's results do not
+// depend on its place): order[g * T ..] and cnt[g].
+__global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
+    __shared__ int at;
+    const int g = blockIdx.x, lane = threadIdx.x & 63;
+    int32_t* out = a.order + size_t(g) * a.T;
+    if (g >= a.E) {
+        for (int t = threadIdx.x; t < a.T; t += kPlanThreads) out[t] = t * a.ks + a.K + (g - a.E);
+        if (threadIdx.x == 0) a.cnt[g] = a.T;
+        return;
     }
+    if (threadIdx.x == 0) at = 0;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int at = 0, nt = 0, used = 0;
-        for (int g = 0; g < G; ++g) {
-            used += g < a.E && cnt[g] > 0;
-            base[g] = at;
-            tile[g] = nt;
-            at += cnt[g];
-            nt += (cnt[g] + a.tm - 1) / a.tm;
+    const int n = a.T * a.K;
+    for (int i0 = 0; i0 < n; i0 += 4 * kPlanThreads) {
+        // four entries per thread, a wave's consecutive ones together
+        int e[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int i = i0 + v * kPlanThreads + threadIdx.x;
+            e[v] = i < n ? a.idx[i] : -1;
         }
-        *a.ntiles = nt;
-        if (a.n_experts) *a.n_experts += (unsigned long long)(used);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int i = i0 + v * kPlanThreads + threadIdx.x;
+            bool hit = e[v] == g;
+            int t = 0, k = 0;
+            if (hit) {
+                t = i / a.K;
+                k = i - t * a.K;
+                for (int j = 0; j < k; ++j) hit &= a.idx[size_t(t) * a.K + j] != g;
+            }
+            const unsigned long long m = __ballot(hit);
+            if (!m) continue;
+            int base = 0;
+            if (lane == 0) base = atomicAdd(&at, __popcll(m));
+            base = __builtin_amdgcn_readfirstlane(base);
+            if (hit) out[base + __popcll(m & ((1ull << lane) - 1ull))] = t * a.ks + k;
+        }
     }
     __syncthreads();
-    for (int g = threadIdx.x; g < G; g += kPlanThreads)
-        for (int j = 0; j * a.tm < cnt[g]; ++j)
-            a.tiles[tile[g] + j] = make_int4(g, base[g] + j * a.tm, min(a.tm, cnt[g] - j * a.tm), 0);
+    if (threadIdx.x == 0) a.cnt[g] = at;
+}
+
+// The tiles of at most tm tokens, experts in order: one workgroup.
+__global__ __launch_bounds__(kPlanThreads) void mx_tiles_kernel(MxArgs a) {
+    __shared__ int cnt[kMaxGroups], tile[kMaxGroups + 1];
+    const int G = a.E + a.ns;
+    for (int g = threadIdx.x; g < G; g += kPlanThreads) cnt[g] = a.cnt[g];
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-        const int e = entry_expert(a, i / a.ks, i % a.ks);
-        if (e >= 0) a.order[atomicAdd(&base[e], 1)] = i;
+    if (threadIdx.x < 64) {
+        // running sums of the tile counts, 64 experts at a time
+        int before = 0, used = 0;
+        for (int g0 = 0; g0 < G; g0 += 64) {
+            const int g = g0 + threadIdx.x, c = g < G ? cnt[g] : 0;
+            int v = (c + a.tm - 1) / a.tm;
+            used += __popcll(__ballot(c > 0 && g < a.E));
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(v, d, 64);
+                if (int(threadIdx.x) >= d) v += o;
+            }
+            if (g < G) tile[g + 1] = before + v;
+            before += __shfl(v, 63, 64);
+        }
+        if (threadIdx.x == 0) {
+            tile[0] = 0;
+            *a.ntiles = before;
+            if (a.n_experts) *a.n_experts += (unsigned long long)(used);
+        }
+    }
+    __syncthreads();
+    for (int g = threadIdx.x >> 4; g < G; g += kPlanThreads >> 4)
+        for (int j = threadIdx.x & 15; j * a.tm < cnt[g]; j += 16)
+            a.tiles[tile[g] + j] = make_int4(g, j * a.tm, min(a.tm, cnt[g] - j * a.tm), 0);
+}
+
+// fp32 hidden states as two bf16 pieces per row: [T][2][H].
+__global__ __launch_bounds__(kThreads) void mx_split_kernel(const float* x, int64_t n4, int H4, uint16_t* o) {
+    for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n4; i += int64_t(gridDim.x) * kThreads) {
+        const float4 v = reinterpret_cast<const float4*>(x)[i];
+        const int64_t t = i / H4;
+        union {
+            __bf16 b[4];
+            uint2 q;
+        } hi, lo;
+        split(v.x, hi.b[0], lo.b[0]);
+        split(v.y, hi.b[1], lo.b[1]);
+        split(v.z, hi.b[2], lo.b[2]);
+        split(v.w, hi.b[3], lo.b[3]);
+        reinterpret_cast<uint2*>(o)[i + t * H4] = hi.q;
+        reinterpret_cast<uint2*>(o)[i + t * H4 + H4] = lo.q;
     }
 }
 
@@ -168,104 +222,157 @@ __device__ __forceinline__ const char* expert_blob(const MxArgs& a, int g) {
     return reinterpret_cast<const char*>(g < a.E ? a.eptr[g] : a.sptr[g - a.E]);
 }
 
-// Gate and up rows of one 16-row block and 16 tokens per wave; activations
-// silu(g) * u as bf16 pieces.
-template <bool XF, bool YF>
-__global__ __launch_bounds__(kThreads) void mx_up_direct(MxArgs a, int nb) {
-    const int tix = blockIdx.x / nb;
-    if (tix >= *a.ntiles) return;
-    const int4 tl = a.tiles[tix];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int rb = int(blockIdx.x % nb) * kWaves + wave;
-    if (rb >= row_blocks(a.I)) return;
-    const char* blobp = expert_blob(a, tl.x);
-    const Blob L = blob(a.H, a.I);
-    const int KT = col_tiles(a.H), KG = col_groups(a.H);
-    const char* gc = blobp + L.gate + size_t(rb) * KT * kTileBytes + lane * 16;
-    const char* uc = blobp + L.up + size_t(rb) * KT * kTileBytes + lane * 16;
-    const char* gs = blobp + L.gate_s + size_t(rb) * KG * kGroupBytes + lane * 4;
-    const char* us = blobp + L.up_s + size_t(rb) * KG * kGroupBytes + lane * 4;
-    const int c = lane & 15, q = lane >> 4;
-    const bool live = c < tl.z;
-    const size_t xrow = live ? size_t(a.order[tl.y + c] / a.ks) * a.H : 0;
-    f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = {0.f, 0.f, 0.f, 0.f};
-    for (int kt = 0; kt < KT; ++kt) {
-        const uint4 gq = *reinterpret_cast<const uint4*>(gc + size_t(kt) * kTileBytes);
-        const uint4 uq = *reinterpret_cast<const uint4*>(uc + size_t(kt) * kTileBytes);
-        const float sg = scale_of(*reinterpret_cast<const uint8_t*>(gs + (kt / kGroupTiles) * kGroupBytes + kt % kGroupTiles));
-        const float su = scale_of(*reinterpret_cast<const uint8_t*>(us + (kt / kGroupTiles) * kGroupBytes + kt % kGroupTiles));
-        const uint32_t gw[4] = {gq.x, gq.y, gq.z, gq.w}, uw[4] = {uq.x, uq.y, uq.z, uq.w};
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int k = kt * kTileCols + q * kBlock + s * 8;
-            const Pieces<XF> xv = load8<XF>(a.x, xrow + k, live && k < a.H);
-            const bf16x8 gv = decode8(gw[s], sg), uv = decode8(uw[s], su);
-#pragma unroll
-            for (int p = 0; p < Pieces<XF>::N; ++p) {
-                g = __builtin_amdgcn_mfma_f32_16x16x32_bf16(gv, xv.p[p], g, 0, 0, 0);
-                u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uv, xv.p[p], u, 0, 0, 0);
-            }
-        }
-    }
-    // lane: token c, rows 4 q .. 4 q + 3 of the block
-    const int row = rb * kTileRows + 4 * q;
-    if (!live || row >= a.I) return;
-    constexpr int NP = Pieces<YF>::N;
-    union {
-        __bf16 h[4];
-        uint2 v;
-    } o[NP];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float v = g[i] / (1.f + expf(-g[i])) * u[i];
-        if constexpr (YF) split(v, o[0].h[i], o[1].h[i]);
-        else o[0].h[i] = __bf16(v);
-    }
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-        *reinterpret_cast<uint2*>(a.act + (size_t(tl.y + c) * NP + p) * a.I + row) = o[p].v;
-}
+__device__ __forceinline__ uint32_t word(const uint4& q, int s) { return s == 0 ? q.x : s == 1 ? q.y : s == 2 ? q.z : q.w; }
 
-// Down rows of one 16-row block and 16 entries per wave, times the gate
-// weight, to the entries' partial rows.
-template <bool YF>
-__global__ __launch_bounds__(kThreads) void mx_down_direct(MxArgs a, int nb) {
-    constexpr int NP = Pieces<YF>::N;
-    const int tix = blockIdx.x / nb;
-    if (tix >= *a.ntiles) return;
+// ---------------------------------------------------------------- prompts
+//
+// A workgroup multiplies 256 weight rows (128 of gate and the same of up, or
+// 256 of down) with a tile of up to 16 NT tokens of one expert.  Each wave
+// holds 64 rows: their codes go from global memory to its registers and are
+// decoded there, once for all tokens of the tile; the tokens' columns pass
+// through LDS, 128 at a time, double-buffered.  A column's 256 bytes lie as 16
+// chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
+// lanes of a read, one chunk of 16 tokens, meet 16 different places.
+template <bool UP, int NP, int NT, bool YF>
+__global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxArgs a, int nb) {
+    constexpr int TM = 16 * NT;
+    constexpr int RB = 4;                                   // row blocks per wave
+    constexpr int CH = kTileCols / 8;                       // chunks per column
+    __shared__ u32x4 xs[2][TM * CH];
+    __shared__ int ent[TM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // consecutive work on one XCD (workgroup i runs on XCD i % 8): the row
+    // blocks of a tile and the tiles of an expert share its L2
+    const int work = *a.ntiles * nb, per = (work + 7) / 8;
+    const int id = int(blockIdx.x % 8) * per + int(blockIdx.x / 8);
+    if (int(blockIdx.x / 8) >= per || id >= work) return;
+    const int tix = id / nb, bk = id - tix * nb;
     const int4 tl = a.tiles[tix];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int rb = int(blockIdx.x % nb) * kWaves + wave;
-    if (rb >= row_blocks(a.H)) return;
     const char* blobp = expert_blob(a, tl.x);
     const Blob L = blob(a.H, a.I);
-    const int KT = col_tiles(a.I), KG = col_groups(a.I);
-    const char* dc = blobp + L.down + size_t(rb) * KT * kTileBytes + lane * 16;
-    const char* ds = blobp + L.down_s + size_t(rb) * KG * kGroupBytes + lane * 4;
-    const int c = lane & 15, q = lane >> 4;
-    const bool live = c < tl.z;
-    const size_t arow = live ? size_t(tl.y + c) * NP * a.I : 0;
-    f32x4 d = {0.f, 0.f, 0.f, 0.f};
-    for (int kt = 0; kt < KT; ++kt) {
-        const uint4 dq = *reinterpret_cast<const uint4*>(dc + size_t(kt) * kTileBytes);
-        const float sd = scale_of(*reinterpret_cast<const uint8_t*>(ds + (kt / kGroupTiles) * kGroupBytes + kt % kGroupTiles));
-        const uint32_t dw[4] = {dq.x, dq.y, dq.z, dq.w};
+    const int C = UP ? a.H : a.I, R = UP ? a.I : a.H;
+    const int KT = col_tiles(C), KG = col_groups(C), NB = row_blocks(R);
+    if (tid < TM) ent[tid] = a.order[size_t(tl.x) * a.T + tl.y + min(tid, tl.z - 1)];
+    // the wave's row blocks; beyond the matrix the last one again, not stored
+    const char *wc[RB], *wsc[RB];
+    int rb[RB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+        rb[i] = UP ? bk * 8 + wave * 2 + (i & 1) : bk * 16 + wave * 4 + i;
+        const int b = min(rb[i], NB - 1);
+        const size_t co = UP ? (i < 2 ? L.gate : L.up) : L.down, so = UP ? (i < 2 ? L.gate_s : L.up_s) : L.down_s;
+        wc[i] = blobp + co + size_t(b) * KT * kTileBytes;
+        wsc[i] = blobp + so + size_t(b) * KG * kGroupBytes;
+    }
+    __syncthreads();
+    // thread: chunk tid % 16 of tokens tid / 16 + 16 j
+    const u32x4* cols = reinterpret_cast<const u32x4*>(UP ? a.x : a.act);
+    uint32_t src[NT];                                       // in chunks
+    const int chunk = tid % CH;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int e = ent[tid / CH + 16 * j];
+        src[j] = uint32_t(UP ? e / a.ks : e) * uint32_t(NP * C / 8);
+    }
+    const int put = tid / CH * CH + (chunk ^ (tid / CH & 15));
+    u32x4 xr[NT], wn[RB];
+    uint32_t sn[RB];
+    // iteration it: piece it % NP of column tile it / NP.  Chunks beyond the
+    // row's end read its first one: their codes are zero, and if the row holds
+    // a NaN or an infinity its results are not finite without it too.
+    auto load = [&](int it) __attribute__((always_inline)) {
+        const int kt = it / NP, p = it - kt * NP;
+        const int at = kt * kTileCols + chunk * 8;
+        const uint32_t off = uint32_t(p * C + (at < C ? at : 0)) / 8;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) xr[j] = cols[src[j] + off];
+#pragma unroll
+        for (int i = 0; i < RB; ++i) {
+            wn[i] = *reinterpret_cast<const u32x4*>(wc[i] + size_t(kt) * kTileBytes + lane * 16);
+            sn[i] = *reinterpret_cast<const uint8_t*>(wsc[i] + size_t(kt / kGroupTiles) * kGroupBytes + kt % kGroupTiles +
+                                                      lane * 4);
+        }
+    };
+    f32x4 acc[RB][NT];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int c = lane & 15, q = lane >> 4, iters = KT * NP;
+    load(0);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) xs[0][put + j * 16 * CH] = xr[j];
+    for (int it = 0; it < iters; ++it) {
+        u32x4 w[RB];
+        float sc[RB];
+#pragma unroll
+        for (int i = 0; i < RB; ++i) {
+            w[i] = wn[i];
+            sc[i] = scale_of(sn[i]);
+        }
+        __syncthreads();
+        if (it + 1 < iters) load(it + 1);
+        const u32x4* buf = xs[it & 1] + c * CH;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int k = kt * kTileCols + q * kBlock + s * 8;
-            const bf16x8 dv = decode8(dw[s], sd);
+            bf16x8 wv[RB];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                const Pieces<false> h = load8<false>(a.act, arow + size_t(p) * a.I + k, live && k < a.I);
-                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dv, h.p[0], d, 0, 0, 0);
+            for (int i = 0; i < RB; ++i) wv[i] = decode8(w[i][s], sc[i]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                union {
+                    u32x4 u;
+                    bf16x8 v;
+                } b;
+                b.u = buf[n * 16 * CH + ((q * 4 + s) ^ c)];
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+                    acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], b.v, acc[i][n], 0, 0, 0);
+            }
+        }
+        if (it + 1 < iters) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) xs[(it + 1) & 1][put + j * 16 * CH] = xr[j];
+        }
+    }
+    // lane: token 16 n + c, rows 4 q .. 4 q + 3 of each block
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (16 * n + c >= tl.z) continue;
+        const int e = ent[16 * n + c];
+        if constexpr (UP) {
+            constexpr int NH = Pieces<YF>::N;
+#pragma unroll
+            for (int i = 0; i < RB / 2; ++i) {
+                const int row = rb[i] * kTileRows + 4 * q;
+                if (row >= a.I) continue;
+                union {
+                    __bf16 h[4];
+                    uint2 v;
+                } o[NH];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float g = acc[i][n][r], v = g / (1.f + expf(-g)) * acc[i + 2][n][r];
+                    if constexpr (YF) split(v, o[0].h[r], o[1].h[r]);
+                    else o[0].h[r] = __bf16(v);
+                }
+#pragma unroll
+                for (int p = 0; p < NH; ++p)
+                    *reinterpret_cast<uint2*>(a.act + (size_t(e) * NH + p) * a.I + row) = o[p].v;
+            }
+        } else {
+            const int t = e / a.ks, k = e - t * a.ks;
+            const float w = k < a.K ? a.w[size_t(t) * a.K + k] : 1.f;
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                const int row = rb[i] * kTileRows + 4 * q;
+                if (row >= a.H) continue;
+                const f32x4 d = acc[i][n];
+                *reinterpret_cast<float4*>(a.part + size_t(e) * a.H + row) =
+                    make_float4(w * d[0], w * d[1], w * d[2], w * d[3]);
             }
         }
     }
-    const int row = rb * kTileRows + 4 * q;
-    if (!live || row >= a.H) return;
-    const int entry = a.order[tl.y + c], t = entry / a.ks, k = entry % a.ks;
-    const float w = k < a.K ? a.w[size_t(t) * a.K + k] : 1.f;
-    *reinterpret_cast<float4*>(a.part + size_t(entry) * a.H + row) = make_float4(w * d[0], w * d[1], w * d[2], w * d[3]);
 }
 
 // y[t] = the sum of its entries' rows, in the entries' order.
@@ -324,8 +431,6 @@ __device__ __forceinline__ Unit load_unit(const char* c, const char* s, int u, i
     r.s = t1 == t ? v & 0xffu : v;
     return r;
 }
-
-__device__ __forceinline__ uint32_t word(const uint4& q, int s) { return s == 0 ? q.x : s == 1 ? q.y : s == 2 ? q.z : q.w; }
 
 template <bool XF, bool YF>
 __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
@@ -552,7 +657,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int 
 
 struct MxLayout {
     int tm, max_tiles, slots, splits;
-    size_t order, tiles, ntiles, act, part, plan, nslots, arrived, split, total;
+    size_t order, cnt, tiles, ntiles, act, part, xs, plan, nslots, arrived, split, total;
 };
 
 // Workgroups of the down launch per row block: 512 in all.
@@ -561,7 +666,13 @@ int down_splits(int H) {
     return rb >= 512 ? 1 : (512 + rb - 1) / rb < 16 ? (512 + rb - 1) / rb : 16;
 }
 
-MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int ydtype) {
+// Tokens per tile: by the tokens an expert gets on average.
+int tile_tokens(int T, int K, int E) {
+    const int mean = T * K / E;
+    return mean > 64 ? 128 : mean > 32 ? 64 : mean > 16 ? 32 : 16;
+}
+
+MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydtype) {
     MxLayout y{};
     const size_t n = size_t(T) * (K + ns);
     size_t off = 0;
@@ -575,13 +686,16 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int ydtype) {
         y.arrived = take(size_t(row_blocks(H)) * sizeof(int32_t));
         y.split = take(size_t(row_blocks(H)) * y.splits * 256 * sizeof(float));
     } else {
-        y.tm = 16;
-        const size_t most = (n + y.tm - 1) / y.tm + E + ns;
+        y.tm = tile_tokens(T, K, E);
+        // a full tile takes tm entries; each expert has at most one that is not full
+        const size_t most = n / y.tm + E + ns;
         y.max_tiles = int(most < n ? most : n);
-        y.order = take(n * sizeof(int32_t));
+        y.order = take(size_t(E + ns) * T * sizeof(int32_t));
+        y.cnt = take(size_t(E + ns) * sizeof(int32_t));
         y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
         y.ntiles = take(sizeof(int32_t));
         y.part = take(n * H * sizeof(float));
+        if (dtype == STMOE_F32) y.xs = take(size_t(T) * H * 2 * sizeof(uint16_t));
     }
     y.total = off;
     return y;
@@ -606,16 +720,39 @@ int launch_decode(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t 
     return STMOE_OK;
 }
 
-template <bool XF, bool YF>
-int launch_direct(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t ev_mid) {
-    hipLaunchKernelGGL(mx_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
-    STMOE_LAUNCHED();
-    const int ub = (row_blocks(a.I) + kWaves - 1) / kWaves, db = (row_blocks(a.H) + kWaves - 1) / kWaves;
-    hipLaunchKernelGGL((mx_up_direct<XF, YF>), dim3(unsigned(ub * L.max_tiles)), dim3(kThreads), 0, s, a, ub);
+template <bool XF, bool YF, int NT>
+int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t ev_mid) {
+    // rounded up to the eight XCDs
+    const auto grid = [&](int nb) { return dim3(unsigned((int64_t(L.max_tiles) * nb + 7) / 8 * 8)); };
+    const int ub = (a.I + 127) / 128, db = (a.H + 255) / 256;
+    hipLaunchKernelGGL((mx_tile_kernel<true, XF ? 2 : 1, NT, YF>), grid(ub), dim3(kThreads), 0, s, a, ub);
     STMOE_LAUNCHED();
     if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
-    hipLaunchKernelGGL((mx_down_direct<YF>), dim3(unsigned(db * L.max_tiles)), dim3(kThreads), 0, s, a, db);
+    hipLaunchKernelGGL((mx_tile_kernel<false, YF ? 2 : 1, NT, YF>), grid(db), dim3(kThreads), 0, s, a, db);
     STMOE_LAUNCHED();
+    return STMOE_OK;
+}
+
+template <bool XF, bool YF>
+int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream_t s, hipEvent_t ev_mid) {
+    MxArgs a = args;
+    hipLaunchKernelGGL(mx_order_kernel, dim3(unsigned(a.E + a.ns)), dim3(kPlanThreads), 0, s, a);
+    STMOE_LAUNCHED();
+    hipLaunchKernelGGL(mx_tiles_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    STMOE_LAUNCHED();
+    if constexpr (XF) {
+        const int64_t n4 = int64_t(a.T) * a.H / 4, wg = (n4 + kThreads - 1) / kThreads;
+        hipLaunchKernelGGL(mx_split_kernel, dim3(unsigned(wg < 8192 ? wg : 8192)), dim3(kThreads), 0, s,
+                           reinterpret_cast<const float*>(a.x), n4, a.H / 4, xs);
+        STMOE_LAUNCHED();
+        a.x = xs;
+    }
+    int rc = STMOE_OK;
+    if (L.tm == 128) rc = launch_tiles<XF, YF, 8>(a, L, s, ev_mid);
+    else if (L.tm == 64) rc = launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
+    else if (L.tm == 32) rc = launch_tiles<XF, YF, 2>(a, L, s, ev_mid);
+    else rc = launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
+    if (rc) return rc;
     hipLaunchKernelGGL((mx_sum_kernel<YF>), dim3(unsigned(a.T)), dim3(kThreads), 0, s, a);
     STMOE_LAUNCHED();
     return STMOE_OK;
@@ -628,7 +765,7 @@ int launch_direct(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t 
 int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int K, int H, int I, int E, int dtype,
                   int ydtype, const void* const* eptr, const void* const* sptr, int n_shared, void* y, void* ws,
                   hipStream_t s, unsigned long long* n_experts, hipEvent_t ev_mid) {
-    const MxLayout L = mx_layout(T, K, E, H, I, n_shared, ydtype);
+    const MxLayout L = mx_layout(T, K, E, H, I, n_shared, dtype, ydtype);
     char* base = reinterpret_cast<char*>(ws);
     MxArgs a{};
     a.x = x;
@@ -646,6 +783,7 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
     a.ks = K + n_shared;
     a.tm = L.tm;
     a.order = reinterpret_cast<int32_t*>(base + L.order);
+    a.cnt = reinterpret_cast<int32_t*>(base + L.cnt);
     a.tiles = reinterpret_cast<int4*>(base + L.tiles);
     a.ntiles = reinterpret_cast<int32_t*>(base + L.ntiles);
     a.act = reinterpret_cast<uint16_t*>(base + L.act);
@@ -660,8 +798,9 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
         if (xf) return yf ? launch_decode<true, true>(a, L, s, ev_mid) : launch_decode<true, false>(a, L, s, ev_mid);
         return yf ? launch_decode<false, true>(a, L, s, ev_mid) : launch_decode<false, false>(a, L, s, ev_mid);
     }
-    if (xf) return yf ? launch_direct<true, true>(a, L, s, ev_mid) : launch_direct<true, false>(a, L, s, ev_mid);
-    return yf ? launch_direct<false, true>(a, L, s, ev_mid) : launch_direct<false, false>(a, L, s, ev_mid);
+    uint16_t* xs = reinterpret_cast<uint16_t*>(base + L.xs);
+    if (xf) return yf ? launch_prompt<true, true>(a, L, xs, s, ev_mid) : launch_prompt<true, false>(a, L, xs, s, ev_mid);
+    return yf ? launch_prompt<false, true>(a, L, xs, s, ev_mid) : launch_prompt<false, false>(a, L, xs, s, ev_mid);
 }
 
 }  // namespace stmoe
@@ -674,7 +813,7 @@ extern "C" size_t moe_expert_ffn_mx_workspace_bytes(int T, int K, int E, int H, 
         I < 8 || I % 8 || I > kMaxI || n_shared < 0 || n_shared > kMaxShared)
         return 0;
     if ((dtype != STMOE_BF16 && dtype != STMOE_F32) || (ydtype != STMOE_BF16 && ydtype != STMOE_F32)) return 0;
-    return mx_layout(T < 1 ? 1 : T, K, E, H, I, n_shared, ydtype).total;
+    return mx_layout(T < 1 ? 1 : T, K, E, H, I, n_shared, dtype, ydtype).total;
 }
 
 extern "C" int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const float* topk_w, int T, int K, int H,
