@@ -137,32 +137,32 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     }
     if (threadIdx.x == 0) at = 0;
     __syncthreads();
-    const int n = a.T * a.K;
-    for (int i0 = 0; i0 < n; i0 += 4 * kPlanThreads) {
-        // four entries per thread, a wave's consecutive ones together
-        int e[4];
+    // a token per thread: the first of its entries that names the expert
+    const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
+    for (int t0 = 0; t0 < a.T; t0 += kPlanThreads) {
+        const int t = t0 + threadIdx.x;
+        int k = -1;
+        if (t < a.T) {
+            const int32_t* row = a.idx + size_t(t) * a.K;
+            if (four) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int i = i0 + v * kPlanThreads + threadIdx.x;
-            e[v] = i < n ? a.idx[i] : -1;
-        }
+                for (int j = kMaxK - 4; j >= 0; j -= 4)
+                    if (j < a.K) {
+                        const int4 e = *reinterpret_cast<const int4*>(row + j);
+                        k = e.x == g ? j : e.y == g ? j + 1 : e.z == g ? j + 2 : e.w == g ? j + 3 : k;
+                    }
+            } else {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int i = i0 + v * kPlanThreads + threadIdx.x;
-            bool hit = e[v] == g;
-            int t = 0, k = 0;
-            if (hit) {
-                t = i / a.K;
-                k = i - t * a.K;
-                for (int j = 0; j < k; ++j) hit &= a.idx[size_t(t) * a.K + j] != g;
+                for (int j = kMaxK - 1; j >= 0; --j)
+                    if (j < a.K && row[j] == g) k = j;
             }
-            const unsigned long long m = __ballot(hit);
-            if (!m) continue;
-            int base = 0;
-            if (lane == 0) base = atomicAdd(&at, __popcll(m));
-            base = __builtin_amdgcn_readfirstlane(base);
-            if (hit) out[base + __popcll(m & ((1ull << lane) - 1ull))] = t * a.ks + k;
         }
+        const unsigned long long m = __ballot(k >= 0);
+        if (!m) continue;
+        int base = 0;
+        if (lane == 0) base = atomicAdd(&at, __popcll(m));
+        base = __builtin_amdgcn_readfirstlane(base);
+        if (k >= 0) out[base + __popcll(m & ((1ull << lane) - 1ull))] = t * a.ks + k;
     }
     __syncthreads();
     if (threadIdx.x == 0) a.cnt[g] = at;
@@ -320,6 +320,7 @@ __global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxAr
             for (int i = 0; i < RB; ++i) wv[i] = decode8(w[i][s], sc[i]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
+                if (n % 2 == 0 && n && 16 * n >= tl.z) break;       // 32 tokens at a time
                 union {
                     u32x4 u;
                     bf16x8 v;

@@ -10,17 +10,23 @@
 //   a_te = g_b E c_e / (n^2 K) + [e = idx_tk] g_tk            (weights p)
 // or, with renormalised weights w_k = softmax over the selected logits, the
 // second term of a_te is replaced by w_k (g_tk - sum_j w_j g_tj) on top of d_te.
-// Both directions are one pass over the logits, a row in a wave's registers.
-#include "gating_dev.h"
+// Both directions are one pass over the logits.  A row belongs to 16 lanes, a
+// row of the vector unit: its sums and maxima are four lane rotations, and a
+// wave works on four rows at once, with up to 16 logits of each in a lane's
+// registers.  The K winners are taken one by one (largest key, lowest index).
+#include <type_traits>
+
+#include "common.h"
 
 namespace stmoe {
 namespace {
 
-using gating::kKeyRegs;
-
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-constexpr int kMaxWg = 512;        // workgroups of the forward pass, each with a row of partial sums
+constexpr int kWaves = 16;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kRowLanes = 16;
+constexpr int kRows = 64 / kRowLanes;      // rows a wave works on
+constexpr int kMaxWg = 256;                // workgroups of the forward pass, each with a row of partial sums
+constexpr int kGradThreads = 256;
 
 struct BalanceArgs {
     const void* logits;            // [T] rows of stride ld
@@ -41,108 +47,187 @@ struct BalanceArgs {
     int wg;
 };
 
-// Logits of row t: lane l holds those of l, l + 64, ...
-template <bool BF>
-__device__ __forceinline__ void load_row(const void* logits, int64_t at, int E, float (&z)[kKeyRegs]) {
-    const int lane = threadIdx.x & 63;
+// Rotations within the 16 lanes of a row.
+template <int N>
+__device__ __forceinline__ uint32_t rotate(uint32_t v) {
+    return uint32_t(__builtin_amdgcn_update_dpp(int(v), int(v), 0x120 + N, 0xf, 0xf, false));
+}
+template <int N>
+__device__ __forceinline__ float rotate(float v) { return __uint_as_float(rotate<N>(__float_as_uint(v))); }
+
+__device__ __forceinline__ float row_sum(float v) {
+    v += rotate<8>(v);
+    v += rotate<4>(v);
+    v += rotate<2>(v);
+    return v + rotate<1>(v);
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+    v = max(v, rotate<8>(v));
+    v = max(v, rotate<4>(v));
+    v = max(v, rotate<2>(v));
+    return max(v, rotate<1>(v));
+}
+__device__ __forceinline__ uint32_t row_min(uint32_t v) {
+    v = min(v, rotate<8>(v));
+    v = min(v, rotate<4>(v));
+    v = min(v, rotate<2>(v));
+    return min(v, rotate<1>(v));
+}
+
+// Candidates' order as unsigned keys: larger logit, larger key; -0 and +0 are
+// one value; NaN 1, below every number; minus infinity is no candidate: 0.
+__device__ __forceinline__ uint32_t key_of(float v) {
+    const uint32_t u = v == 0.f ? 0u : __float_as_uint(v);
+    const uint32_t k = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    return v != v ? 1u : v == -INFINITY ? 0u : k;
+}
+__device__ __forceinline__ float value_of(uint32_t key) {
+    return key == 1u ? __builtin_nanf("") : __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
+}
+
+// Expert of a lane's v-th logit.  VEC: four consecutive ones, loaded at once.
+template <bool VEC>
+__device__ __forceinline__ int expert_at(int v, int l) {
+    return VEC ? (v >> 2) * 4 * kRowLanes + 4 * l + (v & 3) : v * kRowLanes + l;
+}
+
+// A lane's logits of the row at element `at`; minus infinity beyond E.
+template <bool BF, int V, bool VEC>
+__device__ __forceinline__ void load_row(const void* logits, int64_t at, int E, int l, float (&z)[V]) {
+    if constexpr (VEC) {
 #pragma unroll
-    for (int v = 0; v < kKeyRegs; ++v) {
-        const int e = 64 * v + lane;
-        z[v] = -INFINITY;
-        if (e < E)
-            z[v] = BF ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(logits)[at + e]) << 16)
-                      : reinterpret_cast<const float*>(logits)[at + e];
+        for (int v = 0; v < V; v += 4) {
+            const int e = expert_at<true>(v, l);
+            const bool in = e < E;         // E is a multiple of 4
+            if constexpr (BF) {
+                uint2 q = make_uint2(0xff80ff80u, 0xff80ff80u);
+                if (in) q = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(logits) + at + e);
+                z[v] = bf16_lo(q.x);
+                z[v + 1] = bf16_hi(q.x);
+                z[v + 2] = bf16_lo(q.y);
+                z[v + 3] = bf16_hi(q.y);
+            } else {
+                float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                if (in) q = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(logits) + at + e);
+                z[v] = q.x;
+                z[v + 1] = q.y;
+                z[v + 2] = q.z;
+                z[v + 3] = q.w;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = expert_at<false>(v, l);
+            z[v] = -INFINITY;
+            if (e < E)
+                z[v] = BF ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(logits)[at + e]) << 16)
+                          : reinterpret_cast<const float*>(logits)[at + e];
+        }
     }
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, 64));
-    return v;
-}
+// exp(z - top) of a candidate; none (0) for minus infinity.
+__device__ __forceinline__ float term(float z, float top) { return z == -INFINITY ? 0.f : expf(z - top); }
 
-// Softmax terms of a row: its largest logit (NaN aside), exp(z - max), their
-// sum.  Logits of minus infinity are no candidates; false where a row has none.
-__device__ __forceinline__ bool row_softmax(const float (&z)[kKeyRegs], float& top, float (&ex)[kKeyRegs], float& sum) {
-    float m = -INFINITY;
-    bool any = false;
-#pragma unroll
-    for (int v = 0; v < kKeyRegs; ++v) {
-        m = fmaxf(m, z[v]);
-        any |= z[v] != -INFINITY;      // also NaN
-    }
-    top = wave_max(m);
-    float s = 0.f;
-#pragma unroll
-    for (int v = 0; v < kKeyRegs; ++v) {
-        ex[v] = z[v] == -INFINITY ? 0.f : expf(z[v] - top);
-        s += ex[v];
-    }
-    sum = wave_sum(s);
-    return __ballot(any) != 0ull;
-}
-
-template <bool BF>
+template <bool BF, int V, bool VEC>
 __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
-    __shared__ float lp[kWaves][kMaxE];
-    __shared__ int32_t lc[kMaxE];
+    __shared__ float lp[kWaves][V * kRowLanes];
+    __shared__ int32_t lc[V * kRowLanes];
     __shared__ float lz[kWaves];
     __shared__ int32_t ln[kWaves];
-    constexpr int V = kKeyRegs;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int e = threadIdx.x; e < kMaxE; e += kThreads) lc[e] = 0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (kRowLanes - 1), r = lane / kRowLanes;
+    for (int e = threadIdx.x; e < V * kRowLanes; e += kThreads) lc[e] = 0;
     __syncthreads();
     float ps[V], zs = 0.f;
-    int n = 0;
+    int cs[V], n = 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) ps[v] = 0.f;
-    for (int64_t t = int64_t(blockIdx.x) * kWaves + wave; t < a.T; t += int64_t(gridDim.x) * kWaves) {
-        float z[V], ex[V], top, sum;
-        uint32_t key[V];
-        bool ok[V], win[V];
-        int pos[V];
-        const bool masked = a.mask && !a.mask[t];
-        bool live = false;
-        if (!masked) {
-            load_row<BF>(a.logits, t * a.ld, a.E, z);
-            live = row_softmax(z, top, ex, sum);
+    for (int v = 0; v < V; ++v) {
+        ps[v] = 0.f;
+        cs[v] = 0;
+    }
+    const int64_t step = int64_t(gridDim.x) * kWaves * kRows;
+    for (int64_t t0 = (int64_t(blockIdx.x) * kWaves + wave) * kRows; t0 < a.T; t0 += step) {
+        const int64_t t = t0 + r;
+        const bool in = t < a.T;
+        float z[V];
+        // rows beyond the batch and masked ones have no candidates
+        if (in && !(a.mask && !a.mask[t])) {
+            load_row<BF, V, VEC>(a.logits, t * a.ld, a.E, l, z);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) z[v] = -INFINITY;
         }
-        int won = 0;
-        if (live) {
+        uint32_t key[V], best = 0u;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            key[v] = key_of(z[v]);
+            best = max(best, key[v]);
+        }
+        best = row_max(best);
+        const bool live = best != 0u;
+        const float top = value_of(best);
+        float ex[V], sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            ex[v] = live ? term(z[v], top) : 0.f;
+            sum += ex[v];
+        }
+        sum = row_sum(sum);
+        const float inv = live ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) ps[v] += ex[v] * inv;
+        // lane k of the row keeps winner k
+        int mine = -1;
+        uint32_t won = 0u;
+        for (int k = 0; k < a.K; ++k) {
+            if (k) {
+                best = 0u;
+#pragma unroll
+                for (int v = 0; v < V; ++v) best = max(best, key[v]);
+                best = row_max(best);
+            }
+            uint32_t at = ~0u;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) at = key[v] == best ? uint32_t(expert_at<VEC>(v, l)) : at;
+            at = row_min(at);
+            if (l == k && best) {
+                mine = int(at);
+                won = best;
+            }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                ok[v] = 64 * v + lane < a.E && z[v] != -INFINITY;
-                // NaN ranks below every number and above what is no candidate
-                const uint32_t k = gating::order_key(z[v]);
-                key[v] = ok[v] ? (k ? k : 1u) : 0u;
+                const bool hit = best && at == uint32_t(expert_at<VEC>(v, l));
+                key[v] = hit ? 0u : key[v];
+                cs[v] += hit;
             }
-            gating::topk_positions(key, ok, a.E, a.K, win, pos);
-            float q = 0.f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                won += __popcll(__ballot(win[v]));
-                q += win[v] ? ex[v] : 0.f;
-                ps[v] += ex[v] / sum;
-            }
-            const float norm = a.renorm ? wave_sum(q) : sum;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (win[v]) {
-                    a.idx[t * a.K + pos[v]] = 64 * v + lane;
-                    a.w[t * a.K + pos[v]] = ex[v] / norm;
-                    atomicAdd(&lc[64 * v + lane], 1);
-                }
+        }
+        const float wk = mine >= 0 ? expf(value_of(won) - top) : 0.f;
+        const float norm = a.renorm ? 1.f / row_sum(wk) : inv;
+        if (in && l < a.K) {
+            a.idx[t * a.K + l] = mine;
+            a.w[t * a.K + l] = mine >= 0 ? wk * norm : 0.f;
+        }
+        if (live && l == 0) {
             const float lse = top + logf(sum);
             zs += lse * lse;
             ++n;
         }
-        if (lane >= won && lane < a.K) {
-            a.idx[t * a.K + lane] = -1;
-            a.w[t * a.K + lane] = 0.f;
+    }
+    // the wave's four rows, then the waves in order
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        ps[v] += __shfl_xor(ps[v], 16, 64);
+        ps[v] += __shfl_xor(ps[v], 32, 64);
+        cs[v] += __shfl_xor(cs[v], 16, 64);
+        cs[v] += __shfl_xor(cs[v], 32, 64);
+        if (lane < kRowLanes) {
+            lp[wave][expert_at<VEC>(v, l)] = ps[v];
+            if (cs[v]) atomicAdd(&lc[expert_at<VEC>(v, l)], cs[v]);
         }
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) lp[wave][64 * v + lane] = ps[v];
+    zs = wave_sum(zs);
+    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d, 64);
     if (lane == 0) {
         lz[wave] = zs;
         ln[wave] = n;
@@ -150,6 +235,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     __syncthreads();
     for (int e = threadIdx.x; e < a.E; e += kThreads) {
         float s = 0.f;
+#pragma unroll
         for (int u = 0; u < kWaves; ++u) s += lp[u][e];
         a.part_p[size_t(blockIdx.x) * a.E + e] = s;
         a.part_c[size_t(blockIdx.x) * a.E + e] = lc[e];
@@ -166,39 +252,63 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     }
 }
 
-// Sums over the workgroups, in their order, in 64 bits; the losses.
-__global__ __launch_bounds__(kThreads) void balance_finish_kernel(BalanceArgs a) {
-    __shared__ double red[kThreads];
-    __shared__ int nn;
-    const int e = threadIdx.x;
-    if (e == 0) {
-        int n = 0;
-        for (int g = 0; g < a.wg; ++g) n += a.part_n[g];
-        nn = n;
-        *a.n = n;
-    }
-    __syncthreads();
-    const double n = nn > 0 ? nn : 1;
-    double term = 0.0;
+// Sums over the workgroups in 64 bits, in a fixed order; the losses.  Thread
+// (part, expert): every kParts-th workgroup.
+__global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs a) {
+    __shared__ double sp[1024];
+    __shared__ int sc[1024];
+    __shared__ double zz[kMaxWg];
+    __shared__ int nn[kMaxWg];
+    const int tid = threadIdx.x;
+    int EP = 32;                           // experts side by side, a power of two
+    while (EP < a.E) EP *= 2;
+    const int parts = 1024 / EP, e = tid & (EP - 1), part = tid / EP;
+    double p = 0.0;
+    int c = 0;
     if (e < a.E) {
-        double p = 0.0;
-        int c = 0;
-        for (int g = 0; g < a.wg; ++g) {
+#pragma unroll 8
+        for (int g = part; g < a.wg; g += parts) {
             p += a.part_p[size_t(g) * a.E + e];
             c += a.part_c[size_t(g) * a.E + e];
         }
-        a.counts[e] = c;
-        if (a.prob_sum) a.prob_sum[e] = float(p);
-        term = a.E * (c / (n * a.K)) * (p / n);
     }
-    red[e] = term;
+    sp[tid] = p;
+    sc[tid] = c;
+    if (tid < kMaxWg) {
+        zz[tid] = tid < a.wg ? a.part_z[tid] : 0.f;
+        nn[tid] = tid < a.wg ? a.part_n[tid] : 0;
+    }
+    for (int d = kMaxWg / 2; d; d >>= 1) {
+        __syncthreads();
+        if (tid < d) {
+            zz[tid] += zz[tid + d];
+            nn[tid] += nn[tid + d];
+        }
+    }
     __syncthreads();
-    if (e == 0) {
-        double s = 0.0, z = 0.0;
-        for (int i = 0; i < a.E; ++i) s += red[i];
-        for (int g = 0; g < a.wg; ++g) z += a.part_z[g];
-        a.loss[0] = float(s);
-        a.loss[1] = float(z / n);
+    const double n = nn[0] > 0 ? nn[0] : 1;
+    double term = 0.0;
+    if (part == 0) {
+        for (int g = 1; g < parts; ++g) {
+            p += sp[g * EP + e];
+            c += sc[g * EP + e];
+        }
+        if (e < a.E) {
+            a.counts[e] = c;
+            if (a.prob_sum) a.prob_sum[e] = float(p);
+            term = a.E * (c / (n * a.K)) * (p / n);
+        }
+    }
+    __syncthreads();
+    if (part == 0) sp[e] = term;
+    for (int d = EP / 2; d; d >>= 1) {
+        __syncthreads();
+        if (tid < d) sp[tid] += sp[tid + d];
+    }
+    if (tid == 0) {
+        *a.n = nn[0];
+        a.loss[0] = float(sp[0]);
+        a.loss[1] = float(zz[0] / n);
     }
 }
 
@@ -211,70 +321,114 @@ struct BalanceGradArgs {
     void* d_logits;
 };
 
-template <bool BF>
-__global__ __launch_bounds__(kThreads) void balance_grad_kernel(BalanceGradArgs a) {
-    constexpr int V = kKeyRegs;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// The gate weights' part of a row, one term per selected expert, goes through
+// LDS to the lanes that hold those experts.
+template <bool BF, int V, bool VEC>
+__global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradArgs a) {
+    __shared__ float sel[kGradThreads / 64][kRows][V * kRowLanes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (kRowLanes - 1), r = lane / kRowLanes;
+    float* mysel = sel[wave][r];
+#pragma unroll
+    for (int v = 0; v < V; ++v) mysel[v * kRowLanes + l] = 0.f;
     const float n = float(*a.n > 0 ? *a.n : 1);
-    const float gz = 2.f * a.d_loss[1] / n;
+    const float gz = 2.f * a.d_loss[1] / n, cb = a.d_loss[0] * a.E / a.K / n / n;
     float cf[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        cf[v] = 64 * v + lane < a.E ? a.d_loss[0] * a.E / a.K * float(a.counts[64 * v + lane]) / (n * n) : 0.f;
-    for (int64_t t = int64_t(blockIdx.x) * kWaves + wave; t < a.T; t += int64_t(gridDim.x) * kWaves) {
-        const int sel = lane < a.K ? a.idx[t * a.K + lane] : -1;
-        const float dw = a.d_w && sel >= 0 ? a.d_w[t * a.K + lane] : 0.f;
-        float d[V];
+    for (int v = 0; v < V; ++v) {
+        const int e = expert_at<VEC>(v, l);
+        cf[v] = e < a.E ? cb * float(a.counts[e]) : 0.f;
+    }
+    const int64_t step = int64_t(gridDim.x) * (kGradThreads / 64) * kRows;
+    for (int64_t t0 = (int64_t(blockIdx.x) * (kGradThreads / 64) + wave) * kRows; t0 < a.T; t0 += step) {
+        const int64_t t = t0 + r;
+        const bool in = t < a.T;
+        const int mine = in && l < a.K ? a.idx[t * a.K + l] : -1;
+        const bool live = __shfl(mine, r * kRowLanes, 64) >= 0;
+        float z[V];
+        if (live) {
+            load_row<BF, V, VEC>(a.logits, t * a.ld, a.E, l, z);
+        } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) d[v] = 0.f;
-        float z[V], ex[V], top, sum;
-        if (__builtin_amdgcn_readfirstlane(sel) >= 0) {
-            load_row<BF>(a.logits, t * a.ld, a.E, z);
-            row_softmax(z, top, ex, sum);
-            float gw[V];
-            bool hit[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                gw[v] = 0.f;
-                hit[v] = false;
-            }
-            for (int k = 0; k < a.K; ++k) {
-                const int e = __builtin_amdgcn_readlane(sel, k);
-                const float g = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(dw), k));
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (e == 64 * v + lane) {
-                        gw[v] += g;
-                        hit[v] = true;
-                    }
-            }
-            float q = 0.f, qg = 0.f, pa = 0.f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                q += hit[v] ? ex[v] : 0.f;
-                qg += hit[v] ? ex[v] * gw[v] : 0.f;
-            }
-            if (a.renorm) {
-                q = wave_sum(q);
-                qg = wave_sum(qg) / q;
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) pa += ex[v] / sum * (cf[v] + (a.renorm ? 0.f : gw[v]));
-            pa = wave_sum(pa);
-            const float lse = top + logf(sum);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float p = ex[v] / sum;
-                d[v] = p * (cf[v] + (a.renorm ? 0.f : gw[v]) - pa + gz * lse);
-                if (a.renorm && hit[v]) d[v] += ex[v] / q * (gw[v] - qg);
-            }
+            for (int v = 0; v < V; ++v) z[v] = -INFINITY;
         }
+        const bool chosen = a.d_w && live && mine >= 0 && mine < a.E;
+        float g = 0.f, zk = -INFINITY;
+        if (chosen) {
+            g = a.d_w[t * a.K + l];
+            zk = BF ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(a.logits)[t * a.ld + mine]) << 16)
+                    : reinterpret_cast<const float*>(a.logits)[t * a.ld + mine];
+        }
+        // the largest number; a NaN enters by its own term
+        uint32_t best = 0u;
+#pragma unroll
+        for (int v = 0; v < V; ++v) best = max(best, key_of(z[v]));
+        const float top = value_of(row_max(best));
+        float ex[V], sum = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int e = 64 * v + lane;
-            if (e >= a.E) continue;
-            if (BF) reinterpret_cast<__bf16*>(a.d_logits)[t * a.ld_d + e] = __bf16(d[v]);
-            else reinterpret_cast<float*>(a.d_logits)[t * a.ld_d + e] = d[v];
+            ex[v] = live ? term(z[v], top) : 0.f;
+            sum += ex[v];
+        }
+        sum = row_sum(sum);
+        const float inv = live ? 1.f / sum : 0.f;
+        float pa = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            ex[v] *= inv;
+            pa += ex[v] * cf[v];
+        }
+        float base = gz * (live ? top + logf(sum) : 0.f) - row_sum(pa);
+        if (a.d_w) {
+            // lane k: selected expert k with its weight
+            float wk = chosen ? term(zk, top) : 0.f;
+            wk *= a.renorm ? 1.f / row_sum(wk) : inv;
+            const float wg = row_sum(chosen ? wk * g : 0.f);
+            if (!a.renorm) base -= wg;
+            if (chosen) mysel[mine] = a.renorm ? wk * (g - wg) : wk * g;
+            // a wave's LDS accesses complete in order
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        float d[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            d[v] = ex[v] * (cf[v] + base);
+            if (a.d_w) d[v] += mysel[expert_at<VEC>(v, l)];
+            if (!live) d[v] = 0.f;
+        }
+        if (a.d_w) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (chosen) mysel[mine] = 0.f;
+        }
+        if (!in) continue;
+        const int64_t o = t * a.ld_d;
+        if constexpr (VEC) {
+#pragma unroll
+            for (int v = 0; v < V; v += 4) {
+                const int e = expert_at<true>(v, l);
+                if (e >= a.E) continue;
+                if constexpr (BF) {
+                    union {
+                        __bf16 b[4];
+                        uint2 q;
+                    } u;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u.b[i] = __bf16(d[v + i]);
+                    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.d_logits) + o + e) = u.q;
+                } else {
+                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.d_logits) + o + e) =
+                        make_float4(d[v], d[v + 1], d[v + 2], d[v + 3]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int e = expert_at<false>(v, l);
+                if (e >= a.E) continue;
+                if (BF) reinterpret_cast<__bf16*>(a.d_logits)[o + e] = __bf16(d[v]);
+                else reinterpret_cast<float*>(a.d_logits)[o + e] = d[v];
+            }
         }
     }
 }
@@ -286,7 +440,7 @@ struct BalanceLayout {
 
 BalanceLayout balance_layout(int64_t T, int E) {
     BalanceLayout y{};
-    const int64_t wg = (T + kWaves - 1) / kWaves;
+    const int64_t wg = (T + kWaves * kRows - 1) / (kWaves * kRows);
     y.wg = int(wg < 1 ? 1 : wg < kMaxWg ? wg : kMaxWg);
     size_t off = 0;
     auto take = [&](size_t b) { const size_t at = off; off = (off + b + 255) / 256 * 256; return at; };
@@ -296,6 +450,21 @@ BalanceLayout balance_layout(int64_t T, int E) {
     y.n = take(size_t(y.wg) * sizeof(int32_t));
     y.total = off;
     return y;
+}
+
+// Logits per lane for E experts, and whether four at a time: rows of whole
+// groups of four, aligned to them.
+template <class F>
+void with_row(int E, bool vec, F f) {
+    if (E <= 16) f(std::integral_constant<int, 1>(), std::false_type());
+    else if (E <= 32) f(std::integral_constant<int, 2>(), std::false_type());
+    else if (E <= 64) vec ? f(std::integral_constant<int, 4>(), std::true_type()) : f(std::integral_constant<int, 4>(), std::false_type());
+    else if (E <= 128) vec ? f(std::integral_constant<int, 8>(), std::true_type()) : f(std::integral_constant<int, 8>(), std::false_type());
+    else vec ? f(std::integral_constant<int, 16>(), std::true_type()) : f(std::integral_constant<int, 16>(), std::false_type());
+}
+
+bool rows_of_four(const void* p, int64_t ld, int E, int esz) {
+    return E % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * esz) == 0;
 }
 
 int check_router(const char* fn, int64_t T, int64_t ld, int E, int K, int dtype) {
@@ -354,10 +523,15 @@ extern "C" int moe_route_balance(const void* logits, int64_t T, int64_t ld, int 
     a.part_n = reinterpret_cast<int32_t*>(base + L.n);
     a.wg = L.wg;
     hipStream_t s = as_stream(stream);
-    if (dtype == STMOE_BF16) hipLaunchKernelGGL((balance_kernel<true>), dim3(unsigned(L.wg)), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((balance_kernel<false>), dim3(unsigned(L.wg)), dim3(kThreads), 0, s, a);
+    with_row(E, rows_of_four(logits, ld, E, dtype == STMOE_BF16 ? 2 : 4), [&](auto v, auto vec) {
+        const dim3 grid(unsigned(L.wg));
+        if (dtype == STMOE_BF16)
+            hipLaunchKernelGGL((balance_kernel<true, v(), vec()>), grid, dim3(kThreads), 0, s, a);
+        else
+            hipLaunchKernelGGL((balance_kernel<false, v(), vec()>), grid, dim3(kThreads), 0, s, a);
+    });
     STMOE_LAUNCHED();
-    hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(1024), 0, s, a);
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
@@ -388,12 +562,15 @@ extern "C" int moe_route_balance_backward(const void* logits, int64_t T, int64_t
     a.d_w = d_w;
     a.d_loss = d_loss;
     a.d_logits = d_logits;
-    const int64_t wg = (T + kWaves - 1) / kWaves;
-    const dim3 grid(unsigned(wg < 2048 ? wg : 2048));
-    if (dtype == STMOE_BF16)
-        hipLaunchKernelGGL((balance_grad_kernel<true>), grid, dim3(kThreads), 0, as_stream(stream), a);
-    else
-        hipLaunchKernelGGL((balance_grad_kernel<false>), grid, dim3(kThreads), 0, as_stream(stream), a);
+    const int64_t per = kGradThreads / 64 * kRows, wg = (T + per - 1) / per;
+    const dim3 grid(unsigned(wg < 4096 ? wg : 4096));
+    const int b = int(esz);
+    with_row(E, rows_of_four(logits, ld, E, b) && rows_of_four(d_logits, ld_d, E, b), [&](auto v, auto vec) {
+        if (dtype == STMOE_BF16)
+            hipLaunchKernelGGL((balance_grad_kernel<true, v(), vec()>), grid, dim3(kGradThreads), 0, as_stream(stream), a);
+        else
+            hipLaunchKernelGGL((balance_grad_kernel<false, v(), vec()>), grid, dim3(kGradThreads), 0, as_stream(stream), a);
+    });
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
