@@ -68,8 +68,11 @@ struct Pieces<true> {
 };
 
 // A value as two bf16 numbers; infinities and NaN (and what rounds to
-// infinity) keep to the first.
+// infinity) keep to the first.  The difference is that of the rounded value:
+// fused with the product that gave v, it would depend on how the compiler
+// arranged the caller, and a token's bits on the tile it falls into.
 __device__ __forceinline__ void split(float v, __bf16& hi, __bf16& lo) {
+#pragma clang fp contract(off)
     hi = __bf16(v);
     const float h = float(hi);
     lo = __builtin_isfinite(h) ? __bf16(v - h) : __bf16(0.f);
@@ -124,22 +127,21 @@ __device__ __forceinline__ int entry_expert(const MxArgs& a, int t, int k) {
     return e;
 }
 
-// Entries of one expert per workgroup, any order (a token's results do not
-// depend on its place): order[g * T ..] and cnt[g].
+// Entries of one expert per workgroup, by token: order[g * T ..] and cnt[g].
 __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
-    __shared__ int at;
-    const int g = blockIdx.x, lane = threadIdx.x & 63;
+    constexpr int W = kPlanThreads / 64;
+    __shared__ int found[2][W];
+    const int g = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t* out = a.order + size_t(g) * a.T;
     if (g >= a.E) {
         for (int t = threadIdx.x; t < a.T; t += kPlanThreads) out[t] = t * a.ks + a.K + (g - a.E);
         if (threadIdx.x == 0) a.cnt[g] = a.T;
         return;
     }
-    if (threadIdx.x == 0) at = 0;
-    __syncthreads();
     // a token per thread: the first of its entries that names the expert
     const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
-    for (int t0 = 0; t0 < a.T; t0 += kPlanThreads) {
+    int before = 0;
+    for (int t0 = 0, par = 0; t0 < a.T; t0 += kPlanThreads, par ^= 1) {
         const int t = t0 + threadIdx.x;
         int k = -1;
         if (t < a.T) {
@@ -158,14 +160,18 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
             }
         }
         const unsigned long long m = __ballot(k >= 0);
-        if (!m) continue;
-        int base = 0;
-        if (lane == 0) base = atomicAdd(&at, __popcll(m));
-        base = __builtin_amdgcn_readfirstlane(base);
+        if (lane == 0) found[par][wave] = __popcll(m);
+        __syncthreads();
+        int base = before;
+#pragma unroll
+        for (int v = 0; v < W; ++v) {
+            const int c = found[par][v];
+            base += v < wave ? c : 0;
+            before += c;
+        }
         if (k >= 0) out[base + __popcll(m & ((1ull << lane) - 1ull))] = t * a.ks + k;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) a.cnt[g] = at;
+    if (threadIdx.x == 0) a.cnt[g] = before;
 }
 
 // The tiles of at most tm tokens, experts in order: one workgroup.
@@ -234,20 +240,11 @@ __device__ __forceinline__ uint32_t word(const uint4& q, int s) { return s == 0 
 // chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
 // lanes of a read, one chunk of 16 tokens, meet 16 different places.
 template <bool UP, int NP, int NT, bool YF>
-__global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxArgs a, int nb) {
+__device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, u32x4* xs, int* ent) {
     constexpr int TM = 16 * NT;
     constexpr int RB = 4;                                   // row blocks per wave
     constexpr int CH = kTileCols / 8;                       // chunks per column
-    __shared__ u32x4 xs[2][TM * CH];
-    __shared__ int ent[TM];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // consecutive work on one XCD (workgroup i runs on XCD i % 8): the row
-    // blocks of a tile and the tiles of an expert share its L2
-    const int work = *a.ntiles * nb, per = (work + 7) / 8;
-    const int id = int(blockIdx.x % 8) * per + int(blockIdx.x / 8);
-    if (int(blockIdx.x / 8) >= per || id >= work) return;
-    const int tix = id / nb, bk = id - tix * nb;
-    const int4 tl = a.tiles[tix];
     const char* blobp = expert_blob(a, tl.x);
     const Blob L = blob(a.H, a.I);
     const int C = UP ? a.H : a.I, R = UP ? a.I : a.H;
@@ -301,7 +298,7 @@ __global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxAr
     const int c = lane & 15, q = lane >> 4, iters = KT * NP;
     load(0);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) xs[0][put + j * 16 * CH] = xr[j];
+    for (int j = 0; j < NT; ++j) xs[put + j * 16 * CH] = xr[j];
     for (int it = 0; it < iters; ++it) {
         u32x4 w[RB];
         float sc[RB];
@@ -312,7 +309,7 @@ __global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxAr
         }
         __syncthreads();
         if (it + 1 < iters) load(it + 1);
-        const u32x4* buf = xs[it & 1] + c * CH;
+        const u32x4* buf = xs + (it & 1) * TM * CH + c * CH;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             bf16x8 wv[RB];
@@ -320,7 +317,6 @@ __global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxAr
             for (int i = 0; i < RB; ++i) wv[i] = decode8(w[i][s], sc[i]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                if (n % 2 == 0 && n && 16 * n >= tl.z) break;       // 32 tokens at a time
                 union {
                     u32x4 u;
                     bf16x8 v;
@@ -333,7 +329,7 @@ __global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxAr
         }
         if (it + 1 < iters) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xs[(it + 1) & 1][put + j * 16 * CH] = xr[j];
+            for (int j = 0; j < NT; ++j) xs[((it + 1) & 1) * TM * CH + put + j * 16 * CH] = xr[j];
         }
     }
     // lane: token 16 n + c, rows 4 q .. 4 q + 3 of each block
@@ -374,6 +370,25 @@ __global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxAr
             }
         }
     }
+}
+
+template <bool UP, int NP, int NT, bool YF>
+__global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxArgs a, int nb) {
+    constexpr int TM = 16 * NT;
+    __shared__ u32x4 xs[2][TM * kTileCols / 8];
+    __shared__ int ent[TM];
+    // consecutive work on one XCD (workgroup i runs on XCD i % 8): the row
+    // blocks of a tile and the tiles of an expert share its L2
+    const int work = *a.ntiles * nb, per = (work + 7) / 8;
+    const int id = int(blockIdx.x % 8) * per + int(blockIdx.x / 8);
+    if (int(blockIdx.x / 8) >= per || id >= work) return;
+    const int tix = id / nb;
+    const int4 tl = a.tiles[tix];
+    if constexpr (NT > 1) {
+        // an expert's last tile, if at most half full, in half the instructions
+        if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, YF>(a, tl, id - tix * nb, xs[0], ent);
+    }
+    tile_product<UP, NP, NT, YF>(a, tl, id - tix * nb, xs[0], ent);
 }
 
 // y[t] = the sum of its entries' rows, in the entries' order.
