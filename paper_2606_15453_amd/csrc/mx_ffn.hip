@@ -224,11 +224,18 @@ __global__ __launch_bounds__(kThreads) void mx_split_kernel(const float* x, int6
     }
 }
 
-__device__ __forceinline__ const char* expert_blob(const MxArgs& a, int g) {
-    return reinterpret_cast<const char*>(g < a.E ? a.eptr[g] : a.sptr[g - a.E]);
+// Blobs are read through pointers to global memory: a load through a generic
+// pointer counts as an LDS access too, and every wait for LDS would wait for
+// the weights in flight.
+typedef const __attribute__((address_space(1))) char* GlobalBytes;
+template <class T>
+__device__ __forceinline__ T load_global(GlobalBytes p) {
+    return *(const __attribute__((address_space(1))) T*)p;
 }
 
-__device__ __forceinline__ uint32_t word(const uint4& q, int s) { return s == 0 ? q.x : s == 1 ? q.y : s == 2 ? q.z : q.w; }
+__device__ __forceinline__ GlobalBytes expert_blob(const MxArgs& a, int g) {
+    return (GlobalBytes)(g < a.E ? a.eptr[g] : a.sptr[g - a.E]);
+}
 
 // ---------------------------------------------------------------- prompts
 //
@@ -245,13 +252,13 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     constexpr int RB = 4;                                   // row blocks per wave
     constexpr int CH = kTileCols / 8;                       // chunks per column
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const char* blobp = expert_blob(a, tl.x);
+    GlobalBytes blobp = expert_blob(a, tl.x);
     const Blob L = blob(a.H, a.I);
     const int C = UP ? a.H : a.I, R = UP ? a.I : a.H;
     const int KT = col_tiles(C), KG = col_groups(C), NB = row_blocks(R);
     if (tid < TM) ent[tid] = a.order[size_t(tl.x) * a.T + tl.y + min(tid, tl.z - 1)];
     // the wave's row blocks; beyond the matrix the last one again, not stored
-    const char *wc[RB], *wsc[RB];
+    GlobalBytes wc[RB], wsc[RB];
     int rb[RB];
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
@@ -285,9 +292,8 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         for (int j = 0; j < NT; ++j) xr[j] = cols[src[j] + off];
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-            wn[i] = *reinterpret_cast<const u32x4*>(wc[i] + size_t(kt) * kTileBytes + lane * 16);
-            sn[i] = *reinterpret_cast<const uint8_t*>(wsc[i] + size_t(kt / kGroupTiles) * kGroupBytes + kt % kGroupTiles +
-                                                      lane * 4);
+            wn[i] = load_global<u32x4>(wc[i] + size_t(kt) * kTileBytes + lane * 16);
+            sn[i] = load_global<uint8_t>(wsc[i] + size_t(kt / kGroupTiles) * kGroupBytes + kt % kGroupTiles + lane * 4);
         }
     };
     f32x4 acc[RB][NT];
@@ -432,18 +438,18 @@ constexpr int kUnitTiles = 2;       // tiles a wave takes at a time: 2 KiB of co
 constexpr int kDownWaves = 8;
 
 struct Unit {
-    uint4 c[kUnitTiles];
+    u32x4 c[kUnitTiles];
     uint32_t s;                     // the tiles' scale bytes
 };
 
 // Unit u of a row block whose codes and scales begin at c and s.  A missing
 // last tile repeats the one before it (its columns' operands are zero).
-__device__ __forceinline__ Unit load_unit(const char* c, const char* s, int u, int KT, int lane) {
+__device__ __forceinline__ Unit load_unit(GlobalBytes c, GlobalBytes s, int u, int KT, int lane) {
     Unit r;
     const int t = u * kUnitTiles, t1 = t + 1 < KT ? t + 1 : t;
-    r.c[0] = *reinterpret_cast<const uint4*>(c + size_t(t) * kTileBytes + lane * 16);
-    r.c[1] = *reinterpret_cast<const uint4*>(c + size_t(t1) * kTileBytes + lane * 16);
-    const uint32_t v = *reinterpret_cast<const uint16_t*>(s + size_t(t / kGroupTiles) * kGroupBytes + lane * 4 + t % kGroupTiles);
+    r.c[0] = load_global<u32x4>(c + size_t(t) * kTileBytes + lane * 16);
+    r.c[1] = load_global<u32x4>(c + size_t(t1) * kTileBytes + lane * 16);
+    const uint32_t v = load_global<uint16_t>(s + size_t(t / kGroupTiles) * kGroupBytes + lane * 4 + t % kGroupTiles);
     r.s = t1 == t ? v & 0xffu : v;
     return r;
 }
@@ -484,13 +490,13 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
         if (slot - total >= a.ns) return;
         g = a.E + slot - total;
     }
-    const char* blobp = expert_blob(a, g);
+    GlobalBytes blobp = expert_blob(a, g);
     const Blob L = blob(a.H, a.I);
     const int KT = col_tiles(a.H), KG = col_groups(a.H), KU = (KT + kUnitTiles - 1) / kUnitTiles;
-    const char* gc = blobp + L.gate + size_t(rb) * KT * kTileBytes;
-    const char* uc = blobp + L.up + size_t(rb) * KT * kTileBytes;
-    const char* gs = blobp + L.gate_s + size_t(rb) * KG * kGroupBytes;
-    const char* us = blobp + L.up_s + size_t(rb) * KG * kGroupBytes;
+    GlobalBytes gc = blobp + L.gate + size_t(rb) * KT * kTileBytes;
+    GlobalBytes uc = blobp + L.up + size_t(rb) * KT * kTileBytes;
+    GlobalBytes gs = blobp + L.gate_s + size_t(rb) * KG * kGroupBytes;
+    GlobalBytes us = blobp + L.up_s + size_t(rb) * KG * kGroupBytes;
     Unit ng{}, nu{};
     if (wave < KU) {
         ng = load_unit(gc, gs, wave, KT, lane);
@@ -534,7 +540,7 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const Pieces<XF> xv = pieces(xr[j][s]);
-                const bf16x8 gv = decode8(word(cg.c[j], s), sg), uv = decode8(word(cu.c[j], s), su);
+                const bf16x8 gv = decode8(cg.c[j][s], sg), uv = decode8(cu.c[j][s], su);
 #pragma unroll
                 for (int p = 0; p < Pieces<XF>::N; ++p) {
                     ag = __builtin_amdgcn_mfma_f32_16x16x32_bf16(gv, xv.p[p], ag, 0, 0, 0);
@@ -576,7 +582,7 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
 template <bool YF, bool PC>
 __global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int splits) {
     constexpr int NP = Pieces<YF>::N, MP = PC ? 1 : NP;     // pieces; instructions per operand
-    __shared__ const char* base[kMaxE + kMaxShared];
+    __shared__ GlobalBytes base[kMaxE + kMaxShared];
     __shared__ uint8_t sk[kMaxE + kMaxShared][kMaxB];
     __shared__ float red[kDownWaves][4][64];
     __shared__ int last;
@@ -629,7 +635,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int 
             const float sd = scale_of(cur.s >> (8 * j) & 0xffu);
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const bf16x8 dv = decode8(word(cur.c[j], s), sd);
+                const bf16x8 dv = decode8(cur.c[j][s], sd);
 #pragma unroll
                 for (int p = 0; p < MP; ++p)
                     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dv, pieces(h[j][s][p]).p[0], acc, 0, 0, 0);
