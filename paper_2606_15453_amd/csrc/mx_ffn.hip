@@ -37,7 +37,7 @@ struct MxArgs {
     int4* tiles;                    // (expert, first place in its order, tokens, -)
     int32_t* ntiles;
     uint16_t* act;                  // [entry][piece][I] bf16 pieces
-    float* part;                    // [entry][H]
+    void* part;                     // [entry][H] terms of y, of its type
     // decode steps (T <= 16)
     struct DecodeSlot* slots;       // by ascending expert, the shared ones last
     int32_t* nslots;
@@ -114,6 +114,11 @@ __device__ __forceinline__ Pieces<true> pieces(const Raw<true>& r) {
     }
     return o;
 }
+
+// g / (1 + exp(-g)) with the hardware's exponential and reciprocal (2^-23 of
+// their values; the exponent's product rounds to 2^-24 of |g|, so silu is off
+// by less than 2e-6 of itself down to g = -20 and negligible below).
+__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 
 // The expert of an entry, or -1 where it names none or repeats an earlier
 // entry of its token (the first one counts).
@@ -355,7 +360,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
                 } o[NH];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float g = acc[i][n][r], v = g / (1.f + expf(-g)) * acc[i + 2][n][r];
+                    const float g = acc[i][n][r], v = silu(g) * acc[i + 2][n][r];
                     if constexpr (YF) split(v, o[0].h[r], o[1].h[r]);
                     else o[0].h[r] = __bf16(v);
                 }
@@ -371,8 +376,19 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
                 const int row = rb[i] * kTileRows + 4 * q;
                 if (row >= a.H) continue;
                 const f32x4 d = acc[i][n];
-                *reinterpret_cast<float4*>(a.part + size_t(e) * a.H + row) =
-                    make_float4(w * d[0], w * d[1], w * d[2], w * d[3]);
+                const size_t at = size_t(e) * a.H + row;
+                if constexpr (YF) {
+                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.part) + at) =
+                        make_float4(w * d[0], w * d[1], w * d[2], w * d[3]);
+                } else {
+                    union {
+                        __bf16 b[4];
+                        uint2 v;
+                    } o;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o.b[r] = __bf16(w * d[r]);
+                    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.part) + at) = o.v;
+                }
             }
         }
     }
@@ -397,30 +413,41 @@ __global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxAr
     tile_product<UP, NP, NT, YF>(a, tl, id - tix * nb, xs[0], ent);
 }
 
-// y[t] = the sum of its entries' rows, in the entries' order.
+// y[t] = the sum of its entries' terms, in the entries' order, in fp32.  The
+// terms are of y's type: with bf16 y each is rounded once (2^-8 of itself at
+// most, as y is), which halves what the down launch writes and this one reads.
 template <bool YF>
 __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a) {
-    const int t = blockIdx.x;
-    unsigned used = 0u;
-    for (int k = 0; k < a.ks; ++k)
-        if (entry_expert(a, t, k) >= 0) used |= 1u << k;
-    for (int h = threadIdx.x * 4; h < a.H; h += kThreads * 4) {
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < a.ks; ++k) {
-            if (!(used >> k & 1u)) continue;
-            const float4 v = *reinterpret_cast<const float4*>(a.part + (size_t(t) * a.ks + k) * a.H + h);
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
+    constexpr int V = YF ? 4 : 8;           // 16 bytes of terms
+    const int t = blockIdx.y;
+    const int h = (blockIdx.x * kThreads + threadIdx.x) * V;
+    if (h >= a.H) return;
+    float s[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < a.ks; ++k) {
+        if (entry_expert(a, t, k) < 0) continue;
+        const size_t at = (size_t(t) * a.ks + k) * a.H + h;
         if constexpr (YF) {
-            *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.y) + size_t(t) * a.H + h) = s;
+            const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.part) + at);
+            s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
         } else {
-            union {
-                __bf16 b[4];
-                uint2 v;
-            } o;
-            o.b[0] = __bf16(s.x); o.b[1] = __bf16(s.y); o.b[2] = __bf16(s.z); o.b[3] = __bf16(s.w);
-            *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.y) + size_t(t) * a.H + h) = o.v;
+            const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.part) + at);
+            s[0] += bf16_lo(v.x); s[1] += bf16_hi(v.x); s[2] += bf16_lo(v.y); s[3] += bf16_hi(v.y);
+            s[4] += bf16_lo(v.z); s[5] += bf16_hi(v.z); s[6] += bf16_lo(v.w); s[7] += bf16_hi(v.w);
         }
+    }
+    if constexpr (YF) {
+        *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.y) + size_t(t) * a.H + h) = make_float4(s[0], s[1], s[2], s[3]);
+    } else {
+        union {
+            __bf16 b[8];
+            uint4 v;
+        } o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o.b[i] = __bf16(s[i]);
+        *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.y) + size_t(t) * a.H + h) = o.v;
     }
 }
 
@@ -565,7 +592,7 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
     const int row = rb * kTileRows + 4 * q + wave;
     if (!live || row >= a.I) return;
     const float w = k < a.K ? a.w[c * a.K + k] : 1.f;
-    const float h = gsum / (1.f + expf(-gsum)) * usum * w;
+    const float h = silu(gsum) * usum * w;
     constexpr int NP = Pieces<YF>::N;
     __bf16* o = reinterpret_cast<__bf16*>(a.act) + size_t(c * a.ks + k) * NP * a.I + row;
     if constexpr (YF) {
@@ -716,7 +743,7 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
         y.cnt = take(size_t(E + ns) * sizeof(int32_t));
         y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
         y.ntiles = take(sizeof(int32_t));
-        y.part = take(n * H * sizeof(float));
+        y.part = take(n * H * (ydtype == STMOE_F32 ? 4 : 2));
         if (dtype == STMOE_F32) y.xs = take(size_t(T) * H * 2 * sizeof(uint16_t));
     }
     y.total = off;
@@ -775,7 +802,8 @@ int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream
     else if (L.tm == 32) rc = launch_tiles<XF, YF, 2>(a, L, s, ev_mid);
     else rc = launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
     if (rc) return rc;
-    hipLaunchKernelGGL((mx_sum_kernel<YF>), dim3(unsigned(a.T)), dim3(kThreads), 0, s, a);
+    const unsigned sb = unsigned((a.H + kThreads * (YF ? 4 : 8) - 1) / (kThreads * (YF ? 4 : 8)));
+    hipLaunchKernelGGL((mx_sum_kernel<YF>), dim3(sb, unsigned(a.T)), dim3(kThreads), 0, s, a);
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
@@ -813,7 +841,7 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
     a.nslots = reinterpret_cast<int32_t*>(base + L.nslots);
     a.arrived = reinterpret_cast<int32_t*>(base + L.arrived);
     a.split = reinterpret_cast<float*>(base + L.split);
-    a.part = reinterpret_cast<float*>(base + L.part);
+    a.part = base + L.part;
     a.n_experts = n_experts;
     const bool xf = dtype == STMOE_F32, yf = ydtype == STMOE_F32;
     if (T <= kMaxB) {
