@@ -229,18 +229,21 @@ __global__ __launch_bounds__(kThreads) void mx_split_kernel(const float* x, int6
     }
 }
 
-// Blobs are read through pointers to global memory: a load through a generic
-// pointer counts as an LDS access too, and every wait for LDS would wait for
-// the weights in flight.
-typedef const __attribute__((address_space(1))) char* GlobalBytes;
-template <class T>
-__device__ __forceinline__ T load_global(GlobalBytes p) {
-    return *(const __attribute__((address_space(1))) T*)p;
+// A blob as a buffer: its address and size in scalar registers, a uniform
+// offset and the lane's, and nothing read beyond its end.  (A load through a
+// generic pointer would count as an LDS access too, and every wait for LDS
+// would wait for the weights in flight.)
+typedef __amdgpu_buffer_rsrc_t BlobRef;
+
+__device__ __forceinline__ BlobRef expert_blob(const MxArgs& a, const Blob& L, int g) {
+    const void* p = g < a.E ? a.eptr[g] : a.sptr[g - a.E];
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(uint32_t(L.total)), 0x00027000);
 }
 
-__device__ __forceinline__ GlobalBytes expert_blob(const MxArgs& a, int g) {
-    return (GlobalBytes)(g < a.E ? a.eptr[g] : a.sptr[g - a.E]);
+__device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lane) {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, int(lane * 16u), int(at), 0);
 }
+
 
 // ---------------------------------------------------------------- prompts
 //
@@ -256,22 +259,23 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     constexpr int TM = 16 * NT;
     constexpr int RB = 4;                                   // row blocks per wave
     constexpr int CH = kTileCols / 8;                       // chunks per column
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    GlobalBytes blobp = expert_blob(a, tl.x);
+    const uint32_t lane = threadIdx.x & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Blob L = blob(a.H, a.I);
+    const BlobRef ref = expert_blob(a, L, tl.x);
     const int C = UP ? a.H : a.I, R = UP ? a.I : a.H;
     const int KT = col_tiles(C), KG = col_groups(C), NB = row_blocks(R);
     if (tid < TM) ent[tid] = a.order[size_t(tl.x) * a.T + tl.y + min(tid, tl.z - 1)];
     // the wave's row blocks; beyond the matrix the last one again, not stored
-    GlobalBytes wc[RB], wsc[RB];
+    uint32_t wc[RB], wsc[RB];
     int rb[RB];
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
         rb[i] = UP ? bk * 8 + wave * 2 + (i & 1) : bk * 16 + wave * 4 + i;
         const int b = min(rb[i], NB - 1);
         const size_t co = UP ? (i < 2 ? L.gate : L.up) : L.down, so = UP ? (i < 2 ? L.gate_s : L.up_s) : L.down_s;
-        wc[i] = blobp + co + size_t(b) * KT * kTileBytes;
-        wsc[i] = blobp + so + size_t(b) * KG * kGroupBytes;
+        wc[i] = uint32_t(co) + uint32_t(b * KT) * kTileBytes;
+        wsc[i] = uint32_t(so) + uint32_t(b * KG) * kGroupBytes;
     }
     __syncthreads();
     // thread: chunk tid % 16 of tokens tid / 16 + 16 j
@@ -297,8 +301,9 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         for (int j = 0; j < NT; ++j) xr[j] = cols[src[j] + off];
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-            wn[i] = load_global<u32x4>(wc[i] + size_t(kt) * kTileBytes + lane * 16);
-            sn[i] = load_global<uint8_t>(wsc[i] + size_t(kt / kGroupTiles) * kGroupBytes + kt % kGroupTiles + lane * 4);
+            wn[i] = load_codes(ref, wc[i] + uint32_t(kt) * kTileBytes, lane);
+            sn[i] = __builtin_amdgcn_raw_buffer_load_b8(
+                ref, int(lane * 4u), int(wsc[i] + uint32_t(kt / kGroupTiles) * kGroupBytes + uint32_t(kt % kGroupTiles)), 0);
         }
     };
     f32x4 acc[RB][NT];
@@ -306,7 +311,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     for (int i = 0; i < RB; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int c = lane & 15, q = lane >> 4, iters = KT * NP;
+    const int c = int(lane & 15), q = int(lane >> 4), iters = KT * NP;
     load(0);
 #pragma unroll
     for (int j = 0; j < NT; ++j) xs[put + j * 16 * CH] = xr[j];
@@ -321,22 +326,27 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         __syncthreads();
         if (it + 1 < iters) load(it + 1);
         const u32x4* buf = xs + (it & 1) * TM * CH + c * CH;
+        union Column {
+            u32x4 u;
+            bf16x8 v;
+        } b[2][NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) b[0][n].u = buf[n * 16 * CH + ((q * 4) ^ c)];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
+            // the next columns are on their way while these are used
+            if (s < 3) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) b[(s + 1) & 1][n].u = buf[n * 16 * CH + ((q * 4 + s + 1) ^ c)];
+            }
             bf16x8 wv[RB];
 #pragma unroll
             for (int i = 0; i < RB; ++i) wv[i] = decode8(w[i][s], sc[i]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                union {
-                    u32x4 u;
-                    bf16x8 v;
-                } b;
-                b.u = buf[n * 16 * CH + ((q * 4 + s) ^ c)];
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < RB; ++i)
-                    acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], b.v, acc[i][n], 0, 0, 0);
-            }
+                    acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], b[s & 1][n].v, acc[i][n], 0, 0, 0);
         }
         if (it + 1 < iters) {
 #pragma unroll
@@ -395,7 +405,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 }
 
 template <bool UP, int NP, int NT, bool YF>
-__global__ __launch_bounds__(kThreads, NT == 8 ? 2 : 1) void mx_tile_kernel(MxArgs a, int nb) {
+__global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) {
     constexpr int TM = 16 * NT;
     __shared__ u32x4 xs[2][TM * kTileCols / 8];
     __shared__ int ent[TM];
@@ -471,12 +481,13 @@ struct Unit {
 
 // Unit u of a row block whose codes and scales begin at c and s.  A missing
 // last tile repeats the one before it (its columns' operands are zero).
-__device__ __forceinline__ Unit load_unit(GlobalBytes c, GlobalBytes s, int u, int KT, int lane) {
+__device__ __forceinline__ Unit load_unit(BlobRef ref, uint32_t c, uint32_t s, int u, int KT, uint32_t lane) {
     Unit r;
     const int t = u * kUnitTiles, t1 = t + 1 < KT ? t + 1 : t;
-    r.c[0] = load_global<u32x4>(c + size_t(t) * kTileBytes + lane * 16);
-    r.c[1] = load_global<u32x4>(c + size_t(t1) * kTileBytes + lane * 16);
-    const uint32_t v = load_global<uint16_t>(s + size_t(t / kGroupTiles) * kGroupBytes + lane * 4 + t % kGroupTiles);
+    r.c[0] = load_codes(ref, c + uint32_t(t) * kTileBytes, lane);
+    r.c[1] = load_codes(ref, c + uint32_t(t1) * kTileBytes, lane);
+    const uint32_t v = __builtin_amdgcn_raw_buffer_load_b16(
+        ref, int(lane * 4u), int(s + uint32_t(t / kGroupTiles) * kGroupBytes + uint32_t(t % kGroupTiles)), 0);
     r.s = t1 == t ? v & 0xffu : v;
     return r;
 }
@@ -486,7 +497,7 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
     __shared__ uint32_t present[kMaxE / 32];
     __shared__ int entry[kMaxB * kMaxK];
     __shared__ float red[kWaves][2][4][64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int slot = blockIdx.x / nrb, rb = blockIdx.x % nrb;
     // the slot's expert: the slot-th of those present, then the shared ones
     if (tid < kMaxE / 32) present[tid] = 0u;
@@ -517,17 +528,17 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
         if (slot - total >= a.ns) return;
         g = a.E + slot - total;
     }
-    GlobalBytes blobp = expert_blob(a, g);
     const Blob L = blob(a.H, a.I);
+    const BlobRef ref = expert_blob(a, L, g);
     const int KT = col_tiles(a.H), KG = col_groups(a.H), KU = (KT + kUnitTiles - 1) / kUnitTiles;
-    GlobalBytes gc = blobp + L.gate + size_t(rb) * KT * kTileBytes;
-    GlobalBytes uc = blobp + L.up + size_t(rb) * KT * kTileBytes;
-    GlobalBytes gs = blobp + L.gate_s + size_t(rb) * KG * kGroupBytes;
-    GlobalBytes us = blobp + L.up_s + size_t(rb) * KG * kGroupBytes;
+    const uint32_t gc = uint32_t(L.gate) + uint32_t(rb * KT) * kTileBytes;
+    const uint32_t uc = uint32_t(L.up) + uint32_t(rb * KT) * kTileBytes;
+    const uint32_t gs = uint32_t(L.gate_s) + uint32_t(rb * KG) * kGroupBytes;
+    const uint32_t us = uint32_t(L.up_s) + uint32_t(rb * KG) * kGroupBytes;
     Unit ng{}, nu{};
     if (wave < KU) {
-        ng = load_unit(gc, gs, wave, KT, lane);
-        nu = load_unit(uc, us, wave, KT, lane);
+        ng = load_unit(ref, gc, gs, wave, KT, lane);
+        nu = load_unit(ref, uc, us, wave, KT, lane);
     }
     // lane: token c; its first entry that selects the expert
     const int c = lane & 15, q = lane >> 4;
@@ -558,8 +569,8 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
                 xr[j][s] = load_raw<XF>(a.x, xrow + at, live && at < a.H);
             }
         if (u + kWaves < KU) {
-            ng = load_unit(gc, gs, u + kWaves, KT, lane);
-            nu = load_unit(uc, us, u + kWaves, KT, lane);
+            ng = load_unit(ref, gc, gs, u + kWaves, KT, lane);
+            nu = load_unit(ref, uc, us, u + kWaves, KT, lane);
         }
 #pragma unroll
         for (int j = 0; j < kUnitTiles; ++j) {
@@ -609,33 +620,41 @@ __global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
 template <bool YF, bool PC>
 __global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int splits) {
     constexpr int NP = Pieces<YF>::N, MP = PC ? 1 : NP;     // pieces; instructions per operand
-    __shared__ GlobalBytes base[kMaxE + kMaxShared];
+    __shared__ const void* base[kMaxE + kMaxShared];
     __shared__ uint8_t sk[kMaxE + kMaxShared][kMaxB];
     __shared__ float red[kDownWaves][4][64];
     __shared__ int last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rb = blockIdx.x / splits, sp = blockIdx.x % splits;
     const int S = *a.nslots;
     for (int s = tid; s < S; s += 64 * kDownWaves) {
         const DecodeSlot d = a.slots[s];
-        base[s] = expert_blob(a, d.g);
+        base[s] = d.g < a.E ? a.eptr[d.g] : a.sptr[d.g - a.E];
 #pragma unroll
         for (int t = 0; t < kMaxB; ++t) sk[s][t] = d.k[t];
     }
     __syncthreads();
     const Blob L = blob(a.H, a.I);
     const int KT = col_tiles(a.I), KG = col_groups(a.I), KU = (KT + kUnitTiles - 1) / kUnitTiles;
-    const size_t co = L.down + size_t(rb) * KT * kTileBytes, so = L.down_s + size_t(rb) * KG * kGroupBytes;
+    const uint32_t co = uint32_t(L.down) + uint32_t(rb * KT) * kTileBytes;
+    const uint32_t so = uint32_t(L.down_s) + uint32_t(rb * KG) * kGroupBytes;
+    // unit u of all slots' (uniform within a wave)
+    auto load = [&](int u) __attribute__((always_inline)) {
+        const int s = u / KU;
+        const uint64_t p = reinterpret_cast<uint64_t>(base[s]);
+        const uint64_t w = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(p >> 32)))) << 32 |
+                           uint32_t(__builtin_amdgcn_readfirstlane(int(p)));
+        const BlobRef ref =
+            __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(w), 0, int(uint32_t(L.total)), 0x00027000);
+        return load_unit(ref, co, so, u - s * KU, KT, lane);
+    };
     const int c = lane & 15, q = lane >> 4;
     const int t = PC ? c >> 1 : c, pc = PC ? c & 1 : 0;
     const int units = S * KU, step = splits * kDownWaves;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     Unit nx{};
     int u = sp * kDownWaves + wave;
-    if (u < units) {
-        const int s = u / KU;
-        nx = load_unit(base[s] + co, base[s] + so, u - s * KU, KT, lane);
-    }
+    if (u < units) nx = load(u);
     for (; u < units; u += step) {
         const Unit cur = nx;
         const int slot = u / KU, t0 = (u - slot * KU) * kUnitTiles;
@@ -652,10 +671,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int 
                     const int at = (t0 + j) * kTileCols + q * kBlock + s * 8;
                     h[j][s][p] = load_raw<false>(a.act, arow + size_t(p) * a.I + at, live && at < a.I);
                 }
-        if (u + step < units) {
-            const int s = (u + step) / KU;
-            nx = load_unit(base[s] + co, base[s] + so, u + step - s * KU, KT, lane);
-        }
+        if (u + step < units) nx = load(u + step);
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < kUnitTiles; ++j) {
@@ -718,7 +734,7 @@ int down_splits(int H) {
 // Tokens per tile: by the tokens an expert gets on average.
 int tile_tokens(int T, int K, int E) {
     const int mean = T * K / E;
-    return mean > 64 ? 128 : mean > 32 ? 64 : mean > 16 ? 32 : 16;
+    return mean > 32 ? 64 : mean > 16 ? 32 : 16;
 }
 
 MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydtype) {
@@ -797,8 +813,7 @@ int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream
         a.x = xs;
     }
     int rc = STMOE_OK;
-    if (L.tm == 128) rc = launch_tiles<XF, YF, 8>(a, L, s, ev_mid);
-    else if (L.tm == 64) rc = launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
+    if (L.tm == 64) rc = launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
     else if (L.tm == 32) rc = launch_tiles<XF, YF, 2>(a, L, s, ev_mid);
     else rc = launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
     if (rc) return rc;
