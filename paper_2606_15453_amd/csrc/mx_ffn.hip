@@ -31,13 +31,14 @@ struct MxArgs {
     void* y;                        // [T][H]
     int T, K, H, I, E, ns, ks;      // ks = K + ns: entries per token
     int tm;                         // tokens per tile
+    int tsplits;                    // parts of the down launch's contraction
     // workspace
     int32_t* order;                 // [expert][T] its entries (t * ks + k)
     int32_t* cnt;                   // [expert] how many
     int4* tiles;                    // (expert, first place in its order, tokens, -)
     int32_t* ntiles;
     uint16_t* act;                  // [entry][piece][I] bf16 pieces
-    void* part;                     // [entry][H] terms of y, of its type
+    void* part;                     // [part][entry][H] terms of y
     // decode steps (T <= 16)
     struct DecodeSlot* slots;       // by ascending expert, the shared ones last
     int32_t* nslots;
@@ -135,7 +136,7 @@ __device__ __forceinline__ int entry_expert(const MxArgs& a, int t, int k) {
 // Entries of one expert per workgroup, by token: order[g * T ..] and cnt[g].
 __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     constexpr int W = kPlanThreads / 64;
-    __shared__ int found[2][W];
+    __shared__ int found[2][64];
     const int g = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t* out = a.order + size_t(g) * a.T;
     if (g >= a.E) {
@@ -143,38 +144,54 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
         if (threadIdx.x == 0) a.cnt[g] = a.T;
         return;
     }
-    // a token per thread: the first of its entries that names the expert
+    // four tokens per thread and step: the first of a token's entries that
+    // names the expert
+    constexpr int U = 4;
     const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
     int before = 0;
-    for (int t0 = 0, par = 0; t0 < a.T; t0 += kPlanThreads, par ^= 1) {
-        const int t = t0 + threadIdx.x;
-        int k = -1;
-        if (t < a.T) {
-            const int32_t* row = a.idx + size_t(t) * a.K;
+    for (int t0 = 0, par = 0; t0 < a.T; t0 += U * kPlanThreads, par ^= 1) {
+        int k[U];
+        unsigned long long m[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * kPlanThreads + threadIdx.x;
+            const int32_t* row = a.idx + size_t(t < a.T ? t : 0) * a.K;
+            k[u] = -1;
             if (four) {
 #pragma unroll
                 for (int j = kMaxK - 4; j >= 0; j -= 4)
                     if (j < a.K) {
                         const int4 e = *reinterpret_cast<const int4*>(row + j);
-                        k = e.x == g ? j : e.y == g ? j + 1 : e.z == g ? j + 2 : e.w == g ? j + 3 : k;
+                        k[u] = e.x == g ? j : e.y == g ? j + 1 : e.z == g ? j + 2 : e.w == g ? j + 3 : k[u];
                     }
             } else {
 #pragma unroll
                 for (int j = kMaxK - 1; j >= 0; --j)
-                    if (j < a.K && row[j] == g) k = j;
+                    if (j < a.K && row[j] == g) k[u] = j;
             }
+            if (t >= a.T) k[u] = -1;
         }
-        const unsigned long long m = __ballot(k >= 0);
-        if (lane == 0) found[par][wave] = __popcll(m);
-        __syncthreads();
-        int base = before;
 #pragma unroll
-        for (int v = 0; v < W; ++v) {
-            const int c = found[par][v];
-            base += v < wave ? c : 0;
-            before += c;
+        for (int u = 0; u < U; ++u) {
+            m[u] = __ballot(k[u] >= 0);
+            if (lane == 0) found[par][u * W + wave] = __popcll(m[u]);
         }
-        if (k >= 0) out[base + __popcll(m & ((1ull << lane) - 1ull))] = t * a.ks + k;
+        __syncthreads();
+        // lane: the count of place u * W + wave before its own
+        int c = found[par][lane];
+        static_assert(U * W == 64, "one place per lane");
+        int sum = c;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += o;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int base = before + __shfl(sum - c, u * W + wave, 64);
+            if (k[u] >= 0)
+                out[base + __popcll(m[u] & ((1ull << lane) - 1ull))] = (t0 + u * kPlanThreads + int(threadIdx.x)) * a.ks + k[u];
+        }
+        before += __shfl(sum, 63, 64);
     }
     if (threadIdx.x == 0) a.cnt[g] = before;
 }
@@ -254,8 +271,8 @@ __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lan
 // through LDS, 128 at a time, double-buffered.  A column's 256 bytes lie as 16
 // chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
 // lanes of a read, one chunk of 16 tokens, meet 16 different places.
-template <bool UP, int NP, int NT, bool YF>
-__device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, u32x4* xs, int* ent) {
+template <bool UP, int NP, int NT, bool F32>
+__device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, int sp, u32x4* xs, int* ent) {
     constexpr int TM = 16 * NT;
     constexpr int RB = 4;                                   // row blocks per wave
     constexpr int CH = kTileCols / 8;                       // chunks per column
@@ -311,11 +328,13 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     for (int i = 0; i < RB; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int c = int(lane & 15), q = int(lane >> 4), iters = KT * NP;
-    load(0);
+    const int c = int(lane & 15), q = int(lane >> 4);
+    // the workgroup's share of the contraction
+    const int it0 = UP ? 0 : KT * sp / a.tsplits * NP, iters = UP ? KT * NP : KT * (sp + 1) / a.tsplits * NP;
+    load(it0);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) xs[put + j * 16 * CH] = xr[j];
-    for (int it = 0; it < iters; ++it) {
+    for (int j = 0; j < NT; ++j) xs[(it0 & 1) * TM * CH + put + j * 16 * CH] = xr[j];
+    for (int it = it0; it < iters; ++it) {
         u32x4 w[RB];
         float sc[RB];
 #pragma unroll
@@ -359,7 +378,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         if (16 * n + c >= tl.z) continue;
         const int e = ent[16 * n + c];
         if constexpr (UP) {
-            constexpr int NH = Pieces<YF>::N;
+            constexpr int NH = Pieces<F32>::N;
 #pragma unroll
             for (int i = 0; i < RB / 2; ++i) {
                 const int row = rb[i] * kTileRows + 4 * q;
@@ -371,7 +390,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float g = acc[i][n][r], v = silu(g) * acc[i + 2][n][r];
-                    if constexpr (YF) split(v, o[0].h[r], o[1].h[r]);
+                    if constexpr (F32) split(v, o[0].h[r], o[1].h[r]);
                     else o[0].h[r] = __bf16(v);
                 }
 #pragma unroll
@@ -386,8 +405,8 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
                 const int row = rb[i] * kTileRows + 4 * q;
                 if (row >= a.H) continue;
                 const f32x4 d = acc[i][n];
-                const size_t at = size_t(e) * a.H + row;
-                if constexpr (YF) {
+                const size_t at = (size_t(sp) * a.T * a.ks + e) * a.H + row;
+                if constexpr (F32) {
                     *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.part) + at) =
                         make_float4(w * d[0], w * d[1], w * d[2], w * d[3]);
                 } else {
@@ -404,7 +423,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     }
 }
 
-template <bool UP, int NP, int NT, bool YF>
+template <bool UP, int NP, int NT, bool F32>
 __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) {
     constexpr int TM = 16 * NT;
     __shared__ u32x4 xs[2][TM * kTileCols / 8];
@@ -414,42 +433,49 @@ __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) 
     const int work = *a.ntiles * nb, per = (work + 7) / 8;
     const int id = int(blockIdx.x % 8) * per + int(blockIdx.x / 8);
     if (int(blockIdx.x / 8) >= per || id >= work) return;
-    const int tix = id / nb;
+    const int tix = id / nb, rest = id - tix * nb, sp = UP ? 0 : rest % a.tsplits, bk = UP ? rest : rest / a.tsplits;
     const int4 tl = a.tiles[tix];
     if constexpr (NT > 1) {
         // an expert's last tile, if at most half full, in half the instructions
-        if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, YF>(a, tl, id - tix * nb, xs[0], ent);
+        if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, F32>(a, tl, bk, sp, xs[0], ent);
     }
-    tile_product<UP, NP, NT, YF>(a, tl, id - tix * nb, xs[0], ent);
+    tile_product<UP, NP, NT, F32>(a, tl, bk, sp, xs[0], ent);
 }
 
-// y[t] = the sum of its entries' terms, in the entries' order, in fp32.  The
-// terms are of y's type: with bf16 y each is rounded once (2^-8 of itself at
-// most, as y is), which halves what the down launch writes and this one reads.
-template <bool YF>
-__global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a) {
-    constexpr int V = YF ? 4 : 8;           // 16 bytes of terms
-    const int t = blockIdx.y;
-    const int h = (blockIdx.x * kThreads + threadIdx.x) * V;
+// y[t] = the sum of its entries' terms, in the entries' order, in fp32.  With
+// bf16 y and an undivided contraction the terms are bf16 (TF false): each is
+// rounded once, by 2^-8 of itself at most, as y is, which halves what the down
+// launch writes and this one reads.
+template <bool TF, bool YF>
+__global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
+    constexpr int V = 8;
+    const int t = blockIdx.x / nb;
+    const int h = ((blockIdx.x - t * nb) * kThreads + threadIdx.x) * V;
     if (h >= a.H) return;
     float s[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s[i] = 0.f;
+    for (int sp = 0; sp < a.tsplits; ++sp) {
 #pragma unroll 4
-    for (int k = 0; k < a.ks; ++k) {
-        if (entry_expert(a, t, k) < 0) continue;
-        const size_t at = (size_t(t) * a.ks + k) * a.H + h;
-        if constexpr (YF) {
-            const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.part) + at);
-            s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
-        } else {
-            const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.part) + at);
-            s[0] += bf16_lo(v.x); s[1] += bf16_hi(v.x); s[2] += bf16_lo(v.y); s[3] += bf16_hi(v.y);
-            s[4] += bf16_lo(v.z); s[5] += bf16_hi(v.z); s[6] += bf16_lo(v.w); s[7] += bf16_hi(v.w);
+        for (int k = 0; k < a.ks; ++k) {
+            if (entry_expert(a, t, k) < 0) continue;
+            const size_t at = ((size_t(sp) * a.T + t) * a.ks + k) * a.H + h;
+            if constexpr (TF) {
+                const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.part) + at);
+                const float4 u = p[0], v = p[1];
+                s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+                s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+            } else {
+                const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.part) + at);
+                s[0] += bf16_lo(v.x); s[1] += bf16_hi(v.x); s[2] += bf16_lo(v.y); s[3] += bf16_hi(v.y);
+                s[4] += bf16_lo(v.z); s[5] += bf16_hi(v.z); s[6] += bf16_lo(v.w); s[7] += bf16_hi(v.w);
+            }
         }
     }
     if constexpr (YF) {
-        *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.y) + size_t(t) * a.H + h) = make_float4(s[0], s[1], s[2], s[3]);
+        float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.y) + size_t(t) * a.H + h);
+        o[0] = make_float4(s[0], s[1], s[2], s[3]);
+        o[1] = make_float4(s[4], s[5], s[6], s[7]);
     } else {
         union {
             __bf16 b[8];
@@ -721,7 +747,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int 
 }
 
 struct MxLayout {
-    int tm, max_tiles, slots, splits;
+    int tm, max_tiles, tsplits, slots, splits;
     size_t order, cnt, tiles, ntiles, act, part, xs, plan, nslots, arrived, split, total;
 };
 
@@ -735,6 +761,14 @@ int down_splits(int H) {
 int tile_tokens(int T, int K, int E) {
     const int mean = T * K / E;
     return mean > 32 ? 64 : mean > 16 ? 32 : 16;
+}
+
+// Parts of the down launch's contraction: enough for 768 workgroups (three per
+// CU) if half of the experts' last tiles are filled, of four column tiles at least.
+int tile_splits(int tm, size_t n, int E, int ns, int H, int I) {
+    const size_t wg = (n / tm + (E + ns) / 2 + 1) * size_t((H + 255) / 256);
+    const int want = wg >= 768 ? 1 : int(768 / wg), most = col_tiles(I) / 4;
+    return want < 1 ? 1 : most < 1 ? 1 : want < most ? want : most;
 }
 
 MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydtype) {
@@ -759,7 +793,8 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
         y.cnt = take(size_t(E + ns) * sizeof(int32_t));
         y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
         y.ntiles = take(sizeof(int32_t));
-        y.part = take(n * H * (ydtype == STMOE_F32 ? 4 : 2));
+        y.tsplits = tile_splits(y.tm, n, E, ns, H, I);
+        y.part = take(n * y.tsplits * H * (ydtype == STMOE_F32 || y.tsplits > 1 ? 4 : 2));
         if (dtype == STMOE_F32) y.xs = take(size_t(T) * H * 2 * sizeof(uint16_t));
     }
     y.total = off;
@@ -789,11 +824,21 @@ template <bool XF, bool YF, int NT>
 int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t ev_mid) {
     // rounded up to the eight XCDs
     const auto grid = [&](int nb) { return dim3(unsigned((int64_t(L.max_tiles) * nb + 7) / 8 * 8)); };
-    const int ub = (a.I + 127) / 128, db = (a.H + 255) / 256;
-    hipLaunchKernelGGL((mx_tile_kernel<true, XF ? 2 : 1, NT, YF>), grid(ub), dim3(kThreads), 0, s, a, ub);
+    const int ub = (a.I + 127) / 128, db = (a.H + 255) / 256 * L.tsplits;
+    const int sb = (a.H + kThreads * 8 - 1) / (kThreads * 8);
+    const dim3 sgrid(unsigned(a.T) * unsigned(sb)), block(kThreads);
+    hipLaunchKernelGGL((mx_tile_kernel<true, XF ? 2 : 1, NT, YF>), grid(ub), block, 0, s, a, ub);
     STMOE_LAUNCHED();
     if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
-    hipLaunchKernelGGL((mx_tile_kernel<false, YF ? 2 : 1, NT, YF>), grid(db), dim3(kThreads), 0, s, a, db);
+    if (YF || L.tsplits > 1) {
+        hipLaunchKernelGGL((mx_tile_kernel<false, YF ? 2 : 1, NT, true>), grid(db), block, 0, s, a, db);
+        STMOE_LAUNCHED();
+        hipLaunchKernelGGL((mx_sum_kernel<true, YF>), sgrid, block, 0, s, a, sb);
+    } else {
+        hipLaunchKernelGGL((mx_tile_kernel<false, 1, NT, false>), grid(db), block, 0, s, a, db);
+        STMOE_LAUNCHED();
+        hipLaunchKernelGGL((mx_sum_kernel<false, false>), sgrid, block, 0, s, a, sb);
+    }
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
@@ -812,15 +857,9 @@ int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream
         STMOE_LAUNCHED();
         a.x = xs;
     }
-    int rc = STMOE_OK;
-    if (L.tm == 64) rc = launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
-    else if (L.tm == 32) rc = launch_tiles<XF, YF, 2>(a, L, s, ev_mid);
-    else rc = launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
-    if (rc) return rc;
-    const unsigned sb = unsigned((a.H + kThreads * (YF ? 4 : 8) - 1) / (kThreads * (YF ? 4 : 8)));
-    hipLaunchKernelGGL((mx_sum_kernel<YF>), dim3(sb, unsigned(a.T)), dim3(kThreads), 0, s, a);
-    STMOE_LAUNCHED();
-    return STMOE_OK;
+    if (L.tm == 64) return launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
+    if (L.tm == 32) return launch_tiles<XF, YF, 2>(a, L, s, ev_mid);
+    return launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
 }
 
 }  // namespace
@@ -847,6 +886,7 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
     a.ns = n_shared;
     a.ks = K + n_shared;
     a.tm = L.tm;
+    a.tsplits = L.tsplits;
     a.order = reinterpret_cast<int32_t*>(base + L.order);
     a.cnt = reinterpret_cast<int32_t*>(base + L.cnt);
     a.tiles = reinterpret_cast<int4*>(base + L.tiles);
