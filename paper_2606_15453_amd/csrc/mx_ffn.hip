@@ -133,10 +133,54 @@ __device__ __forceinline__ int entry_expert(const MxArgs& a, int t, int k) {
     return e;
 }
 
-// Entries of one expert per workgroup, by token: order[g * T ..] and cnt[g].
+// A barrier for what passes through LDS alone: __syncthreads would also wait
+// for the stores to memory under way (3 us for 1024 scattered ones).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The tiles of at most tm tokens, experts in order (one workgroup; cnt in LDS).
+__device__ __forceinline__ void list_tiles(const MxArgs& a, const int* cnt, int* tile) {
+    const int tid = threadIdx.x, G = a.E + a.ns;
+    if (tid < 64) {
+        // running sums of the tile counts, 64 experts at a time
+        int before = 0, used = 0;
+        for (int g0 = 0; g0 < G; g0 += 64) {
+            const int g = g0 + tid, c = g < G ? cnt[g] : 0;
+            int v = (c + a.tm - 1) / a.tm;
+            used += __popcll(__ballot(c > 0 && g < a.E));
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(v, d, 64);
+                if (tid >= d) v += o;
+            }
+            if (g < G) tile[g + 1] = before + v;
+            before += __shfl(v, 63, 64);
+        }
+        if (tid == 0) {
+            tile[0] = 0;
+            *a.ntiles = before;
+            if (a.n_experts) *a.n_experts += (unsigned long long)(used);
+        }
+    }
+    __syncthreads();
+    for (int g = tid >> 4; g < G; g += kPlanThreads >> 4)
+        for (int j = tid & 15; j * a.tm < cnt[g]; j += 16)
+            a.tiles[tile[g] + j] = make_int4(g, j * a.tm, min(a.tm, cnt[g] - j * a.tm), 0);
+}
+
+__global__ __launch_bounds__(kPlanThreads) void mx_tiles_kernel(MxArgs a) {
+    __shared__ int cnt[kMaxGroups], tile[kMaxGroups + 1];
+    for (int g = threadIdx.x; g < a.E + a.ns; g += kPlanThreads) cnt[g] = a.cnt[g];
+    __syncthreads();
+    list_tiles(a, cnt, tile);
+}
+
+// One expert's entries per workgroup, by token: order[g * T ..] and cnt[g].  A
+// thread compares its token's KU entries (FOUR: K is a multiple of four and
+// they are loaded four at a time) and takes the first that names the expert;
+// a wave's place is its lanes' ballot, the waves' places meet in LDS.
+template <int KU, bool FOUR>
 __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     constexpr int W = kPlanThreads / 64;
-    __shared__ int found[2][64];
+    __shared__ int found[2][W];
     const int g = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t* out = a.order + size_t(g) * a.T;
     if (g >= a.E) {
@@ -144,88 +188,123 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
         if (threadIdx.x == 0) a.cnt[g] = a.T;
         return;
     }
-    // four tokens per thread and step: the first of a token's entries that
-    // names the expert
-    constexpr int U = 4;
-    const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
     int before = 0;
-    for (int t0 = 0, par = 0; t0 < a.T; t0 += U * kPlanThreads, par ^= 1) {
-        int k[U];
-        unsigned long long m[U];
+    for (int t0 = 0, par = 0; t0 < a.T; t0 += kPlanThreads, par ^= 1) {
+        const int t = t0 + threadIdx.x;
+        const int32_t* row = a.idx + size_t(min(t, a.T - 1)) * a.K;
+        int k = -1;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int t = t0 + u * kPlanThreads + threadIdx.x;
-            const int32_t* row = a.idx + size_t(t < a.T ? t : 0) * a.K;
-            k[u] = -1;
-            if (four) {
-#pragma unroll
-                for (int j = kMaxK - 4; j >= 0; j -= 4)
-                    if (j < a.K) {
-                        const int4 e = *reinterpret_cast<const int4*>(row + j);
-                        k[u] = e.x == g ? j : e.y == g ? j + 1 : e.z == g ? j + 2 : e.w == g ? j + 3 : k[u];
-                    }
+        for (int j = KU - (FOUR ? 4 : 1); j >= 0; j -= FOUR ? 4 : 1) {
+            // beyond K the last entry again, which does not count there
+            if constexpr (FOUR) {
+                const int4 e = *reinterpret_cast<const int4*>(row + min(j, a.K - 4));
+                const int f = e.x == g ? j : e.y == g ? j + 1 : e.z == g ? j + 2 : e.w == g ? j + 3 : -1;
+                k = f >= 0 && j < a.K ? f : k;
             } else {
-#pragma unroll
-                for (int j = kMaxK - 1; j >= 0; --j)
-                    if (j < a.K && row[j] == g) k[u] = j;
+                k = row[min(j, a.K - 1)] == g && j < a.K ? j : k;
             }
-            if (t >= a.T) k[u] = -1;
         }
+        if (t >= a.T) k = -1;
+        const unsigned long long m = __ballot(k >= 0);
+        if (lane == 0) found[par][wave] = __popcll(m);
+        lds_barrier();
+        int base = before;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            m[u] = __ballot(k[u] >= 0);
-            if (lane == 0) found[par][u * W + wave] = __popcll(m[u]);
+        for (int v = 0; v < W; ++v) {
+            const int c = found[par][v];
+            base += v < wave ? c : 0;
+            before += c;
         }
-        __syncthreads();
-        // lane: the count of place u * W + wave before its own
-        int c = found[par][lane];
-        static_assert(U * W == 64, "one place per lane");
-        int sum = c;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += o;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int base = before + __shfl(sum - c, u * W + wave, 64);
-            if (k[u] >= 0)
-                out[base + __popcll(m[u] & ((1ull << lane) - 1ull))] = (t0 + u * kPlanThreads + int(threadIdx.x)) * a.ks + k[u];
-        }
-        before += __shfl(sum, 63, 64);
+        if (k >= 0) out[base + __popcll(m & ((1ull << lane) - 1ull))] = t * a.ks + k;
     }
     if (threadIdx.x == 0) a.cnt[g] = before;
 }
 
-// The tiles of at most tm tokens, experts in order: one workgroup.
-__global__ __launch_bounds__(kPlanThreads) void mx_tiles_kernel(MxArgs a) {
+// All experts' entries and the tiles by one workgroup, 1024 tokens at a time.
+// An expert's tokens are bits of a mask in LDS, a token's place the number of
+// bits below its own; a bit that its thread finds set is a repeated expert.
+// For up to 1024 entries: 4 us, where the two launches above take 3 us each;
+// its CU needs 4 us for every 1024 tokens (4096 tokens of top-8: 25 us).
+// The KU entries are handled side by side, without branches, so that their LDS
+// accesses overlap; entries that name no expert meet a word of their own.
+template <int KU>
+__global__ __launch_bounds__(kPlanThreads) void mx_plan_kernel(MxArgs a) {
+    constexpr int W = kPlanThreads / 32;                    // words of a mask
+    __shared__ uint32_t mask[kMaxE + 2][W];                 // the last two: nobody's
+
+    __shared__ uint16_t below[kMaxE][W];
     __shared__ int cnt[kMaxGroups], tile[kMaxGroups + 1];
-    const int G = a.E + a.ns;
-    for (int g = threadIdx.x; g < G; g += kPlanThreads) cnt[g] = a.cnt[g];
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        // running sums of the tile counts, 64 experts at a time
-        int before = 0, used = 0;
-        for (int g0 = 0; g0 < G; g0 += 64) {
-            const int g = g0 + threadIdx.x, c = g < G ? cnt[g] : 0;
-            int v = (c + a.tm - 1) / a.tm;
-            used += __popcll(__ballot(c > 0 && g < a.E));
-            for (int d = 1; d < 64; d <<= 1) {
-                const int o = __shfl_up(v, d, 64);
-                if (int(threadIdx.x) >= d) v += o;
+    const int tid = threadIdx.x, G = a.E + a.ns;
+    const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
+    for (int g = tid; g < G; g += kPlanThreads) cnt[g] = g < a.E ? 0 : a.T;
+    int e[KU];
+    auto load = [&](int t) __attribute__((always_inline)) {
+        const int32_t* row = a.idx + size_t(t < a.T ? t : 0) * a.K;
+#pragma unroll
+        for (int j = 0; j < KU; j += 4) {
+            int4 v = make_int4(-1, -1, -1, -1);
+            if (four) {
+                if (j < a.K) v = *reinterpret_cast<const int4*>(row + j);
+            } else {
+                if (j < a.K) v.x = row[j];
+                if (j + 1 < a.K) v.y = row[j + 1];
+                if (j + 2 < a.K) v.z = row[j + 2];
+                if (j + 3 < a.K) v.w = row[j + 3];
             }
-            if (g < G) tile[g + 1] = before + v;
-            before += __shfl(v, 63, 64);
+            e[j] = t < a.T ? v.x : -1;
+            e[j + 1] = t < a.T ? v.y : -1;
+            e[j + 2] = t < a.T ? v.z : -1;
+            e[j + 3] = t < a.T ? v.w : -1;
         }
-        if (threadIdx.x == 0) {
-            tile[0] = 0;
-            *a.ntiles = before;
-            if (a.n_experts) *a.n_experts += (unsigned long long)(used);
+    };
+    load(tid);
+    for (int t0 = 0; t0 < a.T; t0 += kPlanThreads) {
+        const int t = t0 + tid, w = tid >> 5;
+        for (int i = tid; i < a.E * W; i += kPlanThreads) mask[0][i] = 0u;
+        lds_barrier();
+        uint32_t* word[KU];
+        bool mine[KU];
+#pragma unroll
+        for (int j = 0; j < KU; ++j) {
+            mine[j] = e[j] >= 0 && e[j] < a.E;
+            word[j] = mine[j] ? &mask[e[j]][w] : &mask[kMaxE][tid & 63];
         }
+        const uint32_t bit = 1u << (tid & 31);
+        uint32_t was[KU];
+#pragma unroll
+        for (int j = 0; j < KU; ++j) was[j] = atomicOr(word[j], mine[j] ? bit : 0u);
+#pragma unroll
+        for (int j = 0; j < KU; ++j) mine[j] &= !(was[j] & bit);
+        if (t0 + kPlanThreads < a.T) load(t + kPlanThreads);
+        lds_barrier();
+        // 32 lanes: an expert's words
+        for (int g = w; g < a.E; g += W) {
+            const int l = tid & 31, c = __builtin_popcount(mask[g][l]);
+            int v = c;
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up(v, d, 32);
+                if (l >= d) v += o;
+            }
+            below[g][l] = uint16_t(v - c);
+        }
+        lds_barrier();
+        int at[KU], to[KU];
+#pragma unroll
+        for (int j = 0; j < KU; ++j) {
+            const int g = mine[j] ? int(word[j] - &mask[0][0]) / W : 0;
+            to[j] = g;
+            at[j] = cnt[g] + below[g][w] + __builtin_popcount(mask[g][w] & (bit - 1u));
+        }
+#pragma unroll
+        for (int j = 0; j < KU; ++j)
+            if (mine[j]) a.order[size_t(to[j]) * a.T + at[j]] = t * a.ks + j;
+        if (t < a.T)
+            for (int s = 0; s < a.ns; ++s) a.order[size_t(a.E + s) * a.T + t] = t * a.ks + a.K + s;
+        lds_barrier();
+        if (tid < a.E) cnt[tid] += below[tid][W - 1] + __builtin_popcount(mask[tid][W - 1]);
+        lds_barrier();
     }
-    __syncthreads();
-    for (int g = threadIdx.x >> 4; g < G; g += kPlanThreads >> 4)
-        for (int j = threadIdx.x & 15; j * a.tm < cnt[g]; j += 16)
-            a.tiles[tile[g] + j] = make_int4(g, j * a.tm, min(a.tm, cnt[g] - j * a.tm), 0);
+    list_tiles(a, cnt, tile);
 }
 
 // fp32 hidden states as two bf16 pieces per row: [T][2][H].
@@ -846,9 +925,20 @@ int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t e
 template <bool XF, bool YF>
 int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream_t s, hipEvent_t ev_mid) {
     MxArgs a = args;
-    hipLaunchKernelGGL(mx_order_kernel, dim3(unsigned(a.E + a.ns)), dim3(kPlanThreads), 0, s, a);
-    STMOE_LAUNCHED();
-    hipLaunchKernelGGL(mx_tiles_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    const dim3 block(kPlanThreads);
+    if (a.T * a.K <= 1024) {
+        if (a.K <= 8) hipLaunchKernelGGL((mx_plan_kernel<8>), dim3(1), block, 0, s, a);
+        else hipLaunchKernelGGL((mx_plan_kernel<16>), dim3(1), block, 0, s, a);
+    } else {
+        const dim3 grid(unsigned(a.E + a.ns));
+        const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
+        if (four && a.K <= 8) hipLaunchKernelGGL((mx_order_kernel<8, true>), grid, block, 0, s, a);
+        else if (four) hipLaunchKernelGGL((mx_order_kernel<16, true>), grid, block, 0, s, a);
+        else if (a.K <= 8) hipLaunchKernelGGL((mx_order_kernel<8, false>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((mx_order_kernel<16, false>), grid, block, 0, s, a);
+        STMOE_LAUNCHED();
+        hipLaunchKernelGGL(mx_tiles_kernel, dim3(1), block, 0, s, a);
+    }
     STMOE_LAUNCHED();
     if constexpr (XF) {
         const int64_t n4 = int64_t(a.T) * a.H / 4, wg = (n4 + kThreads - 1) / kThreads;
