@@ -328,10 +328,11 @@ int moe_mx_pack_expert(const uint8_t* gate_codes, const uint8_t* gate_scales, co
  *                bytes, 256-byte aligned, no initial contents required; calls
  *                sharing it must be ordered on one stream
  * dtype and ydtype: STMOE_BF16 or STMOE_F32 each.  Sums are fp32.  fp32 x, and
- * the activations when y is fp32, enter the products as two bf16 pieces (16
- * significant bits); with bf16 y the activations are rounded to bf16.  The
- * same inputs give the same bits, and a token's result does not depend on the
- * others'. */
+ * the activations when y is fp32, enter the products as bf16 pieces that hold
+ * their 24 bits; with bf16 y the activations are rounded to bf16 (and fp32 x
+ * to 16 bits).  The same inputs give the same bits.  With more than 16 tokens
+ * a token's result does not depend on the other tokens' values; up to 16 the
+ * order of its sums goes by the experts that the call selects. */
 size_t moe_expert_ffn_mx_workspace_bytes(int T, int K, int E, int H, int I, int n_shared, int dtype,
                                          int ydtype);
 int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const float* topk_w, int T, int K, int H,

@@ -5,9 +5,11 @@
 // The weights' values are exact in bf16, so both projections run on the bf16
 // matrix instructions with fp32 accumulation: a lane's 16 code bytes become
 // the row operand in registers, tokens are the columns.  fp32 values (x, and
-// the activations when y is fp32) are split into two bf16 pieces, the value's
-// rounding and the rounding of what is left: 16 significant bits, two
-// instructions per operand.
+// the activations when y is fp32) are split into three bf16 pieces, the
+// value's rounding and twice the rounding of what is left, which hold its 24
+// bits: three instructions per operand.  With bf16 y the activations are
+// rounded to bf16 (2^-8 of themselves at most, as y is) and fp32 x goes in two
+// pieces.
 #include "mx_format.h"
 
 namespace stmoe {
@@ -38,80 +40,79 @@ struct MxArgs {
     int4* tiles;                    // (expert, first place in its order, tokens, -)
     int32_t* ntiles;
     uint16_t* act;                  // [entry][piece][I] bf16 pieces
-    void* part;                     // [part][entry][H] terms of y
+    float* part;                    // [part][entry][H] terms of y
     // decode steps (T <= 16)
     struct DecodeSlot* slots;       // by ascending expert, the shared ones last
     int32_t* nslots;
-    int32_t* arrived;               // [row block of H] workgroups of the down launch that are done
-    float* split;                   // [row block][split][256] their sums
+    int smax;                       // slots at most
+    float* split;                   // [chunk][row block of H][256] sums of the down launch
     unsigned long long* n_experts;  // counts distinct routed experts (timed decode layers), or null
 };
 
-// A distinct expert of a decode step and, per token, the entry that selects it.
-struct DecodeSlot {
-    int32_t g;
-    uint8_t k[kMaxB];               // kNone: the token does not select it
-};
-constexpr int kNone = 255;
+// Pieces of an fp32 value: of x, of an activation.
+template <bool XF, bool YF>
+constexpr int kPiecesX = XF ? (YF ? 3 : 2) : 1;
+template <bool YF>
+constexpr int kPiecesH = YF ? 3 : 1;
 
 // Column operand: eight consecutive values of a row as bf16 pieces.
-template <bool F32>
-struct Pieces;
-template <>
-struct Pieces<false> {
-    static constexpr int N = 1;
-    bf16x8 p[1];
-};
-template <>
-struct Pieces<true> {
-    static constexpr int N = 2;
-    bf16x8 p[2];
+template <int N>
+struct Pieces {
+    bf16x8 p[N];
 };
 
-// A value as two bf16 numbers; infinities and NaN (and what rounds to
-// infinity) keep to the first.  The difference is that of the rounded value:
-// fused with the product that gave v, it would depend on how the compiler
-// arranged the caller, and a token's bits on the tile it falls into.
-__device__ __forceinline__ void split(float v, __bf16& hi, __bf16& lo) {
+// A value as N bf16 numbers; infinities and NaN (and what rounds to infinity)
+// keep to the first.  The differences are those of the rounded values: fused
+// with the product that gave v, they would depend on how the compiler arranged
+// the caller, and a token's bits on the tile it falls into.
+template <int N>
+__device__ __forceinline__ void split(float v, __bf16 (&o)[N]) {
 #pragma clang fp contract(off)
-    hi = __bf16(v);
-    const float h = float(hi);
-    lo = __builtin_isfinite(h) ? __bf16(v - h) : __bf16(0.f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        o[i] = __bf16(v);
+        const float f = float(o[i]);
+        v = __builtin_isfinite(f) ? v - f : 0.f;
+    }
 }
 
 // Eight consecutive values as loaded.
 template <bool F32>
 struct Raw {
-    uint4 q[F32 ? 2 : 1];
+    u32x4 q[F32 ? 2 : 1];
 };
 
 template <bool F32>
 __device__ __forceinline__ Raw<F32> load_raw(const void* x, size_t at, bool in) {
     Raw<F32> r;
-    const uint4* s = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(x) + at * (F32 ? 4 : 2));
+    const u32x4* s = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(x) + at * (F32 ? 4 : 2));
 #pragma unroll
-    for (int i = 0; i < (F32 ? 2 : 1); ++i) r.q[i] = in ? s[i] : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) r.q[i] = in ? s[i] : u32x4{0u, 0u, 0u, 0u};
     return r;
 }
 
-__device__ __forceinline__ Pieces<false> pieces(const Raw<false>& r) {
+__device__ __forceinline__ bf16x8 as_operand(u32x4 q) {
     union {
-        uint4 q;
+        u32x4 q;
         bf16x8 v;
     } u;
-    u.q = r.q[0];
-    return Pieces<false>{{u.v}};
+    u.q = q;
+    return u.v;
 }
 
-__device__ __forceinline__ Pieces<true> pieces(const Raw<true>& r) {
-    Pieces<true> o;
-    const uint32_t w[8] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w, r.q[1].x, r.q[1].y, r.q[1].z, r.q[1].w};
+template <int N>
+__device__ __forceinline__ Pieces<N> pieces(const Raw<(N > 1)>& r) {
+    Pieces<N> o;
+    if constexpr (N == 1) {
+        o.p[0] = as_operand(r.q[0]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        __bf16 h, l;
-        split(__uint_as_float(w[i]), h, l);
-        o.p[0][i] = h;
-        o.p[1][i] = l;
+        for (int i = 0; i < 8; ++i) {
+            __bf16 b[N];
+            split(__uint_as_float(r.q[i / 4][i % 4]), b);
+#pragma unroll
+            for (int p = 0; p < N; ++p) o.p[p][i] = b[p];
+        }
     }
     return o;
 }
@@ -307,21 +308,26 @@ __global__ __launch_bounds__(kPlanThreads) void mx_plan_kernel(MxArgs a) {
     list_tiles(a, cnt, tile);
 }
 
-// fp32 hidden states as two bf16 pieces per row: [T][2][H].
+// fp32 hidden states as bf16 pieces, row by row: [T][N][H].
+template <int N>
 __global__ __launch_bounds__(kThreads) void mx_split_kernel(const float* x, int64_t n4, int H4, uint16_t* o) {
     for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n4; i += int64_t(gridDim.x) * kThreads) {
         const float4 v = reinterpret_cast<const float4*>(x)[i];
-        const int64_t t = i / H4;
+        const int64_t t = i / H4, at = t * N * H4 + (i - t * H4);
         union {
             __bf16 b[4];
             uint2 q;
-        } hi, lo;
-        split(v.x, hi.b[0], lo.b[0]);
-        split(v.y, hi.b[1], lo.b[1]);
-        split(v.z, hi.b[2], lo.b[2]);
-        split(v.w, hi.b[3], lo.b[3]);
-        reinterpret_cast<uint2*>(o)[i + t * H4] = hi.q;
-        reinterpret_cast<uint2*>(o)[i + t * H4 + H4] = lo.q;
+        } u[N];
+        const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            __bf16 b[N];
+            split(f[c], b);
+#pragma unroll
+            for (int p = 0; p < N; ++p) u[p].b[c] = b[p];
+        }
+#pragma unroll
+        for (int p = 0; p < N; ++p) reinterpret_cast<uint2*>(o)[at + int64_t(p) * H4] = u[p].q;
     }
 }
 
@@ -331,9 +337,12 @@ __global__ __launch_bounds__(kThreads) void mx_split_kernel(const float* x, int6
 // would wait for the weights in flight.)
 typedef __amdgpu_buffer_rsrc_t BlobRef;
 
-__device__ __forceinline__ BlobRef expert_blob(const MxArgs& a, const Blob& L, int g) {
-    const void* p = g < a.E ? a.eptr[g] : a.sptr[g - a.E];
+__device__ __forceinline__ BlobRef blob_ref(const void* p, const Blob& L) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(uint32_t(L.total)), 0x00027000);
+}
+
+__device__ __forceinline__ BlobRef expert_blob(const MxArgs& a, const Blob& L, int g) {
+    return blob_ref(g < a.E ? a.eptr[g] : a.sptr[g - a.E], L);
 }
 
 __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lane) {
@@ -350,6 +359,7 @@ __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lan
 // through LDS, 128 at a time, double-buffered.  A column's 256 bytes lie as 16
 // chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
 // lanes of a read, one chunk of 16 tokens, meet 16 different places.
+// F32 (up): the activations keep fp32 precision.
 template <bool UP, int NP, int NT, bool F32>
 __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, int sp, u32x4* xs, int* ent) {
     constexpr int TM = 16 * NT;
@@ -457,7 +467,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         if (16 * n + c >= tl.z) continue;
         const int e = ent[16 * n + c];
         if constexpr (UP) {
-            constexpr int NH = Pieces<F32>::N;
+            constexpr int NH = kPiecesH<F32>;
 #pragma unroll
             for (int i = 0; i < RB / 2; ++i) {
                 const int row = rb[i] * kTileRows + 4 * q;
@@ -468,9 +478,10 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
                 } o[NH];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float g = acc[i][n][r], v = silu(g) * acc[i + 2][n][r];
-                    if constexpr (F32) split(v, o[0].h[r], o[1].h[r]);
-                    else o[0].h[r] = __bf16(v);
+                    __bf16 b[NH];
+                    split(silu(acc[i][n][r]) * acc[i + 2][n][r], b);
+#pragma unroll
+                    for (int p = 0; p < NH; ++p) o[p].h[r] = b[p];
                 }
 #pragma unroll
                 for (int p = 0; p < NH; ++p)
@@ -485,18 +496,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
                 if (row >= a.H) continue;
                 const f32x4 d = acc[i][n];
                 const size_t at = (size_t(sp) * a.T * a.ks + e) * a.H + row;
-                if constexpr (F32) {
-                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.part) + at) =
-                        make_float4(w * d[0], w * d[1], w * d[2], w * d[3]);
-                } else {
-                    union {
-                        __bf16 b[4];
-                        uint2 v;
-                    } o;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o.b[r] = __bf16(w * d[r]);
-                    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.part) + at) = o.v;
-                }
+                *reinterpret_cast<float4*>(a.part + at) = make_float4(w * d[0], w * d[1], w * d[2], w * d[3]);
             }
         }
     }
@@ -521,48 +521,30 @@ __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) 
     tile_product<UP, NP, NT, F32>(a, tl, bk, sp, xs[0], ent);
 }
 
-// y[t] = the sum of its entries' terms, in the entries' order, in fp32.  With
-// bf16 y and an undivided contraction the terms are bf16 (TF false): each is
-// rounded once, by 2^-8 of itself at most, as y is, which halves what the down
-// launch writes and this one reads.
-template <bool TF, bool YF>
+// y[t] = the sum of its entries' terms, in the entries' order.
+template <bool YF>
 __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
-    constexpr int V = 8;
     const int t = blockIdx.x / nb;
-    const int h = ((blockIdx.x - t * nb) * kThreads + threadIdx.x) * V;
+    const int h = ((blockIdx.x - t * nb) * kThreads + threadIdx.x) * 4;
     if (h >= a.H) return;
-    float s[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = 0.f;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int sp = 0; sp < a.tsplits; ++sp) {
 #pragma unroll 4
         for (int k = 0; k < a.ks; ++k) {
             if (entry_expert(a, t, k) < 0) continue;
-            const size_t at = ((size_t(sp) * a.T + t) * a.ks + k) * a.H + h;
-            if constexpr (TF) {
-                const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.part) + at);
-                const float4 u = p[0], v = p[1];
-                s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-                s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
-            } else {
-                const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.part) + at);
-                s[0] += bf16_lo(v.x); s[1] += bf16_hi(v.x); s[2] += bf16_lo(v.y); s[3] += bf16_hi(v.y);
-                s[4] += bf16_lo(v.z); s[5] += bf16_hi(v.z); s[6] += bf16_lo(v.w); s[7] += bf16_hi(v.w);
-            }
+            const float4 v = *reinterpret_cast<const float4*>(a.part + ((size_t(sp) * a.T + t) * a.ks + k) * a.H + h);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
     }
     if constexpr (YF) {
-        float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.y) + size_t(t) * a.H + h);
-        o[0] = make_float4(s[0], s[1], s[2], s[3]);
-        o[1] = make_float4(s[4], s[5], s[6], s[7]);
+        *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.y) + size_t(t) * a.H + h) = s;
     } else {
         union {
-            __bf16 b[8];
-            uint4 v;
+            __bf16 b[4];
+            uint2 v;
         } o;
-#pragma unroll
-        for (int i = 0; i < V; ++i) o.b[i] = __bf16(s[i]);
-        *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.y) + size_t(t) * a.H + h) = o.v;
+        o.b[0] = __bf16(s.x); o.b[1] = __bf16(s.y); o.b[2] = __bf16(s.z); o.b[3] = __bf16(s.w);
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.y) + size_t(t) * a.H + h) = o.v;
     }
 }
 
@@ -572,269 +554,429 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
 // select, so each selected expert is read once, and the down projection is one
 // product over the selected experts' concatenated rows: the gate weight goes
 // into the activation, a wave adds a slot's product to a token that selects
-// the slot, and nothing is gathered.  Both launches are bound by the weights'
-// bytes; they split the contraction over the waves of a workgroup (and, down,
-// over workgroups) so that every CU has enough of them in flight.
+// the slot, and nothing is gathered.
+//
+// Both launches are bound by the weights' bytes.  Their workgroups stay: each
+// takes an equal run of the row blocks to compute, its waves share the
+// contraction and keep their columns in registers, so that the loop loads
+// weights alone, the next row block's while the present one's are used.
 
-constexpr int kUnitTiles = 2;       // tiles a wave takes at a time: 2 KiB of codes and 128 scales
-constexpr int kDownWaves = 8;
-
-struct Unit {
-    u32x4 c[kUnitTiles];
-    uint32_t s;                     // the tiles' scale bytes
+// A distinct expert of a decode step and, per token, the entry that selects it.
+struct DecodeSlot {
+    const void* blob;
+    uint8_t k[kMaxB];               // kNone: the token does not select it
 };
+constexpr int kNone = 255;
 
-// Unit u of a row block whose codes and scales begin at c and s.  A missing
-// last tile repeats the one before it (its columns' operands are zero).
-__device__ __forceinline__ Unit load_unit(BlobRef ref, uint32_t c, uint32_t s, int u, int KT, uint32_t lane) {
-    Unit r;
-    const int t = u * kUnitTiles, t1 = t + 1 < KT ? t + 1 : t;
-    r.c[0] = load_codes(ref, c + uint32_t(t) * kTileBytes, lane);
-    r.c[1] = load_codes(ref, c + uint32_t(t1) * kTileBytes, lane);
-    const uint32_t v = __builtin_amdgcn_raw_buffer_load_b16(
-        ref, int(lane * 4u), int(s + uint32_t(t / kGroupTiles) * kGroupBytes + uint32_t(t % kGroupTiles)), 0);
-    r.s = t1 == t ? v & 0xffu : v;
-    return r;
+__device__ __forceinline__ uint32_t load_scale(BlobRef r, uint32_t at, int tile, uint32_t lane) {
+    return __builtin_amdgcn_raw_buffer_load_b8(
+        r, int(lane * 4u), int(at + uint32_t(tile / kGroupTiles) * kGroupBytes + uint32_t(tile % kGroupTiles)), 0);
 }
 
-template <bool XF, bool YF>
-__global__ __launch_bounds__(kThreads) void mx_up_decode(MxArgs a, int nrb) {
-    __shared__ uint32_t present[kMaxE / 32];
-    __shared__ int entry[kMaxB * kMaxK];
-    __shared__ float red[kWaves][2][4][64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int slot = blockIdx.x / nrb, rb = blockIdx.x % nrb;
-    // the slot's expert: the slot-th of those present, then the shared ones
-    if (tid < kMaxE / 32) present[tid] = 0u;
+// The slots of a decode step in LDS: routed experts ascending, then the shared.
+struct SlotTable {
+    const void* blob[kMaxGroups];
+    alignas(16) uint8_t k[kMaxGroups][kMaxB];
+    uint32_t present[kMaxE / 32];
+    uint16_t rank[kMaxE];
+    int entry[kMaxB * kMaxK];
+
+    __device__ __forceinline__ BlobRef ref(int s, const Blob& L) const {
+        const uint64_t p = reinterpret_cast<uint64_t>(blob[s]);
+        const uint64_t u = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(p >> 32)))) << 32 |
+                           uint32_t(__builtin_amdgcn_readfirstlane(int(p)));
+        return blob_ref(reinterpret_cast<const void*>(u), L);
+    }
+};
+
+// Builds the table from the selection (at least 256 threads); returns the number of slots.
+template <int N>
+__device__ __forceinline__ int make_slots(const MxArgs& a, SlotTable& tab) {
+    const int tid = threadIdx.x;
+    if (tid < kMaxE / 32) tab.present[tid] = 0u;
+    for (int s = tid; s < kMaxGroups; s += N) *reinterpret_cast<uint4*>(tab.k[s]) = make_uint4(~0u, ~0u, ~0u, ~0u);
     int mine = tid < a.T * a.K ? a.idx[tid] : -1;
     if (mine >= a.E) mine = -1;
-    entry[tid] = mine;
-    __syncthreads();
-    if (mine >= 0) atomicOr(&present[mine >> 5], 1u << (mine & 31));
-    __syncthreads();
-    int total = 0, g = -1;
+    const void* blob = mine >= 0 ? a.eptr[mine] : nullptr;
+    if (tid < kMaxB * kMaxK) tab.entry[tid] = mine;
+    lds_barrier();
+    if (mine >= 0) atomicOr(&tab.present[mine >> 5], 1u << (mine & 31));
+    lds_barrier();
+    int total = 0, at = 0;
+#pragma unroll
     for (int i = 0; i < kMaxE / 32; ++i) {
-        uint32_t m = __builtin_amdgcn_readfirstlane(present[i]);
-        const int c = __builtin_popcount(m);
-        if (slot >= total && slot < total + c) {
-            for (int j = slot - total; j > 0; --j) m &= m - 1u;
-            g = 32 * i + __builtin_ctz(m);
+        const uint32_t m = tab.present[i];
+        if (mine >= 0) at += i < mine >> 5 ? __builtin_popcount(m) : i == mine >> 5 ? __builtin_popcount(m & ((1u << (mine & 31)) - 1u)) : 0;
+        total += __builtin_popcount(m);
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    if (mine >= 0) {
+        tab.blob[at] = blob;
+        tab.rank[mine] = uint16_t(at);
+    }
+    if (tid < a.ns) tab.blob[total + tid] = a.sptr[tid];
+    lds_barrier();
+    if (tid < a.T) {
+        // the first of a token's entries that names the expert
+        for (int j = a.K - 1; j >= 0; --j) {
+            const int e = tab.entry[tid * a.K + j];
+            if (e >= 0) tab.k[tab.rank[e]][tid] = uint8_t(j);
         }
-        total += c;
+        for (int s = 0; s < a.ns; ++s) tab.k[total + s][tid] = uint8_t(a.K + s);
     }
-    if (blockIdx.x == 0) {
-        if (tid == 0) {
-            *a.nslots = total + a.ns;
-            if (a.n_experts) *a.n_experts += (unsigned long long)(total);
-        }
-        for (int i = tid; i < row_blocks(a.H); i += kThreads) a.arrived[i] = 0;
+    lds_barrier();
+    return total + a.ns;
+}
+
+// What the down launch needs, by the first workgroup.
+template <int N>
+__device__ __forceinline__ void publish_slots(const MxArgs& a, const SlotTable& tab, int S) {
+    for (int s = threadIdx.x; s < S; s += N) {
+        a.slots[s].blob = tab.blob[s];
+        for (int t = 0; t < kMaxB; ++t) a.slots[s].k[t] = tab.k[s][t];
     }
-    if (g < 0) {
-        if (slot - total >= a.ns) return;
-        g = a.E + slot - total;
+    if (threadIdx.x == 0) {
+        *a.nslots = S;
+        if (a.n_experts) *a.n_experts += (unsigned long long)(S - a.ns);
     }
+}
+
+// A run of (slot, row block) of gate and up rows per workgroup.  Wave w holds
+// the columns of the tiles from w TPW on, of every token: a token that does not
+// select the slot is a column that is not stored.
+template <int NH, int NW, int TPW>
+__global__ __launch_bounds__(64 * NW) void mx_up_decode(MxArgs a) {
+    constexpr int N = 64 * NW;
+    __shared__ SlotTable tab;
+    __shared__ float gate_w[kMaxB * kMaxK];
+    __shared__ float red[2][NW][8][64];
+    const uint32_t lane = threadIdx.x & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (tid < a.T * a.K) gate_w[tid] = a.w[tid];
+    const int S = make_slots<N>(a, tab);
+    if (blockIdx.x == 0) publish_slots<N>(a, tab, S);
     const Blob L = blob(a.H, a.I);
-    const BlobRef ref = expert_blob(a, L, g);
-    const int KT = col_tiles(a.H), KG = col_groups(a.H), KU = (KT + kUnitTiles - 1) / kUnitTiles;
-    const uint32_t gc = uint32_t(L.gate) + uint32_t(rb * KT) * kTileBytes;
-    const uint32_t uc = uint32_t(L.up) + uint32_t(rb * KT) * kTileBytes;
-    const uint32_t gs = uint32_t(L.gate_s) + uint32_t(rb * KG) * kGroupBytes;
-    const uint32_t us = uint32_t(L.up_s) + uint32_t(rb * KG) * kGroupBytes;
-    Unit ng{}, nu{};
-    if (wave < KU) {
-        ng = load_unit(ref, gc, gs, wave, KT, lane);
-        nu = load_unit(ref, uc, us, wave, KT, lane);
-    }
-    // lane: token c; its first entry that selects the expert
-    const int c = lane & 15, q = lane >> 4;
-    int k = kNone;
-    if (c < a.T) {
-        if (g >= a.E) k = a.K + g - a.E;
-        else
-            for (int j = a.K - 1; j >= 0; --j)
-                if (entry[c * a.K + j] == g) k = j;
-    }
-    const bool live = k != kNone;
-    if (rb == 0 && tid < kMaxB) {
-        if (tid == 0) a.slots[slot].g = g;
-        a.slots[slot].k[tid] = uint8_t(k);
-    }
-    const size_t xrow = live ? size_t(c) * a.H : 0;
-    f32x4 ag = {0.f, 0.f, 0.f, 0.f}, au = {0.f, 0.f, 0.f, 0.f};
-    for (int u = wave; u < KU; u += kWaves) {
-        const Unit cg = ng, cu = nu;
-        // the unit's columns before the next weights: loads return in order,
-        // and the wait for the columns then leaves the weights in flight
-        Raw<XF> xr[kUnitTiles][4];
+    const int KT = col_tiles(a.H), KG = col_groups(a.H), NB = row_blocks(a.I);
+    const int64_t items = int64_t(S) * NB;
+    const int lo = int(items * blockIdx.x / gridDim.x), hi = int(items * (blockIdx.x + 1) / gridDim.x);
+    if (lo >= hi) return;
+    const int c = int(lane & 15), q = int(lane >> 4);
+    const int kt0 = wave * TPW;
+    Raw<false> x[TPW][4];
 #pragma unroll
-        for (int j = 0; j < kUnitTiles; ++j)
+    for (int j = 0; j < TPW; ++j)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int at = (u * kUnitTiles + j) * kTileCols + q * kBlock + s * 8;
-                xr[j][s] = load_raw<XF>(a.x, xrow + at, live && at < a.H);
-            }
-        if (u + kWaves < KU) {
-            ng = load_unit(ref, gc, gs, u + kWaves, KT, lane);
-            nu = load_unit(ref, uc, us, u + kWaves, KT, lane);
+        for (int s = 0; s < 4; ++s) {
+            const int col = (kt0 + j) * kTileCols + q * kBlock + s * 8;
+            x[j][s] = load_raw<false>(a.x, size_t(c) * a.H + col, c < a.T && col < a.H);
         }
+    struct Stage {
+        u32x4 w[2][TPW];
+        uint32_t s[2];
+    } st[2];
+    // a tile beyond the last one is the last one again: its columns are zero
+    auto load = [&](Stage& d, int item) __attribute__((always_inline)) {
+        if (kt0 >= KT) return;
+        const int slot = item / NB, rb = item - slot * NB;
+        const BlobRef ref = tab.ref(slot, L);
+        const uint32_t wc = uint32_t(rb * KT) * kTileBytes;
+        const uint32_t sc = uint32_t(rb * KG + kt0 / kGroupTiles) * kGroupBytes;
 #pragma unroll
-        for (int j = 0; j < kUnitTiles; ++j) {
-            const float sg = scale_of(cg.s >> (8 * j) & 0xffu), su = scale_of(cu.s >> (8 * j) & 0xffu);
+        for (int m = 0; m < 2; ++m) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const Pieces<XF> xv = pieces(xr[j][s]);
-                const bf16x8 gv = decode8(cg.c[j][s], sg), uv = decode8(cu.c[j][s], su);
+            for (int j = 0; j < TPW; ++j)
+                d.w[m][j] = load_codes(ref, uint32_t(m ? L.up : L.gate) + wc + uint32_t(min(kt0 + j, KT - 1)) * kTileBytes, lane);
+            d.s[m] = __builtin_amdgcn_raw_buffer_load_b32(ref, int(lane * 4u), int(uint32_t(m ? L.up_s : L.gate_s) + sc), 0);
+        }
+    };
+    // TPW tiles never lie in two groups of scales
+    const int sh = 8 * (kt0 % kGroupTiles);
+    auto use = [&](const Stage& d, int item, int buf) __attribute__((always_inline)) {
+        f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        if (kt0 < KT) {
 #pragma unroll
-                for (int p = 0; p < Pieces<XF>::N; ++p) {
-                    ag = __builtin_amdgcn_mfma_f32_16x16x32_bf16(gv, xv.p[p], ag, 0, 0, 0);
-                    au = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uv, xv.p[p], au, 0, 0, 0);
+            for (int j = 0; j < TPW; ++j)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const uint32_t b = kt0 + j < KT ? d.s[m] >> (sh + 8 * j) & 0xffu : 0u;
+                        const bf16x8 wv = decode8(d.w[m][j][s], scale_of(b));
+                        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, as_operand(x[j][s].q[0]), acc[m], 0, 0, 0);
+                    }
                 }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[buf][wave][m * 4 + r][lane] = acc[m][r];
+        lds_barrier();
+        if (wave >= 4) return;
+        // wave r: rows 4 q + r of the block
+        float gsum = 0.f, usum = 0.f;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            gsum += red[buf][v][wave][lane];
+            usum += red[buf][v][4 + wave][lane];
+        }
+        const int slot = item / NB, row = (item - slot * NB) * kTileRows + 4 * q + wave, k = tab.k[slot][c];
+        if (k == kNone || row >= a.I) return;
+        const float w = k < a.K ? gate_w[c * a.K + k] : 1.f;
+        __bf16 b[NH];
+        split(silu(gsum) * usum * w, b);
+        __bf16* o = reinterpret_cast<__bf16*>(a.act) + size_t(c * a.ks + k) * NH * a.I + row;
+#pragma unroll
+        for (int p = 0; p < NH; ++p) o[size_t(p) * a.I] = b[p];
+    };
+    load(st[0], lo);
+    for (int item = lo; item < hi; item += 2) {
+        if (item + 1 < hi) load(st[1], item + 1);
+        use(st[0], item, 0);
+        if (item + 1 >= hi) break;
+        if (item + 2 < hi) load(st[0], item + 2);
+        use(st[1], item + 1, 1);
+    }
+}
+
+// fp32 hidden states, or more than 32 column tiles: a row block of one expert
+// per workgroup, whose four waves take every fourth tile and load its columns
+// with it, of the tokens that select the expert.
+template <int NX, int NH>
+__global__ __launch_bounds__(kThreads) void mx_up_wide(MxArgs a, int nrb) {
+    __shared__ SlotTable tab;
+    __shared__ float red[kWaves][8][64];
+    const uint32_t lane = threadIdx.x & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int slot = blockIdx.x / nrb, rb = int(blockIdx.x % nrb);
+    const int S = make_slots<kThreads>(a, tab);
+    if (blockIdx.x == 0) publish_slots<kThreads>(a, tab, S);
+    if (slot >= S) return;
+    const Blob L = blob(a.H, a.I);
+    const BlobRef ref = tab.ref(slot, L);
+    const int KT = col_tiles(a.H), KG = col_groups(a.H);
+    const int c = int(lane & 15), q = int(lane >> 4), k = tab.k[slot][c];
+    const bool live = k != kNone;
+    const size_t xrow = live ? size_t(c) * a.H : 0;
+    const uint32_t wc = uint32_t(rb * KT) * kTileBytes, sc = uint32_t(rb * KG) * kGroupBytes;
+    struct Stage {
+        u32x4 w[2];
+        uint32_t s[2];
+        Raw<(NX > 1)> x[4];
+    } st[2];
+    auto load = [&](Stage& d, int kt) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            d.w[m] = load_codes(ref, uint32_t(m ? L.up : L.gate) + wc + uint32_t(kt) * kTileBytes, lane);
+            d.s[m] = load_scale(ref, uint32_t(m ? L.up_s : L.gate_s) + sc, kt, lane);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int col = kt * kTileCols + q * kBlock + s * 8;
+            d.x[s] = load_raw<(NX > 1)>(a.x, xrow + col, live && col < a.H);
+        }
+    };
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    auto use = [&](const Stage& d) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const Pieces<NX> xv = pieces<NX>(d.x[s]);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const bf16x8 wv = decode8(d.w[m][s], scale_of(d.s[m]));
+#pragma unroll
+                for (int p = 0; p < NX; ++p)
+                    acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv.p[p], acc[m], 0, 0, 0);
             }
         }
+    };
+    if (wave < KT) load(st[0], wave);
+    for (int kt = wave; kt < KT; kt += 2 * kWaves) {
+        if (kt + kWaves < KT) load(st[1], kt + kWaves);
+        use(st[0]);
+        if (kt + kWaves >= KT) break;
+        if (kt + 2 * kWaves < KT) load(st[0], kt + 2 * kWaves);
+        use(st[1]);
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        red[wave][0][r][lane] = ag[r];
-        red[wave][1][r][lane] = au[r];
-    }
-    __syncthreads();
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) red[wave][m * 4 + r][lane] = acc[m][r];
+    lds_barrier();
     // wave r: rows 4 q + r of the block
     float gsum = 0.f, usum = 0.f;
 #pragma unroll
     for (int v = 0; v < kWaves; ++v) {
-        gsum += red[v][0][wave][lane];
-        usum += red[v][1][wave][lane];
+        gsum += red[v][wave][lane];
+        usum += red[v][4 + wave][lane];
     }
     const int row = rb * kTileRows + 4 * q + wave;
     if (!live || row >= a.I) return;
     const float w = k < a.K ? a.w[c * a.K + k] : 1.f;
-    const float h = silu(gsum) * usum * w;
-    constexpr int NP = Pieces<YF>::N;
-    __bf16* o = reinterpret_cast<__bf16*>(a.act) + size_t(c * a.ks + k) * NP * a.I + row;
-    if constexpr (YF) {
-        __bf16 hi, lo;
-        split(h, hi, lo);
-        o[0] = hi;
-        o[a.I] = lo;
-    } else {
-        o[0] = __bf16(h);
-    }
+    __bf16 b[NH];
+    split(silu(gsum) * usum * w, b);
+    __bf16* o = reinterpret_cast<__bf16*>(a.act) + size_t(c * a.ks + k) * NH * a.I + row;
+#pragma unroll
+    for (int p = 0; p < NH; ++p) o[size_t(p) * a.I] = b[p];
 }
 
-// PC: up to eight tokens with two pieces each: the pieces are columns too.
-template <bool YF, bool PC>
-__global__ __launch_bounds__(64 * kDownWaves) void mx_down_decode(MxArgs a, int splits) {
-    constexpr int NP = Pieces<YF>::N, MP = PC ? 1 : NP;     // pieces; instructions per operand
-    __shared__ const void* base[kMaxE + kMaxShared];
-    __shared__ uint8_t sk[kMaxE + kMaxShared][kMaxB];
-    __shared__ float red[kDownWaves][4][64];
-    __shared__ int last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int rb = blockIdx.x / splits, sp = blockIdx.x % splits;
+// A run of (chunk of column tiles, group of R row blocks) of the down rows per
+// workgroup.  A chunk is NW U tiles of the selected experts' concatenated
+// rows, U per wave, whose activations the wave holds while it goes through the
+// row blocks.  With one chunk the sums are y, else the chunks' sums go to the
+// join launch.  PC: few tokens, whose pieces are columns too.
+template <int NH, bool PC, bool YF, int NW, int U, int R>
+__global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) {
+    constexpr int MP = PC ? 1 : NH;                         // instructions per operand
+    constexpr int N = 64 * NW, OUT = R * 256;
+    static_assert(OUT <= N, "a thread sums one output");
+    __shared__ SlotTable tab;
+    __shared__ float red[2][NW][OUT];
+    const uint32_t lane = threadIdx.x & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int S = *a.nslots;
-    for (int s = tid; s < S; s += 64 * kDownWaves) {
+    for (int s = tid; s < a.smax; s += N) {
         const DecodeSlot d = a.slots[s];
-        base[s] = d.g < a.E ? a.eptr[d.g] : a.sptr[d.g - a.E];
+        tab.blob[s] = d.blob;
 #pragma unroll
-        for (int t = 0; t < kMaxB; ++t) sk[s][t] = d.k[t];
+        for (int t = 0; t < kMaxB; ++t) tab.k[s][t] = d.k[t];
     }
-    __syncthreads();
+    lds_barrier();
     const Blob L = blob(a.H, a.I);
-    const int KT = col_tiles(a.I), KG = col_groups(a.I), KU = (KT + kUnitTiles - 1) / kUnitTiles;
-    const uint32_t co = uint32_t(L.down) + uint32_t(rb * KT) * kTileBytes;
-    const uint32_t so = uint32_t(L.down_s) + uint32_t(rb * KG) * kGroupBytes;
-    // unit u of all slots' (uniform within a wave)
-    auto load = [&](int u) __attribute__((always_inline)) {
-        const int s = u / KU;
-        const uint64_t p = reinterpret_cast<uint64_t>(base[s]);
-        const uint64_t w = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(p >> 32)))) << 32 |
-                           uint32_t(__builtin_amdgcn_readfirstlane(int(p)));
-        const BlobRef ref =
-            __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(w), 0, int(uint32_t(L.total)), 0x00027000);
-        return load_unit(ref, co, so, u - s * KU, KT, lane);
-    };
-    const int c = lane & 15, q = lane >> 4;
-    const int t = PC ? c >> 1 : c, pc = PC ? c & 1 : 0;
-    const int units = S * KU, step = splits * kDownWaves;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    Unit nx{};
-    int u = sp * kDownWaves + wave;
-    if (u < units) nx = load(u);
-    for (; u < units; u += step) {
-        const Unit cur = nx;
-        const int slot = u / KU, t0 = (u - slot * KU) * kUnitTiles;
-        const int k = sk[slot][t];
-        const bool live = k != kNone;
-        const size_t arow = live ? (size_t(t * a.ks + k) * NP + pc) * a.I : 0;
-        Raw<false> h[kUnitTiles][4][MP];
+    const int KT = col_tiles(a.I), KG = col_groups(a.I), NB = row_blocks(a.H), groups = (NB + R - 1) / R;
+    const int units = S * KT, chunks = max(1, (units + NW * U - 1) / (NW * U));
+    const int64_t work = int64_t(chunks) * groups;
+    const int lo = int(work * blockIdx.x / gridDim.x), hi = int(work * (blockIdx.x + 1) / gridDim.x);
+    const int c = int(lane & 15), q = int(lane >> 4);
+    const int t = PC ? c / NH : c, pc = PC ? c % NH : 0;
+    struct Stage {
+        u32x4 w[U][R];
+        uint32_t s[U][R];
+    } st[2];
+    auto load = [&](Stage& d, int item) __attribute__((always_inline)) {
+        const int chunk = item / groups, grp = item - chunk * groups;
 #pragma unroll
-        for (int j = 0; j < kUnitTiles; ++j)
+        for (int j = 0; j < U; ++j) {
+            const int u = (chunk * NW + wave) * U + j;
+            if (u >= units) continue;
+            const int slot = u / KT, kt = u - slot * KT;
+            const BlobRef ref = tab.ref(slot, L);
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int p = 0; p < MP; ++p) {
-                    const int at = (t0 + j) * kTileCols + q * kBlock + s * 8;
-                    h[j][s][p] = load_raw<false>(a.act, arow + size_t(p) * a.I + at, live && at < a.I);
-                }
-        if (u + step < units) nx = load(u + step);
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < kUnitTiles; ++j) {
-            const float sd = scale_of(cur.s >> (8 * j) & 0xffu);
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const bf16x8 dv = decode8(cur.c[j][s], sd);
-#pragma unroll
-                for (int p = 0; p < MP; ++p)
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dv, pieces(h[j][s][p]).p[0], acc, 0, 0, 0);
+            for (int i = 0; i < R; ++i) {
+                const uint32_t b = uint32_t(min(grp * R + i, NB - 1));
+                d.w[j][i] = load_codes(ref, uint32_t(L.down) + (b * uint32_t(KT) + uint32_t(kt)) * kTileBytes, lane);
+                d.s[j][i] = load_scale(ref, uint32_t(L.down_s) + b * uint32_t(KG) * kGroupBytes, kt, lane);
             }
         }
-        // only to the tokens that select the slot: a NaN among its weights stays theirs
+    };
+    Raw<false> h[U][4][MP];
+    bool live[U];
+    auto columns = [&](int chunk) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum[r] += live ? acc[r] : 0.f;
+        for (int j = 0; j < U; ++j) {
+            const int u = (chunk * NW + wave) * U + j, slot = u / KT, kt = u - slot * KT;
+            const int k = u < units ? tab.k[slot][t] : kNone;
+            live[j] = k != kNone;
+            const size_t row = live[j] ? (size_t(t * a.ks + k) * NH + pc) * a.I : 0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int col = kt * kTileCols + q * kBlock + x * 8;
+#pragma unroll
+                for (int y = 0; y < MP; ++y)
+                    h[j][x][y] = load_raw<false>(a.act, row + size_t(y) * a.I + col, live[j] && col < a.I);
+            }
+        }
+    };
+    auto use = [&](const Stage& d, int item, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const bf16x8 wv = decode8(d.w[j][i][x], scale_of(d.s[j][i]));
+#pragma unroll
+                    for (int y = 0; y < MP; ++y)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, as_operand(h[j][x][y].q[0]), acc, 0, 0, 0);
+                }
+                // only to the tokens that select the slot: a NaN among its weights stays theirs
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[r] += live[j] ? acc[r] : 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[buf][wave][(i * 4 + r) * 64 + lane] = sum[r];
+        }
+        lds_barrier();
+        if (tid >= OUT) return;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) v += red[buf][w][tid];
+        if (!direct) {
+            a.split[size_t(item) * OUT + tid] = v;
+            return;
+        }
+        float s = v;
+        if constexpr (PC) {
+            s += __shfl_down(v, 1, 64);
+            s += __shfl_down(v, 2, 64);
+        }
+        const int grp = item, row = (grp * R + tid / 256) * kTileRows + 4 * q + (tid / 64 & 3);
+        if (t >= a.T || pc || row >= a.H) return;
+        if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = s;
+        else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
+    };
+    int chunk = -1;
+    if (lo < hi) load(st[0], lo);
+    for (int item = lo; item < hi; item += 2) {
+        if (item / groups != chunk) columns(chunk = item / groups);
+        if (item + 1 < hi) load(st[1], item + 1);
+        use(st[0], item, 0);
+        if (item + 1 >= hi) break;
+        if ((item + 1) / groups != chunk) columns(chunk = (item + 1) / groups);
+        if (item + 2 < hi) load(st[0], item + 2);
+        use(st[1], item + 1, 1);
     }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) red[wave][r][lane] = sum[r];
-    __syncthreads();
-    const int r = wave & 3;
-    float v = 0.f;
-#pragma unroll
-    for (int x = 0; x < kDownWaves; ++x) v += red[x][r][lane];
-    if (splits > 1) {
-        // the row block's last workgroup adds the others' sums, in their order;
-        // stores and loads at device scope, the count after the stores are done
-        float* mine = a.split + (size_t(rb) * splits + sp) * 256;
-        if (wave < 4) __hip_atomic_store(&mine[r * 64 + lane], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (tid == 0)
-            last = __hip_atomic_fetch_add(&a.arrived[rb], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
-        __syncthreads();
-        if (!last || wave >= 4) return;
-        v = 0.f;
-        for (int x = 0; x < splits; ++x)
-            v += __hip_atomic_load(&a.split[(size_t(rb) * splits + x) * 256 + r * 64 + lane], __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
-    }
-    if (wave >= 4) return;
-    if constexpr (PC) v += __shfl_xor(v, 1, 64);
-    const int row = rb * kTileRows + 4 * q + r;
-    if (t >= a.T || pc || row >= a.H) return;
-    if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = v;
-    else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(v);
 }
+
+// y from the chunks' sums, in their order: a row block per workgroup.
+template <int NH, bool PC, bool YF, int TILES, int R>
+__global__ __launch_bounds__(1024) void mx_join_kernel(MxArgs a) {
+    __shared__ float red[4][256];
+    const int rb = blockIdx.x, tid = threadIdx.x, o = tid & 255, part = tid >> 8;
+    const int groups = (row_blocks(a.H) + R - 1) / R, units = *a.nslots * col_tiles(a.I);
+    const int chunks = max(1, (units + TILES - 1) / TILES);
+    const float* p = a.split + size_t(rb / R) * R * 256 + rb % R * 256 + o;
+    float v = 0.f;
+#pragma unroll 8
+    for (int x = part; x < chunks; x += 4) v += p[size_t(x) * groups * R * 256];
+    red[part][o] = v;
+    __syncthreads();
+    if (tid < 256) red[0][o] = (red[0][o] + red[1][o]) + (red[2][o] + red[3][o]);
+    __syncthreads();
+    for (int i = tid; i < kTileRows * a.T; i += 1024) {
+        const int t = i / kTileRows, rr = i % kTileRows, row = rb * kTileRows + rr;
+        if (row >= a.H) continue;
+        const float* f = &red[0][rr % 4 * 64 + rr / 4 * 16 + (PC ? NH * t : t)];
+        float s = f[0];
+        if constexpr (PC) {
+#pragma unroll
+            for (int c = 1; c < NH; ++c) s += f[c];
+        }
+        if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = s;
+        else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
+    }
+}
+
+// The down launch's forms: up to 48 column tiles of few columns in one chunk of
+// sixteen waves, else chunks of 16 tiles.
+constexpr int kOneWaves = 16, kOneU = 3, kOneR = 1;
+constexpr int kRunWaves = 8, kRunU = 2, kRunR = 2;
 
 struct MxLayout {
-    int tm, max_tiles, tsplits, slots, splits;
-    size_t order, cnt, tiles, ntiles, act, part, xs, plan, nslots, arrived, split, total;
+    int tm, max_tiles, tsplits, slots, units;
+    size_t order, cnt, tiles, ntiles, act, part, xs, plan, nslots, split, total;
 };
-
-// Workgroups of the down launch per row block: 512 in all.
-int down_splits(int H) {
-    const int rb = row_blocks(H);
-    return rb >= 512 ? 1 : (512 + rb - 1) / rb < 16 ? (512 + rb - 1) / rb : 16;
-}
 
 // Tokens per tile: by the tokens an expert gets on average.
 int tile_tokens(int T, int K, int E) {
@@ -855,14 +997,14 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
     const size_t n = size_t(T) * (K + ns);
     size_t off = 0;
     auto take = [&](size_t b) { const size_t at = off; off = (off + b + 255) / 256 * 256; return at; };
-    y.act = take(n * (ydtype == STMOE_F32 ? 2 : 1) * I * sizeof(uint16_t));
+    y.act = take(n * (ydtype == STMOE_F32 ? 3 : 1) * I * sizeof(uint16_t));
     if (T <= kMaxB) {
         y.slots = (E < T * K ? E : T * K) + ns;
-        y.splits = down_splits(H);
+        y.units = y.slots * col_tiles(I);
         y.plan = take(size_t(y.slots) * sizeof(DecodeSlot));
         y.nslots = take(sizeof(int32_t));
-        y.arrived = take(size_t(row_blocks(H)) * sizeof(int32_t));
-        y.split = take(size_t(row_blocks(H)) * y.splits * 256 * sizeof(float));
+        const size_t chunks = (size_t(y.units) + kRunWaves * kRunU - 1) / (kRunWaves * kRunU);
+        y.split = take(chunks * ((row_blocks(H) + kRunR - 1) / kRunR * kRunR) * 256 * sizeof(float));
     } else {
         y.tm = tile_tokens(T, K, E);
         // a full tile takes tm entries; each expert has at most one that is not full
@@ -873,30 +1015,56 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
         y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
         y.ntiles = take(sizeof(int32_t));
         y.tsplits = tile_splits(y.tm, n, E, ns, H, I);
-        y.part = take(n * y.tsplits * H * (ydtype == STMOE_F32 || y.tsplits > 1 ? 4 : 2));
-        if (dtype == STMOE_F32) y.xs = take(size_t(T) * H * 2 * sizeof(uint16_t));
+        y.part = take(n * y.tsplits * H * sizeof(float));
+        if (dtype == STMOE_F32) y.xs = take(size_t(T) * H * (ydtype == STMOE_F32 ? 3 : 2) * sizeof(uint16_t));
     }
     y.total = off;
     return y;
 }
 
-template <bool XF, bool YF>
-int launch_decode(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t ev_mid) {
-    const int rb = row_blocks(a.I);
-    hipLaunchKernelGGL((mx_up_decode<XF, YF>), dim3(unsigned(rb * L.slots)), dim3(kThreads), 0, s, a, rb);
-    STMOE_LAUNCHED();
-    if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
-    const dim3 grid(unsigned(row_blocks(a.H) * L.splits)), block(64 * kDownWaves);
-    if constexpr (YF) {
-        if (a.T <= kMaxB / 2) {
-            hipLaunchKernelGGL((mx_down_decode<YF, true>), grid, block, 0, s, a, L.splits);
+template <int NX, int NH>
+void launch_up_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
+    const int KT = col_tiles(a.H), NB = row_blocks(a.I);
+    const int64_t items = int64_t(L.slots) * NB;
+    const auto grid = [&](int most) { return dim3(unsigned(items < most ? items : most)); };
+    if (NX > 1 || KT > 32) hipLaunchKernelGGL((mx_up_wide<NX, NH>), dim3(unsigned(items)), dim3(kThreads), 0, s, a, NB);
+    else if (KT <= 4) hipLaunchKernelGGL((mx_up_decode<NH, 4, 1>), grid(1024), dim3(256), 0, s, a);
+    else if (KT <= 8) hipLaunchKernelGGL((mx_up_decode<NH, 4, 2>), grid(1024), dim3(256), 0, s, a);
+    else if (KT <= 16) hipLaunchKernelGGL((mx_up_decode<NH, 4, 4>), grid(512), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((mx_up_decode<NH, 8, 4>), grid(256), dim3(512), 0, s, a);
+}
+
+template <int NH, bool PC, bool YF>
+int launch_down_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
+    const int NB = row_blocks(a.H);
+    if constexpr (PC || NH == 1) {
+        if (L.units <= kOneWaves * kOneU) {
+            hipLaunchKernelGGL((mx_down_decode<NH, PC, YF, kOneWaves, kOneU, kOneR>), dim3(unsigned(NB < 256 ? NB : 256)),
+                               dim3(64 * kOneWaves), 0, s, a, 1);
             STMOE_LAUNCHED();
             return STMOE_OK;
         }
     }
-    hipLaunchKernelGGL((mx_down_decode<YF, false>), grid, block, 0, s, a, L.splits);
+    const int64_t chunks = (L.units + kRunWaves * kRunU - 1) / (kRunWaves * kRunU);
+    const int64_t work = chunks * ((NB + kRunR - 1) / kRunR);
+    hipLaunchKernelGGL((mx_down_decode<NH, PC, YF, kRunWaves, kRunU, kRunR>), dim3(unsigned(work < 256 ? work : 256)),
+                       dim3(64 * kRunWaves), 0, s, a, chunks == 1);
     STMOE_LAUNCHED();
+    if (chunks > 1) {
+        hipLaunchKernelGGL((mx_join_kernel<NH, PC, YF, kRunWaves * kRunU, kRunR>), dim3(unsigned(NB)), dim3(1024), 0, s, a);
+        STMOE_LAUNCHED();
+    }
     return STMOE_OK;
+}
+
+template <bool XF, bool YF>
+int launch_decode(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t ev_mid) {
+    constexpr int NX = kPiecesX<XF, YF>, NH = kPiecesH<YF>;
+    launch_up_decode<NX, NH>(a, L, s);
+    STMOE_LAUNCHED();
+    if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
+    if (YF && a.T * NH <= kMaxB) return launch_down_decode<NH, YF, YF>(a, L, s);
+    return launch_down_decode<NH, false, YF>(a, L, s);
 }
 
 template <bool XF, bool YF, int NT>
@@ -904,20 +1072,13 @@ int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t e
     // rounded up to the eight XCDs
     const auto grid = [&](int nb) { return dim3(unsigned((int64_t(L.max_tiles) * nb + 7) / 8 * 8)); };
     const int ub = (a.I + 127) / 128, db = (a.H + 255) / 256 * L.tsplits;
-    const int sb = (a.H + kThreads * 8 - 1) / (kThreads * 8);
-    const dim3 sgrid(unsigned(a.T) * unsigned(sb)), block(kThreads);
-    hipLaunchKernelGGL((mx_tile_kernel<true, XF ? 2 : 1, NT, YF>), grid(ub), block, 0, s, a, ub);
+    const int sb = (a.H + kThreads * 4 - 1) / (kThreads * 4);
+    hipLaunchKernelGGL((mx_tile_kernel<true, kPiecesX<XF, YF>, NT, YF>), grid(ub), dim3(kThreads), 0, s, a, ub);
     STMOE_LAUNCHED();
     if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
-    if (YF || L.tsplits > 1) {
-        hipLaunchKernelGGL((mx_tile_kernel<false, YF ? 2 : 1, NT, true>), grid(db), block, 0, s, a, db);
-        STMOE_LAUNCHED();
-        hipLaunchKernelGGL((mx_sum_kernel<true, YF>), sgrid, block, 0, s, a, sb);
-    } else {
-        hipLaunchKernelGGL((mx_tile_kernel<false, 1, NT, false>), grid(db), block, 0, s, a, db);
-        STMOE_LAUNCHED();
-        hipLaunchKernelGGL((mx_sum_kernel<false, false>), sgrid, block, 0, s, a, sb);
-    }
+    hipLaunchKernelGGL((mx_tile_kernel<false, kPiecesH<YF>, NT, true>), grid(db), dim3(kThreads), 0, s, a, db);
+    STMOE_LAUNCHED();
+    hipLaunchKernelGGL((mx_sum_kernel<YF>), dim3(unsigned(a.T) * unsigned(sb)), dim3(kThreads), 0, s, a, sb);
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
@@ -942,7 +1103,7 @@ int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream
     STMOE_LAUNCHED();
     if constexpr (XF) {
         const int64_t n4 = int64_t(a.T) * a.H / 4, wg = (n4 + kThreads - 1) / kThreads;
-        hipLaunchKernelGGL(mx_split_kernel, dim3(unsigned(wg < 8192 ? wg : 8192)), dim3(kThreads), 0, s,
+        hipLaunchKernelGGL((mx_split_kernel<kPiecesX<XF, YF>>), dim3(unsigned(wg < 8192 ? wg : 8192)), dim3(kThreads), 0, s,
                            reinterpret_cast<const float*>(a.x), n4, a.H / 4, xs);
         STMOE_LAUNCHED();
         a.x = xs;
@@ -984,9 +1145,9 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
     a.act = reinterpret_cast<uint16_t*>(base + L.act);
     a.slots = reinterpret_cast<DecodeSlot*>(base + L.plan);
     a.nslots = reinterpret_cast<int32_t*>(base + L.nslots);
-    a.arrived = reinterpret_cast<int32_t*>(base + L.arrived);
+    a.smax = L.slots;
     a.split = reinterpret_cast<float*>(base + L.split);
-    a.part = base + L.part;
+    a.part = reinterpret_cast<float*>(base + L.part);
     a.n_experts = n_experts;
     const bool xf = dtype == STMOE_F32, yf = ydtype == STMOE_F32;
     if (T <= kMaxB) {

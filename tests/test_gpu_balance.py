@@ -260,7 +260,7 @@ def test_layer_of_a_training_batch():
     o, f = _check_forward(z, K, True, mask)
     y = _run(ex, E, H, I, x, o["idx"], o["w"], torch.float32)
     want = mxref.moe_ffn(_f64(x), f["idx"], _f64(o["w"]), ex.values)
-    assert _err(y, want) <= 3e-5 and not y[140:].any()
+    assert _err(y, want) <= 2e-5 and not y[140:].any()
     # loss = sum(y * r): the gradient of gate weight k is r . (expert output k), here from 64 bits
     r = np.random.default_rng(0).normal(size=(T, H))
     d_w = np.zeros((T, K))

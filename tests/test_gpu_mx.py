@@ -1,14 +1,12 @@
 """GPU: 4-bit experts against the plain 64-bit forms.
 
-Tolerances.  Quantising and reading back are exact.  The FFN: a rounding to
-bf16 is off by at most 2^-8 of the value, two bf16 pieces by 2^-16, fp32 sums
-of n products by about sqrt(n) 2^-24 of the root sum of their squares (7e-6 at
-n = 14336); the roundings of the operands are independent, so a projection's
-relative L2 error is at most theirs, and silu (slope at most 1.1) times up adds
-the two projections' errors.  Relative L2 per token:
-  bf16 x, fp32 y   activations in pieces: 2^-16, sums twice: 3e-5 in all
-  fp32 x, fp32 y   pieces on both sides: (1.1 + 1 + 1) 2^-16 + sums: 6e-5
-  bf16 y           activations 2^-8 and y 2^-8: 2^-7
+Tolerances.  Quantising and reading back are exact.  The FFN, relative L2 per
+token: three bf16 pieces hold an fp32 value's 24 bits, so with fp32 y what is
+left are the fp32 sums of n products, about sqrt(n) 2^-24 of the root sum of
+their squares (7e-6 at n = 14336), in a projection, in silu (its slope at most
+1.1) times up and in the sum over experts, and the hardware exponential's 2e-6:
+2e-5 in all.  With bf16 y the activations (2^-8 at most, independent of each
+other) and y itself (2^-8) are rounded: 2^-7.
 """
 import numpy as np
 import pytest
@@ -20,7 +18,7 @@ DEV = "cuda:0"
 
 
 def _tol(x_bf16, y_bf16):
-    return 2.0 ** -7 if y_bf16 else 3e-5 if x_bf16 else 6e-5
+    return 2.0 ** -7 if y_bf16 else 2e-5
 
 
 def _f64(t):
@@ -285,8 +283,8 @@ def test_ffn_values_beyond_bf16_range_of_fp32_x():
 
 @pytest.mark.parametrize("T", [1, 9, 16, 70, 600])
 def test_ffn_same_bits_and_independent_tokens(T):
-    """The same call twice gives the same bits; a token's result does not depend on the tokens beside it as long as
-    the call's size stays, nor on what lies behind the outputs."""
+    """The same call twice gives the same bits; beyond a decode step's 16 tokens a token's bits do not depend on the
+    tokens beside it as long as the call's size stays (in a step the order of its sums goes by the experts selected)."""
     import torch
     H, I, E, K = 520, 264, 12, 3
     ex = Experts(E, H, I, 8)
@@ -300,7 +298,10 @@ def test_ffn_same_bits_and_independent_tokens(T):
         x2, idx2, w2 = _inputs(T, K, E, H, 5, torch.bfloat16)
         x2[T // 2], idx2[T // 2], w2[T // 2] = x[T // 2], idx[T // 2], w[T // 2]
         c = _run(ex, E, H, I, x2, idx2, w2, torch.float32)
-        assert torch.equal(c[T // 2], b[T // 2])
+        if T > 16:
+            assert torch.equal(c[T // 2], b[T // 2])
+        else:
+            assert _err(c[T // 2:T // 2 + 1], _f64(b[T // 2:T // 2 + 1])) <= _tol(True, False)
 
 
 def test_ffn_no_tokens():
