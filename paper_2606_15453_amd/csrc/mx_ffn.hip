@@ -345,8 +345,11 @@ __device__ __forceinline__ BlobRef expert_blob(const MxArgs& a, const Blob& L, i
     return blob_ref(g < a.E ? a.eptr[g] : a.sptr[g - a.E], L);
 }
 
+// ONCE: read by one workgroup only, past the caches (DeepSeek-V2-Lite sizes, 16
+// tokens: gate and up 38 us through them, 33 past them).
+template <bool ONCE>
 __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lane) {
-    return __builtin_amdgcn_raw_buffer_load_b128(r, int(lane * 16u), int(at), 0);
+    return __builtin_amdgcn_raw_buffer_load_b128(r, int(lane * 16u), int(at), ONCE ? 2 : 0);
 }
 
 
@@ -359,12 +362,20 @@ __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lan
 // through LDS, 128 at a time, double-buffered.  A column's 256 bytes lie as 16
 // chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
 // lanes of a read, one chunk of 16 tokens, meet 16 different places.
+// Pieces of a column staged together: all of them for few tokens, where the
+// rounds' latency counts, else one (LDS).  One number for all tiles of a
+// launch: it is part of the order of a sum.
+template <int NP, int NT>
+constexpr int kStagePieces = NT <= 2 ? NP : 1;
+
 // F32 (up): the activations keep fp32 precision.
-template <bool UP, int NP, int NT, bool F32>
+template <bool UP, int NP, int P, int NT, bool F32>
 __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, int sp, u32x4* xs, int* ent) {
     constexpr int TM = 16 * NT;
     constexpr int RB = 4;                                   // row blocks per wave
     constexpr int CH = kTileCols / 8;                       // chunks per column
+    constexpr int Q = NP / P;                               // P pieces staged together, in Q rounds per column tile
+    constexpr int SZ = P * TM * CH;                         // chunks of a buffer
     const uint32_t lane = threadIdx.x & 63;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Blob L = blob(a.H, a.I);
@@ -394,20 +405,22 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         src[j] = uint32_t(UP ? e / a.ks : e) * uint32_t(NP * C / 8);
     }
     const int put = tid / CH * CH + (chunk ^ (tid / CH & 15));
-    u32x4 xr[NT], wn[RB];
+    u32x4 xr[P][NT], wn[RB];
     uint32_t sn[RB];
-    // iteration it: piece it % NP of column tile it / NP.  Chunks beyond the
-    // row's end read its first one: their codes are zero, and if the row holds
-    // a NaN or an infinity its results are not finite without it too.
+    // iteration it: round it % Q of column tile it / Q.  Chunks beyond the row's
+    // end read its first one: their codes are zero, and if the row holds a NaN
+    // or an infinity its results are not finite without it too.
     auto load = [&](int it) __attribute__((always_inline)) {
-        const int kt = it / NP, p = it - kt * NP;
-        const int at = kt * kTileCols + chunk * 8;
-        const uint32_t off = uint32_t(p * C + (at < C ? at : 0)) / 8;
+        const int kt = it / Q, p0 = (it - kt * Q) * P, at = kt * kTileCols + chunk * 8;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) xr[j] = cols[src[j] + off];
+        for (int p = 0; p < P; ++p) {
+            const uint32_t off = uint32_t((p0 + p) * C + (at < C ? at : 0)) / 8;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) xr[p][j] = cols[size_t(src[j]) + off];
+        }
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-            wn[i] = load_codes(ref, wc[i] + uint32_t(kt) * kTileBytes, lane);
+            wn[i] = load_codes<false>(ref, wc[i] + uint32_t(kt) * kTileBytes, lane);
             sn[i] = __builtin_amdgcn_raw_buffer_load_b8(
                 ref, int(lane * 4u), int(wsc[i] + uint32_t(kt / kGroupTiles) * kGroupBytes + uint32_t(kt % kGroupTiles)), 0);
         }
@@ -419,10 +432,15 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         for (int n = 0; n < NT; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int c = int(lane & 15), q = int(lane >> 4);
     // the workgroup's share of the contraction
-    const int it0 = UP ? 0 : KT * sp / a.tsplits * NP, iters = UP ? KT * NP : KT * (sp + 1) / a.tsplits * NP;
-    load(it0);
+    const int it0 = UP ? 0 : KT * sp / a.tsplits * Q, iters = UP ? KT * Q : KT * (sp + 1) / a.tsplits * Q;
+    auto keep = [&](int it) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) xs[(it0 & 1) * TM * CH + put + j * 16 * CH] = xr[j];
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) xs[(it & 1) * SZ + p * TM * CH + put + j * 16 * CH] = xr[p][j];
+    };
+    load(it0);
+    keep(it0);
     for (int it = it0; it < iters; ++it) {
         u32x4 w[RB];
         float sc[RB];
@@ -433,33 +451,32 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         }
         __syncthreads();
         if (it + 1 < iters) load(it + 1);
-        const u32x4* buf = xs + (it & 1) * TM * CH + c * CH;
-        union Column {
-            u32x4 u;
-            bf16x8 v;
-        } b[2][NT];
+        const u32x4* buf = xs + (it & 1) * SZ + c * CH;
+        bf16x8 b[2][P][NT];
+        auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) b[0][n].u = buf[n * 16 * CH + ((q * 4) ^ c)];
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    b[s & 1][p][n] = as_operand(buf[p * TM * CH + n * 16 * CH + ((q * 4 + s) ^ c)]);
+        };
+        fetch(0);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             // the next columns are on their way while these are used
-            if (s < 3) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) b[(s + 1) & 1][n].u = buf[n * 16 * CH + ((q * 4 + s + 1) ^ c)];
-            }
+            if (s < 3) fetch(s + 1);
             bf16x8 wv[RB];
 #pragma unroll
             for (int i = 0; i < RB; ++i) wv[i] = decode8(w[i][s], sc[i]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < RB; ++i)
-                    acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], b[s & 1][n].v, acc[i][n], 0, 0, 0);
-        }
-        if (it + 1 < iters) {
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xs[((it + 1) & 1) * TM * CH + put + j * 16 * CH] = xr[j];
+                    for (int i = 0; i < RB; ++i)
+                        acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], b[s & 1][p][n], acc[i][n], 0, 0, 0);
         }
+        if (it + 1 < iters) keep(it + 1);
     }
     // lane: token 16 n + c, rows 4 q .. 4 q + 3 of each block
 #pragma unroll
@@ -504,8 +521,8 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 
 template <bool UP, int NP, int NT, bool F32>
 __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) {
-    constexpr int TM = 16 * NT;
-    __shared__ u32x4 xs[2][TM * kTileCols / 8];
+    constexpr int TM = 16 * NT, P = kStagePieces<NP, NT>;
+    __shared__ u32x4 xs[2][P * TM * kTileCols / 8];
     __shared__ int ent[TM];
     // consecutive work on one XCD (workgroup i runs on XCD i % 8): the row
     // blocks of a tile and the tiles of an expert share its L2
@@ -516,9 +533,9 @@ __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) 
     const int4 tl = a.tiles[tix];
     if constexpr (NT > 1) {
         // an expert's last tile, if at most half full, in half the instructions
-        if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, F32>(a, tl, bk, sp, xs[0], ent);
+        if (tl.z <= TM / 2) return tile_product<UP, NP, P, NT / 2, F32>(a, tl, bk, sp, xs[0], ent);
     }
-    tile_product<UP, NP, NT, F32>(a, tl, bk, sp, xs[0], ent);
+    tile_product<UP, NP, P, NT, F32>(a, tl, bk, sp, xs[0], ent);
 }
 
 // y[t] = the sum of its entries' terms, in the entries' order.
@@ -685,7 +702,7 @@ __global__ __launch_bounds__(64 * NW) void mx_up_decode(MxArgs a) {
         for (int m = 0; m < 2; ++m) {
 #pragma unroll
             for (int j = 0; j < TPW; ++j)
-                d.w[m][j] = load_codes(ref, uint32_t(m ? L.up : L.gate) + wc + uint32_t(min(kt0 + j, KT - 1)) * kTileBytes, lane);
+                d.w[m][j] = load_codes<true>(ref, uint32_t(m ? L.up : L.gate) + wc + uint32_t(min(kt0 + j, KT - 1)) * kTileBytes, lane);
             d.s[m] = __builtin_amdgcn_raw_buffer_load_b32(ref, int(lane * 4u), int(uint32_t(m ? L.up_s : L.gate_s) + sc), 0);
         }
     };
@@ -766,7 +783,7 @@ __global__ __launch_bounds__(kThreads) void mx_up_wide(MxArgs a, int nrb) {
     auto load = [&](Stage& d, int kt) __attribute__((always_inline)) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            d.w[m] = load_codes(ref, uint32_t(m ? L.up : L.gate) + wc + uint32_t(kt) * kTileBytes, lane);
+            d.w[m] = load_codes<true>(ref, uint32_t(m ? L.up : L.gate) + wc + uint32_t(kt) * kTileBytes, lane);
             d.s[m] = load_scale(ref, uint32_t(m ? L.up_s : L.gate_s) + sc, kt, lane);
         }
 #pragma unroll
@@ -828,7 +845,6 @@ template <int NH, bool PC, bool YF, int NW, int U, int R>
 __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) {
     constexpr int MP = PC ? 1 : NH;                         // instructions per operand
     constexpr int N = 64 * NW, OUT = R * 256;
-    static_assert(OUT <= N, "a thread sums one output");
     __shared__ SlotTable tab;
     __shared__ float red[2][NW][OUT];
     const uint32_t lane = threadIdx.x & 63;
@@ -863,7 +879,7 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const uint32_t b = uint32_t(min(grp * R + i, NB - 1));
-                d.w[j][i] = load_codes(ref, uint32_t(L.down) + (b * uint32_t(KT) + uint32_t(kt)) * kTileBytes, lane);
+                d.w[j][i] = load_codes<true>(ref, uint32_t(L.down) + (b * uint32_t(KT) + uint32_t(kt)) * kTileBytes, lane);
                 d.s[j][i] = load_scale(ref, uint32_t(L.down_s) + b * uint32_t(KG) * kGroupBytes, kt, lane);
             }
         }
@@ -908,23 +924,25 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
             for (int r = 0; r < 4; ++r) red[buf][wave][(i * 4 + r) * 64 + lane] = sum[r];
         }
         lds_barrier();
-        if (tid >= OUT) return;
-        float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) v += red[buf][w][tid];
-        if (!direct) {
-            a.split[size_t(item) * OUT + tid] = v;
-            return;
+        for (int o = tid; o < OUT; o += N) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) v += red[buf][w][o];
+            if (!direct) {
+                a.split[size_t(item) * OUT + o] = v;
+                continue;
+            }
+            float s = v;
+            if constexpr (PC) {
+                s += __shfl_down(v, 1, 64);
+                s += __shfl_down(v, 2, 64);
+            }
+            const int row = (item * R + o / 256) * kTileRows + 4 * q + (o / 64 & 3);
+            if (t >= a.T || pc || row >= a.H) continue;
+            if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = s;
+            else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
         }
-        float s = v;
-        if constexpr (PC) {
-            s += __shfl_down(v, 1, 64);
-            s += __shfl_down(v, 2, 64);
-        }
-        const int grp = item, row = (grp * R + tid / 256) * kTileRows + 4 * q + (tid / 64 & 3);
-        if (t >= a.T || pc || row >= a.H) return;
-        if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = s;
-        else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
     };
     int chunk = -1;
     if (lo < hi) load(st[0], lo);
@@ -969,9 +987,9 @@ __global__ __launch_bounds__(1024) void mx_join_kernel(MxArgs a) {
 }
 
 // The down launch's forms: up to 48 column tiles of few columns in one chunk of
-// sixteen waves, else chunks of 16 tiles.
+// sixteen waves, else chunks of eight tiles.
 constexpr int kOneWaves = 16, kOneU = 3, kOneR = 1;
-constexpr int kRunWaves = 8, kRunU = 2, kRunR = 2;
+constexpr int kRunWaves = 8, kRunU = 1, kRunR = 4;
 
 struct MxLayout {
     int tm, max_tiles, tsplits, slots, units;
@@ -1047,7 +1065,7 @@ int launch_down_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
     }
     const int64_t chunks = (L.units + kRunWaves * kRunU - 1) / (kRunWaves * kRunU);
     const int64_t work = chunks * ((NB + kRunR - 1) / kRunR);
-    hipLaunchKernelGGL((mx_down_decode<NH, PC, YF, kRunWaves, kRunU, kRunR>), dim3(unsigned(work < 256 ? work : 256)),
+    hipLaunchKernelGGL((mx_down_decode<NH, PC, YF, kRunWaves, kRunU, kRunR>), dim3(unsigned(work < 512 ? work : 512)),
                        dim3(64 * kRunWaves), 0, s, a, chunks == 1);
     STMOE_LAUNCHED();
     if (chunks > 1) {

@@ -281,27 +281,30 @@ def test_ffn_values_beyond_bf16_range_of_fp32_x():
     assert _err(y[2:], want[2:]) <= _tol(False, False)
 
 
-@pytest.mark.parametrize("T", [1, 9, 16, 70, 600])
-def test_ffn_same_bits_and_independent_tokens(T):
+@pytest.mark.parametrize("x_bf16,y_bf16", [(True, False), (False, False), (False, True)])
+@pytest.mark.parametrize("T", [1, 9, 16, 40, 70, 200, 600])
+def test_ffn_same_bits_and_independent_tokens(T, x_bf16, y_bf16):
     """The same call twice gives the same bits; beyond a decode step's 16 tokens a token's bits do not depend on the
     tokens beside it as long as the call's size stays (in a step the order of its sums goes by the experts selected)."""
     import torch
     H, I, E, K = 520, 264, 12, 3
+    xd, yd = (torch.bfloat16 if b else torch.float32 for b in (x_bf16, y_bf16))
     ex = Experts(E, H, I, 8)
-    x, idx, w = _inputs(T, K, E, H, 4, torch.bfloat16)
-    out = torch.full((T + 2, H), 5.0, device=DEV)
-    a = _run(ex, E, H, I, x, idx, w, torch.float32, y=out[:T])
+    x, idx, w = _inputs(T, K, E, H, 4, xd)
+    out = torch.full((T + 2, H), 5.0, dtype=yd, device=DEV)
+    a = _run(ex, E, H, I, x, idx, w, yd, y=out[:T])
     assert bool((out[T:] == 5).all())
-    b = _run(ex, E, H, I, x, idx, w, torch.float32)
+    b = _run(ex, E, H, I, x, idx, w, yd)
     assert torch.equal(a, b)
     if T > 1:
-        x2, idx2, w2 = _inputs(T, K, E, H, 5, torch.bfloat16)
-        x2[T // 2], idx2[T // 2], w2[T // 2] = x[T // 2], idx[T // 2], w[T // 2]
-        c = _run(ex, E, H, I, x2, idx2, w2, torch.float32)
+        x2, idx2, w2 = _inputs(T, K, E, H, 5, xd)
+        keep = slice(T // 2, T // 2 + 9) if T > 32 else slice(T // 2, T // 2 + 1)
+        x2[keep], idx2[keep], w2[keep] = x[keep], idx[keep], w[keep]
+        c = _run(ex, E, H, I, x2, idx2, w2, yd)
         if T > 16:
-            assert torch.equal(c[T // 2], b[T // 2])
+            assert torch.equal(c[keep], b[keep])
         else:
-            assert _err(c[T // 2:T // 2 + 1], _f64(b[T // 2:T // 2 + 1])) <= _tol(True, False)
+            assert _err(c[keep], _f64(b[keep])) <= _tol(x_bf16, y_bf16)
 
 
 def test_ffn_no_tokens():
