@@ -259,27 +259,40 @@ def _dt(name, t):
     return d
 
 
-def _dense(name, t, shape, dtypes):
-    """t: a contiguous CUDA tensor of this shape and one of these dtypes, on the current device."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _device(name, t):
+    """Index of t's device, which has to be the current one."""
+    d = t.get_device()
+    if d < 0 or d != torch.cuda.current_device():
         raise ValueError(f"{name} must be on the current CUDA device")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor, not {list(t.shape)}")
+    return d
+
+
+def _dense(name, t, shape, dtypes, dev):
+    """t: a contiguous tensor of this shape and one of these dtypes, on device dev."""
+    if t.get_device() == dev and t.shape == shape and t.dtype in dtypes and t.is_contiguous():
+        return
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the current CUDA device")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} has dtype {t.dtype}")
+    raise ValueError(f"{name} must be a contiguous {list(shape)} tensor, not {list(t.shape)}")
 
 
 def _rows(name, t):
     """(rows, columns, row stride) of a matrix whose rows are contiguous and do not overlap."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current CUDA device")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
     r, c = t.shape
-    ld = t.stride(0) if r > 1 else max(c, 1)
+    s, one = t.stride()
+    if one != 1 and c > 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    ld = s if r > 1 else max(c, 1)
     if ld < c:
         raise ValueError(f"the rows of {name} overlap")
     return r, c, ld
+
+
+_I32, _F32, _U8 = (torch.int32,), (torch.float32,), (torch.uint8,)
 
 
 # ------------------------------------------------------------- router of a batch
@@ -291,34 +304,38 @@ def route_balance(logits, K, idx, w, counts, n_tokens, loss, ws, renorm=False, m
                   stream=None):
     """Top-K, per-expert counts, balance and z loss of a batch of logits [T][E] (rows may be strided)."""
     T, E, ld = _rows("logits", logits)
-    _dense("idx", idx, (T, K), (torch.int32,))
-    _dense("w", w, (T, K), (torch.float32,))
-    _dense("counts", counts, (E,), (torch.int32,))
-    _dense("n_tokens", n_tokens, (1,), (torch.int32,))
-    _dense("loss", loss, (2,), (torch.float32,))
+    dev = _device("logits", logits)
+    _dense("idx", idx, (T, K), _I32, dev)
+    _dense("w", w, (T, K), _F32, dev)
+    _dense("counts", counts, (E,), _I32, dev)
+    _dense("n_tokens", n_tokens, (1,), _I32, dev)
+    _dense("loss", loss, (2,), _F32, dev)
     if prob_sum is not None:
-        _dense("prob_sum", prob_sum, (E,), (torch.float32,))
+        _dense("prob_sum", prob_sum, (E,), _F32, dev)
     if mask is not None:
-        _dense("mask", mask, (T,), (torch.uint8, torch.bool))
-    _call("moe_route_balance", _p(logits), T, ld, E, K, _dt("logits", logits), int(renorm), _p(mask), _p(idx),
-          _p(w), _p(counts), _p(n_tokens), _p(prob_sum), _p(loss), _p(ws), ws.numel() * ws.element_size(), _s(stream))
+        _dense("mask", mask, (T,), (torch.uint8, torch.bool), dev)
+    _call("moe_route_balance", logits.data_ptr(), T, ld, E, K, _dt("logits", logits), int(renorm), _p(mask),
+          idx.data_ptr(), w.data_ptr(), counts.data_ptr(), n_tokens.data_ptr(), _p(prob_sum), loss.data_ptr(),
+          ws.data_ptr(), ws.nbytes, _s(stream))
 
 
 def route_balance_backward(logits, idx, counts, n_tokens, d_loss, d_logits, d_w=None, renorm=False, stream=None):
     """d_logits of route_balance, from the gradients of the gate weights and of the two losses."""
     T, E, ld = _rows("logits", logits)
-    K = idx.shape[1]
-    _dense("idx", idx, (T, K), (torch.int32,))
-    _dense("counts", counts, (E,), (torch.int32,))
-    _dense("n_tokens", n_tokens, (1,), (torch.int32,))
-    _dense("d_loss", d_loss, (2,), (torch.float32,))
-    if d_w is not None:
-        _dense("d_w", d_w, (T, K), (torch.float32,))
     Td, Ed, ld_d = _rows("d_logits", d_logits)
-    if (Td, Ed) != (T, E) or d_logits.dtype != logits.dtype:
-        raise ValueError("d_logits must have the shape and dtype of logits")
-    _call("moe_route_balance_backward", _p(logits), T, ld, E, K, _dt("logits", logits), int(renorm), _p(idx),
-          _p(counts), _p(n_tokens), _p(d_w), _p(d_loss), _p(d_logits), ld_d, _s(stream))
+    dev = _device("logits", logits)
+    K = idx.shape[1]
+    if (Td, Ed) != (T, E) or d_logits.dtype != logits.dtype or d_logits.get_device() != dev:
+        raise ValueError("d_logits must have the shape, dtype and device of logits")
+    _dense("idx", idx, (T, K), _I32, dev)
+    _dense("counts", counts, (E,), _I32, dev)
+    _dense("n_tokens", n_tokens, (1,), _I32, dev)
+    _dense("d_loss", d_loss, (2,), _F32, dev)
+    if d_w is not None:
+        _dense("d_w", d_w, (T, K), _F32, dev)
+    _call("moe_route_balance_backward", logits.data_ptr(), T, ld, E, K, _dt("logits", logits), int(renorm),
+          idx.data_ptr(), counts.data_ptr(), n_tokens.data_ptr(), _p(d_w), d_loss.data_ptr(), d_logits.data_ptr(), ld_d,
+          _s(stream))
 
 
 # ------------------------------------------------------------- predictor
@@ -419,25 +436,28 @@ def expert_ffn_noalloc(x, idx, w, H, I, E, dtype, expert_ptrs, y, shared_ptrs=No
 def mx_quantize(x, codes, scales, stream=None):
     """x [rows][cols] (rows may be strided) to codes [rows][ceil(cols/2)] and scales [rows][ceil(cols/32)], uint8."""
     r, c, ld = _rows("x", x)
-    _dense("codes", codes, (r, (c + 1) // 2), (torch.uint8,))
-    _dense("scales", scales, (r, (c + 31) // 32), (torch.uint8,))
-    _call("moe_mx_quantize", _p(x), r, c, ld, _dt("x", x), _p(codes), _p(scales), _s(stream))
+    dev = _device("x", x)
+    _dense("codes", codes, (r, (c + 1) // 2), _U8, dev)
+    _dense("scales", scales, (r, (c + 31) // 32), _U8, dev)
+    _call("moe_mx_quantize", x.data_ptr(), r, c, ld, _dt("x", x), codes.data_ptr(), scales.data_ptr(), _s(stream))
 
 
 def mx_dequantize(codes, scales, y, stream=None):
     """The values of codes and scales into y [rows][cols] (rows may be strided)."""
     r, c, ld = _rows("y", y)
-    _dense("codes", codes, (r, (c + 1) // 2), (torch.uint8,))
-    _dense("scales", scales, (r, (c + 31) // 32), (torch.uint8,))
-    _call("moe_mx_dequantize", _p(codes), _p(scales), r, c, _p(y), ld, _dt("y", y), _s(stream))
+    dev = _device("y", y)
+    _dense("codes", codes, (r, (c + 1) // 2), _U8, dev)
+    _dense("scales", scales, (r, (c + 31) // 32), _U8, dev)
+    _call("moe_mx_dequantize", codes.data_ptr(), scales.data_ptr(), r, c, y.data_ptr(), ld, _dt("y", y), _s(stream))
 
 
 def mx_pack_expert(gate, up, down, H, I, blob, stream=None):
     """Pack an expert for expert_ffn_mx: gate, up [I][H] and down [H][I], each (codes, scales), into blob (device)."""
+    dev = _device("blob", blob)
     for name, (codes, scales), r, c in (("gate", gate, I, H), ("up", up, I, H), ("down", down, H, I)):
-        _dense(f"{name} codes", codes, (r, c // 2), (torch.uint8,))
-        _dense(f"{name} scales", scales, (r, (c + 31) // 32), (torch.uint8,))
-    _dense("blob", blob, (blob_bytes(H, I, MXFP4),), (torch.uint8,))
+        _dense(f"{name} codes", codes, (r, c // 2), _U8, dev)
+        _dense(f"{name} scales", scales, (r, (c + 31) // 32), _U8, dev)
+    _dense("blob", blob, (blob_bytes(H, I, MXFP4),), _U8, dev)
     _call("moe_mx_pack_expert", _p(gate[0]), _p(gate[1]), _p(up[0]), _p(up[1]), _p(down[0]), _p(down[1]), H, I,
           _p(blob), _s(stream))
 
@@ -450,15 +470,17 @@ def ffn_mx_workspace_bytes(T, K, E, H, I, n_shared=0, dtype=torch.bfloat16, y_dt
 def expert_ffn_mx(x, idx, w, H, I, E, expert_ptrs, y, ws, shared_ptrs=None, n_shared=0, stream=None):
     """The expert FFN of tokens x [T][H] over MXFP4 blobs (mx_pack_expert)."""
     T, K = idx.shape
-    _dense("x", x, (T, H), tuple(_DTYPES))
-    _dense("idx", idx, (T, K), (torch.int32,))
-    _dense("w", w, (T, K), (torch.float32,))
-    _dense("y", y, (T, H), tuple(_DTYPES))
-    _dense("expert_ptrs", expert_ptrs, (E,), (torch.int64,))
+    dev = _device("x", x)
+    _dense("x", x, (T, H), _DTYPES, dev)
+    _dense("idx", idx, (T, K), _I32, dev)
+    _dense("w", w, (T, K), _F32, dev)
+    _dense("y", y, (T, H), _DTYPES, dev)
+    _dense("expert_ptrs", expert_ptrs, (E,), (torch.int64,), dev)
     if n_shared:
-        _dense("shared_ptrs", shared_ptrs, (n_shared,), (torch.int64,))
-    _call("moe_expert_ffn_mx", _p(x), _p(idx), _p(w), T, K, H, I, E, _dt("x", x), _dt("y", y), _p(expert_ptrs),
-          _p(shared_ptrs), n_shared, _p(y), _p(ws), ws.numel() * ws.element_size(), _s(stream))
+        _dense("shared_ptrs", shared_ptrs, (n_shared,), (torch.int64,), dev)
+    _call("moe_expert_ffn_mx", x.data_ptr(), idx.data_ptr(), w.data_ptr(), T, K, H, I, E, _DTYPES[x.dtype],
+          _DTYPES[y.dtype], expert_ptrs.data_ptr(), _p(shared_ptrs), n_shared, y.data_ptr(), ws.data_ptr(), ws.nbytes,
+          _s(stream))
 
 
 # ------------------------------------------------------------- cache policy
