@@ -15,25 +15,46 @@ using namespace mx;
 constexpr int kThreads = 256;
 constexpr int kUnit = 8;                        // columns per lane
 constexpr int kUnitsPerBlock = kBlock / kUnit;  // lanes per block
+constexpr int kAhead = 2;                       // units a lane has in flight
+
+// Rows start at any element: the loads and stores below are whole vectors of
+// their type's own alignment, which the memory pipeline takes at any address.
+// x is read once, past the caches (14336 x 4096 bf16: 30.5 us through them, 26.8
+// past them).
+template <class V, class E>
+__device__ __forceinline__ V load_once(const E* p) {
+    typedef V Any __attribute__((aligned(alignof(E))));
+    return __builtin_nontemporal_load(reinterpret_cast<const Any*>(p));
+}
+template <class V, class E>
+__device__ __forceinline__ V load_vec(const E* p) {
+    V v;
+    __builtin_memcpy(&v, __builtin_assume_aligned(p, alignof(E)), sizeof(V));
+    return v;
+}
+template <class V, class E>
+__device__ __forceinline__ void store_vec(E* p, V v) {
+    __builtin_memcpy(__builtin_assume_aligned(p, alignof(E)), &v, sizeof(V));
+}
 
 template <bool BF>
-__device__ __forceinline__ void load_unit(const void* x, int64_t at, int n, bool vec, float (&v)[kUnit]) {
+__device__ __forceinline__ void load_unit(const void* x, int64_t at, int n, float (&v)[kUnit]) {
     if (BF) {
         const uint16_t* p = reinterpret_cast<const uint16_t*>(x) + at;
-        if (vec && n == kUnit) {
-            const uint4 q = *reinterpret_cast<const uint4*>(p);
-            v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
-            v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
+        if (n == kUnit) {
+            const u32x4 q = load_once<u32x4>(p);
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) v[i] = i % 2 ? bf16_hi(q[i / 2]) : bf16_lo(q[i / 2]);
         } else {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) v[i] = i < n ? __uint_as_float(uint32_t(p[i]) << 16) : 0.f;
         }
     } else {
         const float* p = reinterpret_cast<const float*>(x) + at;
-        if (vec && n == kUnit) {
-            const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        if (n == kUnit) {
+            const f32x4 a = load_once<f32x4>(p), b = load_once<f32x4>(p + 4);
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) v[i] = i < 4 ? a[i & 3] : b[i & 3];
         } else {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) v[i] = i < n ? p[i] : 0.f;
@@ -41,83 +62,136 @@ __device__ __forceinline__ void load_unit(const void* x, int64_t at, int n, bool
     }
 }
 
-// `vec`: x and its row stride are 16-byte aligned.  `vec_out`: so are the rows
-// of codes to 4 bytes.
-template <bool BF>
+// A unit's row and column.  FLAT: whole blocks in contiguous rows, where the
+// matrix is one long row; else a 32-bit division (a 64-bit one where the units
+// need it would cost more than the unit's memory time).
+template <bool FLAT, int W>
+__device__ __forceinline__ void place(int64_t u, int upr, int64_t& row, int& col) {
+    if (FLAT) return;
+    if (u >> 32 == 0) {
+        row = int64_t(uint32_t(u) / uint32_t(upr));
+    } else {
+        row = u / upr;
+    }
+    col = int(u - row * upr) * W;
+}
+
+template <bool BF, bool FLAT>
 __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const void* x, int64_t rows, int cols, int64_t ld,
-                                                              uint8_t* codes, uint8_t* scales, int vec, int vec_out) {
+                                                              uint8_t* codes, uint8_t* scales) {
     const int nb = (cols + kBlock - 1) / kBlock, upr = nb * kUnitsPerBlock, cb = (cols + 1) / 2;
     const int64_t total = rows * upr, step = int64_t(gridDim.x) * kThreads;
-    // the four lanes of a block run the same rounds: total and kThreads are multiples of four
-    for (int64_t u = int64_t(blockIdx.x) * kThreads + threadIdx.x; u < total; u += step) {
-        const int64_t row = u / upr;
-        const int c = int(u - row * upr), col = c * kUnit;
-        const int n = cols - col < 0 ? 0 : cols - col < kUnit ? cols - col : kUnit;
-        float v[kUnit];
-        load_unit<BF>(x, row * ld + col, n, vec != 0, v);
-        uint32_t top = 0u;
+    // the four lanes of a block go together: total and kThreads are multiples of four
+    for (int64_t u0 = int64_t(blockIdx.x) * kThreads + threadIdx.x; u0 < total; u0 += kAhead * step) {
+        float v[kAhead][kUnit];
+        int64_t row[kAhead];
+        int col[kAhead], n[kAhead];
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) {
-            const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
-            top = a > top ? a : top;
+        for (int a = 0; a < kAhead; ++a) {
+            const int64_t u = u0 + a * step;
+            row[a] = 0;
+            col[a] = 0;
+            n[a] = 0;
+            if (u < total) {
+                place<FLAT, kUnit>(u, upr, row[a], col[a]);
+                n[a] = FLAT ? kUnit : max(0, min(kUnit, cols - col[a]));
+            }
+            load_unit<BF>(x, FLAT ? u * kUnit : row[a] * ld + col[a], n[a], v[a]);
         }
 #pragma unroll
-        for (int m = 1; m < kUnitsPerBlock; m <<= 1) {
-            const uint32_t o = uint32_t(__shfl_xor(int(top), m, 64));
-            top = o > top ? o : top;
+        for (int a = 0; a < kAhead; ++a) {
+            const int64_t u = u0 + a * step;
+            if (u >= total) break;
+            uint32_t top = 0u;
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) top = max(top, __float_as_uint(v[a][i]) & 0x7fffffffu);
+            // the block's four lanes: their neighbour, then the other pair
+            top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0xB1, 0xf, 0xf, false)));
+            top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0x4E, 0xf, 0xf, false)));
+            const uint32_t s = scale_byte(top);
+            const uint32_t q = s == 255u ? 0u : encode8(v[a], scale_of(s));
+            if (FLAT) {
+                reinterpret_cast<uint32_t*>(codes)[u] = q;
+                if (u % kUnitsPerBlock == 0) scales[u / kUnitsPerBlock] = uint8_t(s);
+                continue;
+            }
+            uint8_t* o = codes + row[a] * cb + col[a] / 2;
+            if (n[a] == kUnit) {
+                store_vec(o, q);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kUnit / 2; ++i)
+                    if (2 * i < n[a]) o[i] = uint8_t(q >> (8 * i));
+            }
+            if (col[a] % kBlock == 0) scales[row[a] * nb + col[a] / kBlock] = uint8_t(s);
         }
-        const uint32_t s = scale_byte(top);
-        const uint32_t q = s == 255u ? 0u : encode8(v, scale_of(s));
-        uint8_t* o = codes + row * cb + col / 2;
-        if (vec_out && n == kUnit) {
-            *reinterpret_cast<uint32_t*>(o) = q;
-        } else {
-            for (int i = 0; 2 * i < n; ++i) o[i] = uint8_t(q >> (8 * i));
-        }
-        if (c % kUnitsPerBlock == 0) scales[row * nb + c / kUnitsPerBlock] = uint8_t(s);
     }
 }
 
+// Reading back, a lane takes the columns of one 16-byte store, so that a wave's
+// stores are contiguous (1000 x 2061 fp32: 17 us with eight columns a lane, 5
+// with four).
 template <bool BF>
-__global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(const uint8_t* codes, const uint8_t* scales,
-                                                                int64_t rows, int cols, void* y, int64_t ld,
-                                                                int vec_in, int vec) {
-    const int nb = (cols + kBlock - 1) / kBlock, upr = (cols + kUnit - 1) / kUnit, cb = (cols + 1) / 2;
-    const int64_t total = rows * upr, step = int64_t(gridDim.x) * kThreads;
-    for (int64_t u = int64_t(blockIdx.x) * kThreads + threadIdx.x; u < total; u += step) {
-        const int64_t row = u / upr;
-        const int c = int(u - row * upr), col = c * kUnit;
-        const int n = cols - col < kUnit ? cols - col : kUnit;
-        const uint8_t* p = codes + row * cb + col / 2;
-        uint32_t q = 0u;
-        if (vec_in && n == kUnit) {
-            q = *reinterpret_cast<const uint32_t*>(p);
+constexpr int kOut = BF ? 8 : 4;
+
+template <bool BF>
+__device__ __forceinline__ void store_unit(void* y, int64_t at, int n, uint32_t codes, float scale) {
+    const bf16x8 d = decode8(codes, scale);
+    if (BF) {
+        __bf16* o = reinterpret_cast<__bf16*>(y) + at;
+        if (n == 8) {
+            store_vec(o, d);
         } else {
-            for (int i = 0; 2 * i < n; ++i) q |= uint32_t(p[i]) << (8 * i);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) o[i] = d[i];
         }
-        const float s = scale_of(scales[row * nb + c / kUnitsPerBlock]);
-        union {
-            bf16x8 v;
-            uint4 q;
-            uint16_t h[8];
-        } d;
-        d.v = decode8(q, s);
-        if (BF) {
-            uint16_t* o = reinterpret_cast<uint16_t*>(y) + row * ld + col;
-            if (vec && n == kUnit) {
-                *reinterpret_cast<uint4*>(o) = d.q;
-            } else {
-                for (int i = 0; i < n; ++i) o[i] = d.h[i];
-            }
+    } else {
+        float* o = reinterpret_cast<float*>(y) + at;
+        if (n == 4) {
+            store_vec(o, f32x4{float(d[0]), float(d[1]), float(d[2]), float(d[3])});
         } else {
-            float* o = reinterpret_cast<float*>(y) + row * ld + col;
-            if (vec && n == kUnit) {
-                *reinterpret_cast<float4*>(o) = make_float4(bf16_lo(d.q.x), bf16_hi(d.q.x), bf16_lo(d.q.y), bf16_hi(d.q.y));
-                *reinterpret_cast<float4*>(o + 4) =
-                    make_float4(bf16_lo(d.q.z), bf16_hi(d.q.z), bf16_lo(d.q.w), bf16_hi(d.q.w));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < n) o[i] = float(d[i]);
+        }
+    }
+}
+
+template <bool BF, bool FLAT>
+__global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(const uint8_t* codes, const uint8_t* scales,
+                                                                int64_t rows, int cols, void* y, int64_t ld) {
+    constexpr int W = kOut<BF>, PB = kBlock / W;            // columns per lane, lanes per block
+    const int nb = (cols + kBlock - 1) / kBlock, upr = (cols + W - 1) / W, cb = (cols + 1) / 2;
+    const int64_t total = rows * upr, step = int64_t(gridDim.x) * kThreads;
+    for (int64_t u0 = int64_t(blockIdx.x) * kThreads + threadIdx.x; u0 < total; u0 += kAhead * step) {
+        uint32_t q[kAhead], s[kAhead];
+        int64_t row[kAhead];
+        int col[kAhead], n[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int64_t u = u0 + a * step;
+            q[a] = 0u;
+            if (u >= total) break;
+            row[a] = 0;
+            col[a] = 0;
+            place<FLAT, W>(u, upr, row[a], col[a]);
+            n[a] = FLAT ? W : min(W, cols - col[a]);
+            const uint8_t* p = codes + (FLAT ? u * (W / 2) : row[a] * cb + col[a] / 2);
+            if (n[a] == W) {
+                q[a] = W == 8 ? load_vec<uint32_t>(p) : load_vec<uint16_t>(p);
             } else {
-                for (int i = 0; i < n; ++i) o[i] = __uint_as_float(uint32_t(d.h[i]) << 16);
+#pragma unroll
+                for (int i = 0; i < W / 2; ++i)
+                    if (2 * i < n[a]) q[a] |= uint32_t(p[i]) << (8 * i);
             }
+            s[a] = scales[FLAT ? u / PB : row[a] * nb + col[a] / kBlock];
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int64_t u = u0 + a * step;
+            if (u >= total) break;
+            store_unit<BF>(y, FLAT ? u * W : row[a] * ld + col[a], n[a], q[a], scale_of(s[a]));
         }
     }
 }
@@ -145,9 +219,10 @@ __global__ __launch_bounds__(kThreads) void mx_pack_kernel(const uint8_t* codes,
         in ? scales[size_t(row) * nb + blk] : 0;
 }
 
+// One unit per lane up to a few rounds of workgroups, then kAhead.
 int grid_of(int64_t units) {
     const int64_t wg = (units + kThreads - 1) / kThreads;
-    return int(wg < 1 ? 1 : wg < 65536 ? wg : 65536);
+    return int(wg <= 2048 ? (wg < 1 ? 1 : wg) : wg <= 2048 * kAhead ? 2048 : wg / kAhead < 16384 ? wg / kAhead : 16384);
 }
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -176,15 +251,17 @@ extern "C" int moe_mx_quantize(const void* x, int64_t rows, int cols, int64_t ld
     STMOE_CHECK(x && codes && scales, "null pointer");
     const size_t esz = dtype == STMOE_BF16 ? 2 : 4;
     STMOE_CHECK(aligned(x, esz), "x must be aligned to its elements");
-    const int vec = aligned(x, 16) && ld * esz % 16 == 0, vec_out = aligned(codes, 4) && (cols + 1) / 2 % 4 == 0;
     const int nb = (cols + mx::kBlock - 1) / mx::kBlock;
-    const dim3 grid(unsigned(grid_of(rows * nb * kUnitsPerBlock)));
-    if (dtype == STMOE_BF16)
-        hipLaunchKernelGGL((mx_quantize_kernel<true>), grid, dim3(kThreads), 0, as_stream(stream), x, rows, cols, ld,
-                           codes, scales, vec, vec_out);
-    else
-        hipLaunchKernelGGL((mx_quantize_kernel<false>), grid, dim3(kThreads), 0, as_stream(stream), x, rows, cols, ld,
-                           codes, scales, vec, vec_out);
+    const dim3 grid(unsigned(grid_of(rows * nb * kUnitsPerBlock))), block(kThreads);
+    const bool flat = ld == cols && cols % mx::kBlock == 0 && aligned(codes, 4);
+    hipStream_t s = as_stream(stream);
+    if (dtype == STMOE_BF16) {
+        if (flat) hipLaunchKernelGGL((mx_quantize_kernel<true, true>), grid, block, 0, s, x, rows, cols, ld, codes, scales);
+        else hipLaunchKernelGGL((mx_quantize_kernel<true, false>), grid, block, 0, s, x, rows, cols, ld, codes, scales);
+    } else {
+        if (flat) hipLaunchKernelGGL((mx_quantize_kernel<false, true>), grid, block, 0, s, x, rows, cols, ld, codes, scales);
+        else hipLaunchKernelGGL((mx_quantize_kernel<false, false>), grid, block, 0, s, x, rows, cols, ld, codes, scales);
+    }
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
@@ -197,14 +274,17 @@ extern "C" int moe_mx_dequantize(const uint8_t* codes, const uint8_t* scales, in
     STMOE_CHECK(y && codes && scales, "null pointer");
     const size_t esz = dtype == STMOE_BF16 ? 2 : 4;
     STMOE_CHECK(aligned(y, esz), "y must be aligned to its elements");
-    const int vec = aligned(y, 16) && ld * esz % 16 == 0, vec_in = aligned(codes, 4) && (cols + 1) / 2 % 4 == 0;
-    const dim3 grid(unsigned(grid_of(rows * ((cols + kUnit - 1) / kUnit))));
-    if (dtype == STMOE_BF16)
-        hipLaunchKernelGGL((mx_dequantize_kernel<true>), grid, dim3(kThreads), 0, as_stream(stream), codes, scales,
-                           rows, cols, y, ld, vec_in, vec);
-    else
-        hipLaunchKernelGGL((mx_dequantize_kernel<false>), grid, dim3(kThreads), 0, as_stream(stream), codes, scales,
-                           rows, cols, y, ld, vec_in, vec);
+    const int w = dtype == STMOE_BF16 ? kOut<true> : kOut<false>;
+    const dim3 grid(unsigned(grid_of(rows * ((cols + w - 1) / w)))), block(kThreads);
+    const bool flat = ld == cols && cols % mx::kBlock == 0 && aligned(codes, 4);
+    hipStream_t s = as_stream(stream);
+    if (dtype == STMOE_BF16) {
+        if (flat) hipLaunchKernelGGL((mx_dequantize_kernel<true, true>), grid, block, 0, s, codes, scales, rows, cols, y, ld);
+        else hipLaunchKernelGGL((mx_dequantize_kernel<true, false>), grid, block, 0, s, codes, scales, rows, cols, y, ld);
+    } else {
+        if (flat) hipLaunchKernelGGL((mx_dequantize_kernel<false, true>), grid, block, 0, s, codes, scales, rows, cols, y, ld);
+        else hipLaunchKernelGGL((mx_dequantize_kernel<false, false>), grid, block, 0, s, codes, scales, rows, cols, y, ld);
+    }
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
