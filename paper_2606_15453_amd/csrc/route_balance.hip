@@ -127,8 +127,10 @@ __device__ __forceinline__ void load_row(const void* logits, int64_t at, int E, 
     }
 }
 
-// exp(z - top) of a candidate; none (0) for minus infinity.
-__device__ __forceinline__ float term(float z, float top) { return z == -INFINITY ? 0.f : expf(z - top); }
+// exp(z - top) of a candidate; none (0) for minus infinity.  The hardware's
+// exponential: the product with log2(e) rounds to 2^-24 of |z - top|, as the
+// difference itself does.
+__device__ __forceinline__ float term(float z, float top) { return z == -INFINITY ? 0.f : __expf(z - top); }
 
 template <bool BF, int V, bool VEC>
 __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
@@ -151,13 +153,12 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
         const int64_t t = t0 + r;
         const bool in = t < a.T;
         float z[V];
-        // rows beyond the batch and masked ones have no candidates
-        if (in && !(a.mask && !a.mask[t])) {
-            load_row<BF, V, VEC>(a.logits, t * a.ld, a.E, l, z);
-        } else {
+        // rows beyond the batch and masked ones have no candidates (the row and
+        // its mask are loaded side by side)
+        const uint8_t counts = in && a.mask ? a.mask[t] : uint8_t(in);
+        load_row<BF, V, VEC>(a.logits, (in ? t : a.T - 1) * a.ld, a.E, l, z);
 #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = -INFINITY;
-        }
+        for (int v = 0; v < V; ++v) z[v] = counts ? z[v] : -INFINITY;
         uint32_t key[V], best = 0u;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -190,19 +191,18 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
             uint32_t at = ~0u;
 #pragma unroll
             for (int v = V - 1; v >= 0; --v) at = key[v] == best ? uint32_t(expert_at<VEC>(v, l)) : at;
-            at = row_min(at);
+            at = best ? row_min(at) : ~0u;
             if (l == k && best) {
                 mine = int(at);
                 won = best;
             }
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const bool hit = best && at == uint32_t(expert_at<VEC>(v, l));
-                key[v] = hit ? 0u : key[v];
-                cs[v] += hit;
-            }
+            for (int v = 0; v < V; ++v) key[v] = at == uint32_t(expert_at<VEC>(v, l)) ? 0u : key[v];
         }
-        const float wk = mine >= 0 ? expf(value_of(won) - top) : 0.f;
+        // what is left of the candidates
+#pragma unroll
+        for (int v = 0; v < V; ++v) cs[v] += z[v] != -INFINITY && key[v] == 0u;
+        const float wk = mine >= 0 ? term(value_of(won), top) : 0.f;
         const float norm = a.renorm ? 1.f / row_sum(wk) : inv;
         if (in && l < a.K) {
             a.idx[t * a.K + l] = mine;
@@ -342,19 +342,17 @@ __global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradA
     for (int64_t t0 = (int64_t(blockIdx.x) * (kGradThreads / 64) + wave) * kRows; t0 < a.T; t0 += step) {
         const int64_t t = t0 + r;
         const bool in = t < a.T;
+        // the row, its selection and the weights' gradients side by side
         const int mine = in && l < a.K ? a.idx[t * a.K + l] : -1;
-        const bool live = __shfl(mine, r * kRowLanes, 64) >= 0;
+        float g = a.d_w && in && l < a.K ? a.d_w[t * a.K + l] : 0.f;
         float z[V];
-        if (live) {
-            load_row<BF, V, VEC>(a.logits, t * a.ld, a.E, l, z);
-        } else {
+        load_row<BF, V, VEC>(a.logits, (in ? t : a.T - 1) * a.ld, a.E, l, z);
+        const bool live = __shfl(mine, r * kRowLanes, 64) >= 0;
 #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = -INFINITY;
-        }
+        for (int v = 0; v < V; ++v) z[v] = live ? z[v] : -INFINITY;
         const bool chosen = a.d_w && live && mine >= 0 && mine < a.E;
-        float g = 0.f, zk = -INFINITY;
+        float zk = -INFINITY;
         if (chosen) {
-            g = a.d_w[t * a.K + l];
             zk = BF ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(a.logits)[t * a.ld + mine]) << 16)
                     : reinterpret_cast<const float*>(a.logits)[t * a.ld + mine];
         }
@@ -563,7 +561,7 @@ extern "C" int moe_route_balance_backward(const void* logits, int64_t T, int64_t
     a.d_loss = d_loss;
     a.d_logits = d_logits;
     const int64_t per = kGradThreads / 64 * kRows, wg = (T + per - 1) / per;
-    const dim3 grid(unsigned(wg < 4096 ? wg : 4096));
+    const dim3 grid(unsigned(wg < 1024 ? wg : 1024));
     const int b = int(esz);
     with_row(E, rows_of_four(logits, ld, E, b) && rows_of_four(d_logits, ld_d, E, b), [&](auto v, auto vec) {
         if (dtype == STMOE_BF16)
