@@ -20,6 +20,7 @@ using namespace mx;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanEntries = 1024;
 constexpr int kMaxShared = 8;
 constexpr int kMaxT = 65536;
 constexpr int kMaxGroups = kMaxE + kMaxShared;
@@ -224,90 +225,81 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     if (threadIdx.x == 0) a.cnt[g] = before;
 }
 
-// All experts' entries and the tiles by one workgroup, 1024 tokens at a time.
-// An expert's tokens are bits of a mask in LDS, a token's place the number of
-// bits below its own; a bit that its thread finds set is a repeated expert.
-// For up to 1024 entries: 4 us, where the two launches above take 3 us each;
-// its CU needs 4 us for every 1024 tokens (4096 tokens of top-8: 25 us).
-// The KU entries are handled side by side, without branches, so that their LDS
-// accesses overlap; entries that name no expert meet a word of their own.
+// All experts' entries and the tiles by one workgroup, a thread per token.  For
+// at most kPlanEntries entries, where it saves a launch (whole calls, H 512, I
+// 128 to 256, against the two launches above: 20 tokens of top-2 16.6 and 17.6
+// us, 128 of top-8 21.8 both, 256 of top-8 25.2 and 24.3).  An expert's tokens are bits of a mask in LDS, a token's
+// place the number of bits below its own; a bit that its thread finds set is a
+// repeated expert.  The KU entries are handled side by side, without branches,
+// so that their LDS accesses overlap; entries that name no expert meet words of
+// their own.
 template <int KU>
 __global__ __launch_bounds__(kPlanThreads) void mx_plan_kernel(MxArgs a) {
     constexpr int W = kPlanThreads / 32;                    // words of a mask
     __shared__ uint32_t mask[kMaxE + 2][W];                 // the last two: nobody's
-
     __shared__ uint16_t below[kMaxE][W];
     __shared__ int cnt[kMaxGroups], tile[kMaxGroups + 1];
-    const int tid = threadIdx.x, G = a.E + a.ns;
+    const int tid = threadIdx.x, t = tid, w = tid >> 5;
     const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
-    for (int g = tid; g < G; g += kPlanThreads) cnt[g] = g < a.E ? 0 : a.T;
+    const int32_t* row = a.idx + size_t(t < a.T ? t : 0) * a.K;
     int e[KU];
-    auto load = [&](int t) __attribute__((always_inline)) {
-        const int32_t* row = a.idx + size_t(t < a.T ? t : 0) * a.K;
 #pragma unroll
-        for (int j = 0; j < KU; j += 4) {
-            int4 v = make_int4(-1, -1, -1, -1);
-            if (four) {
-                if (j < a.K) v = *reinterpret_cast<const int4*>(row + j);
-            } else {
-                if (j < a.K) v.x = row[j];
-                if (j + 1 < a.K) v.y = row[j + 1];
-                if (j + 2 < a.K) v.z = row[j + 2];
-                if (j + 3 < a.K) v.w = row[j + 3];
-            }
-            e[j] = t < a.T ? v.x : -1;
-            e[j + 1] = t < a.T ? v.y : -1;
-            e[j + 2] = t < a.T ? v.z : -1;
-            e[j + 3] = t < a.T ? v.w : -1;
+    for (int j = 0; j < KU; j += 4) {
+        int4 v = make_int4(-1, -1, -1, -1);
+        if (four) {
+            if (j < a.K) v = *reinterpret_cast<const int4*>(row + j);
+        } else {
+            if (j < a.K) v.x = row[j];
+            if (j + 1 < a.K) v.y = row[j + 1];
+            if (j + 2 < a.K) v.z = row[j + 2];
+            if (j + 3 < a.K) v.w = row[j + 3];
         }
-    };
-    load(tid);
-    for (int t0 = 0; t0 < a.T; t0 += kPlanThreads) {
-        const int t = t0 + tid, w = tid >> 5;
-        for (int i = tid; i < a.E * W; i += kPlanThreads) mask[0][i] = 0u;
-        lds_barrier();
-        uint32_t* word[KU];
-        bool mine[KU];
-#pragma unroll
-        for (int j = 0; j < KU; ++j) {
-            mine[j] = e[j] >= 0 && e[j] < a.E;
-            word[j] = mine[j] ? &mask[e[j]][w] : &mask[kMaxE][tid & 63];
-        }
-        const uint32_t bit = 1u << (tid & 31);
-        uint32_t was[KU];
-#pragma unroll
-        for (int j = 0; j < KU; ++j) was[j] = atomicOr(word[j], mine[j] ? bit : 0u);
-#pragma unroll
-        for (int j = 0; j < KU; ++j) mine[j] &= !(was[j] & bit);
-        if (t0 + kPlanThreads < a.T) load(t + kPlanThreads);
-        lds_barrier();
-        // 32 lanes: an expert's words
-        for (int g = w; g < a.E; g += W) {
-            const int l = tid & 31, c = __builtin_popcount(mask[g][l]);
-            int v = c;
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up(v, d, 32);
-                if (l >= d) v += o;
-            }
-            below[g][l] = uint16_t(v - c);
-        }
-        lds_barrier();
-        int at[KU], to[KU];
-#pragma unroll
-        for (int j = 0; j < KU; ++j) {
-            const int g = mine[j] ? int(word[j] - &mask[0][0]) / W : 0;
-            to[j] = g;
-            at[j] = cnt[g] + below[g][w] + __builtin_popcount(mask[g][w] & (bit - 1u));
-        }
-#pragma unroll
-        for (int j = 0; j < KU; ++j)
-            if (mine[j]) a.order[size_t(to[j]) * a.T + at[j]] = t * a.ks + j;
-        if (t < a.T)
-            for (int s = 0; s < a.ns; ++s) a.order[size_t(a.E + s) * a.T + t] = t * a.ks + a.K + s;
-        lds_barrier();
-        if (tid < a.E) cnt[tid] += below[tid][W - 1] + __builtin_popcount(mask[tid][W - 1]);
-        lds_barrier();
+        e[j] = t < a.T ? v.x : -1;
+        e[j + 1] = t < a.T ? v.y : -1;
+        e[j + 2] = t < a.T ? v.z : -1;
+        e[j + 3] = t < a.T ? v.w : -1;
     }
+    for (int i = tid; i < a.E * W; i += kPlanThreads) mask[0][i] = 0u;
+    lds_barrier();
+    uint32_t* word[KU];
+    bool mine[KU];
+#pragma unroll
+    for (int j = 0; j < KU; ++j) {
+        mine[j] = e[j] >= 0 && e[j] < a.E;
+        word[j] = mine[j] ? &mask[e[j]][w] : &mask[kMaxE][tid & 63];
+    }
+    const uint32_t bit = 1u << (tid & 31);
+    uint32_t was[KU];
+#pragma unroll
+    for (int j = 0; j < KU; ++j) was[j] = atomicOr(word[j], mine[j] ? bit : 0u);
+#pragma unroll
+    for (int j = 0; j < KU; ++j) mine[j] &= !(was[j] & bit);
+    lds_barrier();
+    // 32 lanes: an expert's words
+    for (int g = w; g < a.E; g += W) {
+        const int l = tid & 31, c = __builtin_popcount(mask[g][l]);
+        int v = c;
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up(v, d, 32);
+            if (l >= d) v += o;
+        }
+        below[g][l] = uint16_t(v - c);
+        if (l == 31) cnt[g] = v;
+    }
+    if (tid < a.ns) cnt[a.E + tid] = a.T;
+    lds_barrier();
+    int at[KU], to[KU];
+#pragma unroll
+    for (int j = 0; j < KU; ++j) {
+        const int g = mine[j] ? int(word[j] - &mask[0][0]) / W : 0;
+        to[j] = g;
+        at[j] = below[g][w] + __builtin_popcount(mask[g][w] & (bit - 1u));
+    }
+#pragma unroll
+    for (int j = 0; j < KU; ++j)
+        if (mine[j]) a.order[size_t(to[j]) * a.T + at[j]] = t * a.ks + j;
+    if (t < a.T)
+        for (int s = 0; s < a.ns; ++s) a.order[size_t(a.E + s) * a.T + t] = t * a.ks + a.K + s;
     list_tiles(a, cnt, tile);
 }
 
@@ -365,24 +357,17 @@ __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lan
 // through LDS, 128 at a time, double-buffered.  A column's 256 bytes lie as 16
 // chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
 // lanes of a read, one chunk of 16 tokens, meet 16 different places.
-// Pieces of a column staged together: all of them for few tokens, where the
-// rounds' latency counts, else one (LDS).  One number for all tiles of a
-// launch: it is part of the order of a sum.
-template <int NP, int NT>
-constexpr int kStagePieces = NT <= 2 ? NP : 1;
-
 // F32: the activations keep fp32 precision (up), the terms of y are fp32
 // (down); else activations are bf16, and terms fp16 with a power of two per 64:
 // off by 2^-11 of themselves at most, an eighth of what y's own rounding is,
 // and half the bytes that the down launch writes and the sum reads (Qwen3-30B
 // sizes, 4096 tokens: 393 us with fp32 terms, 349 with these).
-template <bool UP, int NP, int P, int NT, bool F32>
+template <bool UP, int NP, int NT, bool F32>
 __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, int sp, u32x4* xs, int* ent) {
     constexpr int TM = 16 * NT;
     constexpr int RB = 4;                                   // row blocks per wave
     constexpr int CH = kTileCols / 8;                       // chunks per column
-    constexpr int Q = NP / P;                               // P pieces staged together, in Q rounds per column tile
-    constexpr int SZ = P * TM * CH;                         // chunks of a buffer
+    constexpr int SZ = NP * TM * CH;                        // chunks of a buffer
     const uint32_t lane = threadIdx.x & 63;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Blob L = blob(a.H, a.I);
@@ -412,16 +397,16 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         src[j] = uint32_t(UP ? e / a.ks : e) * uint32_t(NP * C / 8);
     }
     const int put = tid / CH * CH + (chunk ^ (tid / CH & 15));
-    u32x4 xr[P][NT], wn[RB];
+    u32x4 xr[NP][NT], wn[RB];
     uint32_t sn[RB];
-    // iteration it: round it % Q of column tile it / Q.  Chunks beyond the row's
-    // end read its first one: their codes are zero, and if the row holds a NaN
-    // or an infinity its results are not finite without it too.
-    auto load = [&](int it) __attribute__((always_inline)) {
-        const int kt = it / Q, p0 = (it - kt * Q) * P, at = kt * kTileCols + chunk * 8;
+    // Chunks beyond the row's end read its first one: their codes are zero, and
+    // if the row holds a NaN or an infinity its results are not finite without
+    // it too.
+    auto load = [&](int kt) __attribute__((always_inline)) {
+        const int at = kt * kTileCols + chunk * 8;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const uint32_t off = uint32_t((p0 + p) * C + (at < C ? at : 0)) / 8;
+        for (int p = 0; p < NP; ++p) {
+            const uint32_t off = uint32_t(p * C + (at < C ? at : 0)) / 8;
 #pragma unroll
             for (int j = 0; j < NT; ++j) xr[p][j] = cols[size_t(src[j]) + off];
         }
@@ -439,16 +424,16 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         for (int n = 0; n < NT; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int c = int(lane & 15), q = int(lane >> 4);
     // the workgroup's share of the contraction
-    const int it0 = UP ? 0 : KT * sp / a.tsplits * Q, iters = UP ? KT * Q : KT * (sp + 1) / a.tsplits * Q;
-    auto keep = [&](int it) __attribute__((always_inline)) {
+    const int first = UP ? 0 : KT * sp / a.tsplits, last = UP ? KT : KT * (sp + 1) / a.tsplits;
+    auto keep = [&](int kt) __attribute__((always_inline)) {
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xs[(it & 1) * SZ + p * TM * CH + put + j * 16 * CH] = xr[p][j];
+            for (int j = 0; j < NT; ++j) xs[(kt & 1) * SZ + p * TM * CH + put + j * 16 * CH] = xr[p][j];
     };
-    load(it0);
-    keep(it0);
-    for (int it = it0; it < iters; ++it) {
+    load(first);
+    keep(first);
+    for (int kt = first; kt < last; ++kt) {
         u32x4 w[RB];
         float sc[RB];
 #pragma unroll
@@ -457,12 +442,12 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
             sc[i] = scale_of(sn[i]);
         }
         __syncthreads();
-        if (it + 1 < iters) load(it + 1);
-        const u32x4* buf = xs + (it & 1) * SZ + c * CH;
-        bf16x8 b[2][P][NT];
+        if (kt + 1 < last) load(kt + 1);
+        const u32x4* buf = xs + (kt & 1) * SZ + c * CH;
+        bf16x8 b[2][NP][NT];
         auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     b[s & 1][p][n] = as_operand(buf[p * TM * CH + n * 16 * CH + ((q * 4 + s) ^ c)]);
@@ -476,14 +461,14 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 #pragma unroll
             for (int i = 0; i < RB; ++i) wv[i] = decode8(w[i][s], sc[i]);
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int i = 0; i < RB; ++i)
                         acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], b[s & 1][p][n], acc[i][n], 0, 0, 0);
         }
-        if (it + 1 < iters) keep(it + 1);
+        if (kt + 1 < last) keep(kt + 1);
     }
     // lane: token 16 n + c, rows 4 q .. 4 q + 3 of each block
 #pragma unroll
@@ -555,8 +540,8 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 
 template <bool UP, int NP, int NT, bool F32>
 __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) {
-    constexpr int TM = 16 * NT, P = kStagePieces<NP, NT>;
-    __shared__ u32x4 xs[2][P * TM * kTileCols / 8];
+    constexpr int TM = 16 * NT;
+    __shared__ u32x4 xs[2][NP * TM * kTileCols / 8];
     __shared__ int ent[TM];
     // consecutive work on one XCD (workgroup i runs on XCD i % 8): the row
     // blocks of a tile and the tiles of an expert share its L2
@@ -567,9 +552,9 @@ __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) 
     const int4 tl = a.tiles[tix];
     if constexpr (NT > 1) {
         // an expert's last tile, if at most half full, in half the instructions
-        if (tl.z <= TM / 2) return tile_product<UP, NP, P, NT / 2, F32>(a, tl, bk, sp, xs[0], ent);
+        if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, F32>(a, tl, bk, sp, xs[0], ent);
     }
-    tile_product<UP, NP, P, NT, F32>(a, tl, bk, sp, xs[0], ent);
+    tile_product<UP, NP, NT, F32>(a, tl, bk, sp, xs[0], ent);
 }
 
 // y[t] = the sum of its entries' terms (TF: fp32, else fp16 with their power of
@@ -1051,14 +1036,24 @@ struct MxLayout {
     size_t order, cnt, tiles, ntiles, act, part, tscale, xs, plan, nslots, split, total;
 };
 
-// Tokens per tile: by the tokens an expert gets on average.
-int tile_tokens(int T, int K, int E) {
+// Tokens per tile: 64 where an expert gets more than 32 on average, both x and
+// y are bf16 and that leaves 1536 workgroups of the up launch (two rounds of
+// three per CU); else 32 above 12 on average, else 16.  Measured in us with
+// tiles of 16, 32 and 64 (H 2048, I 768, 64 experts, top 4 unless said):
+//    128 tokens   41    42    44       512 tokens   56    57    61
+//    256          50    45    46      2048         135   113   125  (960 workgroups)
+//   4096, 128 experts, top 8, bf16:   393 with 32, 365 with 64; fp32: 862, 803, 890
+//    512, H 4096, I 14336, 8 experts, top 2, bf16:  557 with 32, 432 with 64
+int tile_tokens(int T, int K, int E, int ns, int I, bool bf16) {
     const int mean = T * K / E;
-    return mean > 32 ? 64 : mean > 16 ? 32 : 16;
+    const int64_t wg = (int64_t(T) * (K + ns) / 64 + (E + ns) / 2) * ((I + 127) / 128);
+    return mean > 32 && bf16 && wg >= 1536 ? 64 : mean > 12 ? 32 : 16;
 }
 
 // Parts of the down launch's contraction: enough for 768 workgroups (three per
-// CU) if half of the experts' last tiles are filled, of four column tiles at least.
+// CU) if half of the experts' last tiles are filled, of four column tiles at
+// least (32 tokens, H 1024, I 8192, 8 experts: 84 us unsplit, 48 split; 20
+// tokens, H 2048, I 1408, 16 experts: 37 and 34).
 int tile_splits(int tm, size_t n, int E, int ns, int H, int I) {
     const size_t wg = (n / tm + (E + ns) / 2 + 1) * size_t((H + 255) / 256);
     const int want = wg >= 768 ? 1 : int(768 / wg), most = col_tiles(I) / 4;
@@ -1079,7 +1074,7 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
         const size_t chunks = (size_t(y.units) + kRunWaves * kRunU - 1) / (kRunWaves * kRunU);
         y.split = take(chunks * ((row_blocks(H) + kRunR - 1) / kRunR * kRunR) * 256 * sizeof(float));
     } else {
-        y.tm = tile_tokens(T, K, E);
+        y.tm = tile_tokens(T, K, E, ns, I, dtype == STMOE_BF16 && ydtype == STMOE_BF16);
         // a full tile takes tm entries; each expert has at most one that is not full
         const size_t most = n / y.tm + E + ns;
         y.max_tiles = int(most < n ? most : n);
@@ -1105,7 +1100,7 @@ void launch_up_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
     if (NX > 1 || KT > 32) hipLaunchKernelGGL((mx_up_wide<NX, NH>), dim3(unsigned(items)), dim3(kThreads), 0, s, a, NB);
     else if (KT <= 4) hipLaunchKernelGGL((mx_up_decode<NH, 4, 1>), grid(1024), dim3(256), 0, s, a);
     else if (KT <= 8) hipLaunchKernelGGL((mx_up_decode<NH, 4, 2>), grid(1024), dim3(256), 0, s, a);
-    else if (KT <= 16) hipLaunchKernelGGL((mx_up_decode<NH, 4, 4>), grid(512), dim3(256), 0, s, a);
+    else if (KT <= 16) hipLaunchKernelGGL((mx_up_decode<NH, 4, 4>), grid(items <= 1024 ? 1024 : 512), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((mx_up_decode<NH, 8, 4>), grid(256), dim3(512), 0, s, a);
 }
 
@@ -1169,7 +1164,7 @@ template <bool XF, bool YF>
 int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream_t s, hipEvent_t ev_mid) {
     MxArgs a = args;
     const dim3 block(kPlanThreads);
-    if (a.T * a.K <= 1024) {
+    if (a.T * a.K <= kPlanEntries) {
         if (a.K <= 8) hipLaunchKernelGGL((mx_plan_kernel<8>), dim3(1), block, 0, s, a);
         else hipLaunchKernelGGL((mx_plan_kernel<16>), dim3(1), block, 0, s, a);
     } else {
@@ -1190,9 +1185,16 @@ int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream
         STMOE_LAUNCHED();
         a.x = xs;
     }
-    if (L.tm == 64) return launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
+    if constexpr (!XF && !YF) {
+        if (L.tm == 64) return launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
+    }
     if (L.tm == 32) return launch_tiles<XF, YF, 2>(a, L, s, ev_mid);
     return launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
+}
+
+// The launches index the activations in 16-byte chunks of 32 bits.
+bool too_large(int T, int K, int I, int ns, int ydtype) {
+    return size_t(T) * (K + ns) * (ydtype == STMOE_F32 ? 3 : 1) * I / 8 > size_t(1) << 32;
 }
 
 }  // namespace
@@ -1252,6 +1254,7 @@ extern "C" size_t moe_expert_ffn_mx_workspace_bytes(int T, int K, int E, int H, 
         I < 8 || I % 8 || I > kMaxI || n_shared < 0 || n_shared > kMaxShared)
         return 0;
     if ((dtype != STMOE_BF16 && dtype != STMOE_F32) || (ydtype != STMOE_BF16 && ydtype != STMOE_F32)) return 0;
+    if (too_large(T, K, I, n_shared, ydtype)) return 0;
     return mx_layout(T < 1 ? 1 : T, K, E, H, I, n_shared, dtype, ydtype).total;
 }
 
@@ -1269,6 +1272,7 @@ extern "C" int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const f
     STMOE_CHECK(dtype == STMOE_BF16 || dtype == STMOE_F32, "dtype must be STMOE_BF16 or STMOE_F32");
     STMOE_CHECK(ydtype == STMOE_BF16 || ydtype == STMOE_F32, "ydtype must be STMOE_BF16 or STMOE_F32");
     if (T == 0) return STMOE_OK;
+    STMOE_CHECK(!too_large(T, K, I, n_shared, ydtype), "the tokens' activations exceed 64 GiB");
     STMOE_CHECK(x && topk_idx && topk_w && expert_ptrs && y && ws, "null pointer");
     STMOE_CHECK(n_shared == 0 || shared_ptrs, "shared_ptrs is required when n_shared > 0");
     STMOE_CHECK(ws_bytes >= moe_expert_ffn_mx_workspace_bytes(T, K, E, H, I, n_shared, dtype, ydtype),
@@ -1276,6 +1280,9 @@ extern "C" int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const f
     STMOE_CHECK((reinterpret_cast<uintptr_t>(x) & 15) == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0 &&
                     (reinterpret_cast<uintptr_t>(ws) & 255) == 0,
                 "x and y must be 16-byte and ws 256-byte aligned");
+    STMOE_CHECK((reinterpret_cast<uintptr_t>(topk_idx) & 3) == 0 && (reinterpret_cast<uintptr_t>(topk_w) & 3) == 0 &&
+                    (reinterpret_cast<uintptr_t>(expert_ptrs) & 7) == 0 && (reinterpret_cast<uintptr_t>(shared_ptrs) & 7) == 0,
+                "topk_idx, topk_w and the pointer arrays must be aligned to their elements");
     return mx_ffn_launch(x, topk_idx, topk_w, T, K, H, I, E, dtype, ydtype, expert_ptrs, shared_ptrs, n_shared, y, ws,
                          as_stream(stream), nullptr, nullptr);
 }

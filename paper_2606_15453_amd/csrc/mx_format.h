@@ -11,9 +11,8 @@
 // their scales.  A matrix [R][C] is cut into tiles of 16 rows x 128 columns,
 // row block by row block; a tile's 1024 code bytes lie as the 16-byte pieces
 // of the lanes of a wave: lane l has row l % 16 and the block of 32 columns
-// l / 16, which is the row operand of four 16x16x32 matrix instructions
-// (and, two row blocks side by side, of 32x32x16 ones), so a wave reads one
-// contiguous KiB per tile.  Scales lie in groups of four tiles: lane l's four
+// l / 16, which is the row operand of four 16x16x32 matrix instructions, so a
+// wave reads one contiguous KiB per tile.  Scales lie in groups of four tiles: lane l's four
 // bytes at 4 l of 256.  Rows and columns beyond the matrix hold zero codes.
 #pragma once
 
@@ -58,9 +57,7 @@ inline __host__ __device__ Blob blob(int H, int I) {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // The conversions take the scale as a float and use its exponent field alone:
 // byte s sits there as s << 23 (0 is 2^-127, 255 NaN).

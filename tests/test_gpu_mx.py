@@ -207,6 +207,105 @@ def test_ffn_large_experts(H, I, T):
     assert _err(y, want) <= _tol(True, False)
 
 
+@pytest.mark.parametrize("y_bf16", [False, True])
+@pytest.mark.parametrize("T,K,E,off", [
+    (5, 8, 20, 0), (6, 8, 20, 1), (16, 16, 256, 0), (16, 9, 256, 3), (17, 16, 20, 0), (20, 9, 12, 0), (64, 16, 16, 1),
+    (65, 16, 20, 0), (100, 8, 16, 1), (120, 9, 11, 0), (130, 16, 20, 0), (130, 16, 20, 1), (300, 8, 16, 2), (1024, 1, 256, 0),
+    (1025, 1, 2, 0), (1100, 12, 64, 0)])
+def test_ffn_selections_of_every_width(T, K, E, off, y_bf16):
+    """1 to 16 experts per token, in selections at any alignment, around the borders between the ways they are
+    sorted; every 7th token repeats its first expert at its end and every 11th selects none."""
+    import torch
+    H, I = 64, 72
+    yd = torch.bfloat16 if y_bf16 else torch.float32
+    ex = Experts(E, H, I, T)
+    x, sel, w = _inputs(T, K, E, H, K, torch.bfloat16)
+    sel[::7, K - 1] = sel[::7, 0]
+    sel[::11] = -1
+    idx = torch.full((T * K + off,), 2 ** 30, dtype=torch.int32, device=DEV)[off:].view(T, K)
+    idx.copy_(sel)
+    y = _run(ex, E, H, I, x, idx, w, yd)
+    want = mxref.moe_ffn(_f64(x), sel.cpu().numpy(), _f64(w), ex.values)
+    assert _err(y, want) <= _tol(True, y_bf16)
+
+
+@pytest.mark.parametrize("T", [16, 40, 300])
+def test_ffn_bf16_results_of_any_size(T):
+    """Tokens whose results lie near both ends of bf16's range, whose experts' terms lie 2^40 apart, or that overflow;
+    and a row of W_down 2^12 times its neighbours.  Beyond 16 tokens a term below 2^-14 of the largest of its 64 is off
+    by 2^-25 of that: 2^-13 of the neighbours' size for each of two terms, and 2^-7 as everywhere."""
+    import torch
+    from paper_2606_15453_amd import stmoe as S
+    H, I, E, K = 264, 136, 4, 2
+    ex = Experts(E, H, I, 21)
+    x, idx, w = _inputs(T, K, E, H, 6, torch.float32)
+    x[0] *= 2.0 ** 60
+    x[1] *= 2.0 ** -56
+    w[2, 0], w[2, 1] = 1.0, 2.0 ** -40
+    x[3] *= 2.0 ** 70
+    x = x.to(torch.bfloat16)
+    y = _run(ex, E, H, I, x, idx, w, torch.bfloat16)
+    want = mxref.moe_ffn(_f64(x), idx.cpu().numpy(), _f64(w), ex.values)
+    rest = [t for t in range(T) if t != 3]
+    assert _err(y[rest], want[rest]) <= _tol(True, True)
+    assert not bool(y[3].isfinite().all())
+    # one row of every expert's W_down, as its scale bytes: row 5, lanes 5, 21, 37 and 53 of the first row block
+    h = S.blob_bytes(H, I, S.MXFP4) - 17 * 256
+    for e in range(E):
+        for lane in (5, 21, 37, 53):
+            s = ex.blobs[e][h + 4 * lane:h + 4 * lane + 4]
+            s.copy_(torch.where(s > 0, s + 12, s))
+        ex.values[e][2][5] *= 4096.0
+    keep = [t for t in range(4, T)]
+    y = _run(ex, E, H, I, x, idx, w, torch.bfloat16)
+    want = mxref.moe_ffn(_f64(x), idx.cpu().numpy(), _f64(w), ex.values)
+    others = [r for r in range(H) if r != 5]
+    assert _err(y[keep][:, others], want[keep][:, others]) <= _tol(True, True) + 2 * 2.0 ** -13
+    # row 5 itself, a single sum that may cancel: against the sum of its products' magnitudes, of which rounding the
+    # activations loses 2^-8, rounding y 2^-8 and rounding the terms 2^-11 (and fp32 the 2e-5 of the other results)
+    size = np.zeros(T)
+    for t in keep:
+        xt = _f64(x[t])
+        for e, wk in zip(idx[t].tolist(), _f64(w[t])):
+            g, u, d = ex.values[e]
+            gx = g @ xt
+            size[t] += wk * (np.abs(d[5]) @ np.abs(gx / (1 + np.exp(-gx)) * (u @ xt)))
+    off = np.abs(_f64(y)[keep, 5] - want[keep, 5])
+    assert (off <= (2.0 ** -7 + 2.0 ** -11 + 2e-5) * size[keep]).all()
+
+
+@pytest.mark.parametrize("T", [1, 16, 90])
+def test_ffn_two_calls_at_once(T):
+    """Two streams, a workspace each, both ways of sorting and both result types: the bits of each call alone."""
+    import torch
+    H, I, E, K = 520, 264, 12, 3
+    ex = Experts(E, H, I, 8)
+    calls = []
+    for i, yd in enumerate((torch.float32, torch.bfloat16)):
+        x, idx, w = _inputs(T, K, E, H, i, torch.bfloat16)
+        calls.append((x, idx, w, yd, torch.empty((T, H), dtype=yd, device=DEV), _ws(T, K, E, H, I, 0, x.dtype, yd),
+                      torch.cuda.Stream(), _run(ex, E, H, I, x, idx, w, yd)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, idx, w, yd, y, ws, s, _alone in calls:
+            _run(ex, E, H, I, x, idx, w, yd, y=y, ws=ws, stream=s)
+    torch.cuda.synchronize()
+    for *_rest, y, _ws_, _s, alone in calls:
+        assert torch.equal(y, alone)
+
+
+@pytest.mark.parametrize("T", [1, 16, 40, 200])
+def test_ffn_in_place(T):
+    """y may be x."""
+    import torch
+    H, I, E, K = 264, 136, 6, 2
+    ex = Experts(E, H, I, 3)
+    x, idx, w = _inputs(T, K, E, H, 1, torch.bfloat16)
+    y = _run(ex, E, H, I, x, idx, w, torch.bfloat16)
+    _run(ex, E, H, I, x, idx, w, torch.bfloat16, y=x)
+    assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("T", [1, 4, 16, 40, 200])
 @pytest.mark.parametrize("y_bf16", [False, True])
 def test_ffn_odd_selections(T, y_bf16):

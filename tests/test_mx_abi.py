@@ -62,6 +62,16 @@ def test_ffn_refusals():
     for a in [(-1, 2, 8, 64, 64, 0, 1, 0), (65537, 2, 8, 64, 64, 0, 1, 0), (4, 9, 8, 64, 64, 0, 1, 0),
               (4, 2, 8, 60, 64, 0, 1, 0), (4, 2, 8, 64, 64, 9, 1, 0), (4, 2, 8, 64, 64, 0, 2, 0), (4, 2, 8, 64, 64, 0, 1, 2)]:
         assert n(*a) == 0
+    # activations beyond 64 GiB (the launches count their 16-byte chunks in 32 bits)
+    assert n(65536, 16, 16, 64, 32768, 0, S.BF16, S.BF16) > 0
+    big = (65536, 16, 16, 64, 32776, 0, S.BF16, S.BF16)
+    assert n(*big) == 0 and n(*big[:4], 10928, 0, S.BF16, S.F32) == 0 and n(*big[:4], 10920, 0, S.BF16, S.F32) > 0
+    assert f(256, 256, 256, 65536, 16, 64, 32776, 16, S.BF16, S.BF16, 256, None, 0, 256, 256, 1 << 62, None) == S.EINVAL
+    # pointers that their elements do not allow
+    for bad in [dict(idx=258), dict(w=258), dict(ep=260), dict(ns=1, sp=260)]:
+        a = dict(ok, **bad)
+        assert f(a["x"], a["idx"], a["w"], a["T"], a["K"], a["H"], a["I"], a["E"], a["dt"], a["yt"], a["ep"], a["sp"],
+                 a["ns"], a["y"], a["ws"], a["n"], None) == S.EINVAL, bad
     # the other FFN entries keep to row-major blobs
     assert L.moe_expert_ffn(256, 256, 256, 1, 2, 64, 64, 8, S.MXFP4, 256, None, 0, 256, 256, 1 << 30, None) == S.EINVAL
 
