@@ -84,15 +84,6 @@ struct Raw {
     u32x4 q[F32 ? 2 : 1];
 };
 
-template <bool F32>
-__device__ __forceinline__ Raw<F32> load_raw(const void* x, size_t at, bool in) {
-    Raw<F32> r;
-    const u32x4* s = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(x) + at * (F32 ? 4 : 2));
-#pragma unroll
-    for (int i = 0; i < (F32 ? 2 : 1); ++i) r.q[i] = in ? s[i] : u32x4{0u, 0u, 0u, 0u};
-    return r;
-}
-
 __device__ __forceinline__ bf16x8 as_operand(u32x4 q) {
     union {
         u32x4 q;
@@ -625,17 +616,79 @@ struct DecodeSlot {
 };
 constexpr int kNone = 255;
 
-__device__ __forceinline__ uint32_t load_scale(BlobRef r, uint32_t at, int tile, uint32_t lane) {
-    return __builtin_amdgcn_raw_buffer_load_b8(
-        r, int(lane * 4u), int(at + uint32_t(tile / kGroupTiles) * kGroupBytes + uint32_t(tile % kGroupTiles)), 0);
+// Rows of values as a buffer (below 2 GiB): what is not wanted is asked for
+// beyond its end, which gives zeros.  Loads behind a branch inside a loop would
+// make the compiler wait for every load in flight where their values meet.
+__device__ __forceinline__ BlobRef rows_ref(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(bytes), 0x00027000);
 }
+
+template <bool F32>
+__device__ __forceinline__ Raw<F32> load_row(BlobRef rows, uint32_t at, bool in) {
+    Raw<F32> r;
+    const uint32_t off = in ? at * (F32 ? 4u : 2u) : 0x80000000u;
+#pragma unroll
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) r.q[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, int(off + 16u * i), 0, 0);
+    return r;
+}
+
+// Nothing that uses the values is moved before this.
+template <class A, class B>
+__device__ __forceinline__ void hold(A& a, B& b) { asm volatile("" : "+v"(a), "+v"(b)); }
+
+// Work items lo, lo + step .. below hi (at least one), the next one's loads
+// (into the other of two stages) under way while one is used.  ready(i) comes
+// before the next loads, so that what it loads is waited for without them.
+// Three things would make every use wait for the loads that are to overlap it:
+// loads behind a branch of the loop, loads that the compiler puts off to save
+// registers, and uses that it draws forward before them (pin).
+template <class S, class Load, class Ready, class Use>
+__device__ __forceinline__ void pipeline(S (&st)[2], int lo, int hi, int step, Load load, Ready ready, Use use) {
+    const auto both = [&](S& now, S& next, int i, int s) __attribute__((always_inline)) {
+        load(next, i + step);
+        __builtin_amdgcn_sched_barrier(0);
+        now.pin();
+        use(now, i, s);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    load(st[0], lo);
+    int i = lo;
+    for (; i + 2 * step < hi; i += 2 * step) {
+        ready(i);
+        both(st[0], st[1], i, 0);
+        ready(i + step);
+        both(st[1], st[0], i + step, 1);
+    }
+    ready(i);
+    if (i + step < hi) {
+        both(st[0], st[1], i, 0);
+        ready(i + step);
+        use(st[1], i + step, 1);
+    } else {
+        use(st[0], i, 0);
+    }
+}
+
+// Where workgroup wg of n's equal share of the items begins (items n < 2^32: at
+// most 4.4 million items of 512 workgroups).  In a scalar register, with what
+// depends on it: a buffer load whose offset is not becomes a loop over lanes.
+__device__ __forceinline__ int share(uint32_t items, uint32_t wg, uint32_t n) {
+    return __builtin_amdgcn_readfirstlane(int(items * wg / n));
+}
+
+// The scales of the group of column tiles that holds this one, and this one's.
+// (As a byte it would be extended where two stages' values meet, and waited
+// for there.)
+__device__ __forceinline__ uint32_t load_scales(BlobRef r, uint32_t at, int tile, uint32_t lane) {
+    return __builtin_amdgcn_raw_buffer_load_b32(r, int(lane * 4u), int(at + uint32_t(tile / kGroupTiles) * kGroupBytes), 0);
+}
+__device__ __forceinline__ float scale_in(uint32_t group, int tile) { return scale_of(group >> 8 * (tile % kGroupTiles) & 0xffu); }
 
 // The slots of a decode step in LDS: routed experts ascending, then the shared.
 struct SlotTable {
     const void* blob[kMaxGroups];
     alignas(16) uint8_t k[kMaxGroups][kMaxB];
     uint32_t present[kMaxE / 32];
-    uint16_t rank[kMaxE];
     int entry[kMaxB * kMaxK];
 
     __device__ __forceinline__ BlobRef ref(int s, const Blob& L) const {
@@ -646,7 +699,8 @@ struct SlotTable {
     }
 };
 
-// Builds the table from the selection (at least 256 threads); returns the number of slots.
+// Builds the table from the selection (at least 256 threads, one per entry);
+// returns the number of slots.
 template <int N>
 __device__ __forceinline__ int make_slots(const MxArgs& a, SlotTable& tab) {
     const int tid = threadIdx.x;
@@ -658,29 +712,30 @@ __device__ __forceinline__ int make_slots(const MxArgs& a, SlotTable& tab) {
     if (tid < kMaxB * kMaxK) tab.entry[tid] = mine;
     lds_barrier();
     if (mine >= 0) atomicOr(&tab.present[mine >> 5], 1u << (mine & 31));
+    // the first of a token's entries that names the expert
+    const int t = tid / a.K, k = tid - t * a.K;
+    bool first = mine >= 0;
+#pragma unroll
+    for (int j = 0; j < kMaxK; ++j) {
+        const int e = tab.entry[min(t * a.K + j, kMaxB * kMaxK - 1)];
+        first &= !((j < k) & (e == mine));
+    }
     lds_barrier();
     int total = 0, at = 0;
 #pragma unroll
     for (int i = 0; i < kMaxE / 32; ++i) {
         const uint32_t m = tab.present[i];
-        if (mine >= 0) at += i < mine >> 5 ? __builtin_popcount(m) : i == mine >> 5 ? __builtin_popcount(m & ((1u << (mine & 31)) - 1u)) : 0;
+        const int below = max(0, min(32, mine - 32 * i));       // experts of this word before this one
+        at += __builtin_popcount(m & uint32_t((1ull << below) - 1ull));
         total += __builtin_popcount(m);
     }
     total = __builtin_amdgcn_readfirstlane(total);
-    if (mine >= 0) {
+    if (first) {
         tab.blob[at] = blob;
-        tab.rank[mine] = uint16_t(at);
+        tab.k[at][t] = uint8_t(k);
     }
+    for (int i = tid; i < a.ns * a.T; i += N) tab.k[total + i / a.T][i % a.T] = uint8_t(a.K + i / a.T);
     if (tid < a.ns) tab.blob[total + tid] = a.sptr[tid];
-    lds_barrier();
-    if (tid < a.T) {
-        // the first of a token's entries that names the expert
-        for (int j = a.K - 1; j >= 0; --j) {
-            const int e = tab.entry[tid * a.K + j];
-            if (e >= 0) tab.k[tab.rank[e]][tid] = uint8_t(j);
-        }
-        for (int s = 0; s < a.ns; ++s) tab.k[total + s][tid] = uint8_t(a.K + s);
-    }
     lds_barrier();
     return total + a.ns;
 }
@@ -710,31 +765,36 @@ __global__ __launch_bounds__(64 * NW) void mx_up_decode(MxArgs a) {
     const uint32_t lane = threadIdx.x & 63;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid < a.T * a.K) gate_w[tid] = a.w[tid];
-    const int S = make_slots<N>(a, tab);
-    if (blockIdx.x == 0) publish_slots<N>(a, tab, S);
-    const Blob L = blob(a.H, a.I);
     const int KT = col_tiles(a.H), KG = col_groups(a.H), NB = row_blocks(a.I);
-    const int64_t items = int64_t(S) * NB;
-    const int lo = int(items * blockIdx.x / gridDim.x), hi = int(items * (blockIdx.x + 1) / gridDim.x);
-    if (lo >= hi) return;
     const int c = int(lane & 15), q = int(lane >> 4);
     const int kt0 = wave * TPW;
+    const BlobRef rows = rows_ref(a.x, uint32_t(a.T * a.H) * 2u);
     Raw<false> x[TPW][4];
 #pragma unroll
     for (int j = 0; j < TPW; ++j)
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const int col = (kt0 + j) * kTileCols + q * kBlock + s * 8;
-            x[j][s] = load_raw<false>(a.x, size_t(c) * a.H + col, c < a.T && col < a.H);
+            x[j][s] = load_row<false>(rows, uint32_t(c * a.H + col), c < a.T && col < a.H);
         }
+    const int S = make_slots<N>(a, tab);
+    if (blockIdx.x == 0) publish_slots<N>(a, tab, S);
+    const Blob L = blob(a.H, a.I);
+    const int lo = share(S * NB, blockIdx.x, gridDim.x), hi = share(S * NB, blockIdx.x + 1, gridDim.x);
+    if (lo >= hi) return;
     struct Stage {
         u32x4 w[2][TPW];
         uint32_t s[2];
+        __device__ __forceinline__ void pin() {
+#pragma unroll
+            for (int j = 0; j < TPW; ++j) hold(w[0][j], w[1][j]);
+            hold(s[0], s[1]);
+        }
     } st[2];
-    // a tile beyond the last one is the last one again: its columns are zero
+    // A tile beyond the last one is the last one again, with columns of zeros.
+    // TPW tiles never lie in two groups of scales.
     auto load = [&](Stage& d, int item) __attribute__((always_inline)) {
-        if (kt0 >= KT) return;
-        const int slot = item / NB, rb = item - slot * NB;
+        const int slot = __builtin_amdgcn_readfirstlane(item / NB), rb = item - slot * NB;
         const BlobRef ref = tab.ref(slot, L);
         const uint32_t wc = uint32_t(rb * KT) * kTileBytes;
         const uint32_t sc = uint32_t(rb * KG + kt0 / kGroupTiles) * kGroupBytes;
@@ -746,23 +806,19 @@ __global__ __launch_bounds__(64 * NW) void mx_up_decode(MxArgs a) {
             d.s[m] = __builtin_amdgcn_raw_buffer_load_b32(ref, int(lane * 4u), int(uint32_t(m ? L.up_s : L.gate_s) + sc), 0);
         }
     };
-    // TPW tiles never lie in two groups of scales
-    const int sh = 8 * (kt0 % kGroupTiles);
-    auto use = [&](const Stage& d, int item, int buf) __attribute__((always_inline)) {
-        f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-        if (kt0 < KT) {
+    auto multiply = [&](const Stage& d, f32x4 (&acc)[2]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < TPW; ++j)
+        for (int j = 0; j < TPW; ++j)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
+            for (int s = 0; s < 4; ++s) {
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        const uint32_t b = kt0 + j < KT ? d.s[m] >> (sh + 8 * j) & 0xffu : 0u;
-                        const bf16x8 wv = decode8(d.w[m][j][s], scale_of(b));
-                        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, as_operand(x[j][s].q[0]), acc[m], 0, 0, 0);
-                    }
+                for (int m = 0; m < 2; ++m) {
+                    const bf16x8 wv = decode8(d.w[m][j][s], scale_in(d.s[m], kt0 + j));
+                    acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, as_operand(x[j][s].q[0]), acc[m], 0, 0, 0);
                 }
-        }
+            }
+    };
+    auto finish = [&](const f32x4 (&acc)[2], int item, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -785,14 +841,19 @@ __global__ __launch_bounds__(64 * NW) void mx_up_decode(MxArgs a) {
 #pragma unroll
         for (int p = 0; p < NH; ++p) o[size_t(p) * a.I] = b[p];
     };
-    load(st[0], lo);
-    for (int item = lo; item < hi; item += 2) {
-        if (item + 1 < hi) load(st[1], item + 1);
-        use(st[0], item, 0);
-        if (item + 1 >= hi) break;
-        if (item + 2 < hi) load(st[0], item + 2);
-        use(st[1], item + 1, 1);
+    // waves without columns add zeros
+    if (kt0 >= KT) {
+        const f32x4 none[2] = {};
+        for (int item = lo; item < hi; ++item) finish(none, item, (item - lo) & 1);
+        return;
     }
+    pipeline(
+        st, lo, hi, 1, load, [](int) {},
+        [&](const Stage& d, int item, int buf) __attribute__((always_inline)) {
+            f32x4 acc[2] = {};
+            multiply(d, acc);
+            finish(acc, item, buf);
+        });
 }
 
 // fp32 hidden states, or more than 32 column tiles: a row block of one expert
@@ -813,47 +874,49 @@ __global__ __launch_bounds__(kThreads) void mx_up_wide(MxArgs a, int nrb) {
     const int KT = col_tiles(a.H), KG = col_groups(a.H);
     const int c = int(lane & 15), q = int(lane >> 4), k = tab.k[slot][c];
     const bool live = k != kNone;
-    const size_t xrow = live ? size_t(c) * a.H : 0;
+    const BlobRef rows = rows_ref(a.x, uint32_t(a.T * a.H) * (NX > 1 ? 4u : 2u));
     const uint32_t wc = uint32_t(rb * KT) * kTileBytes, sc = uint32_t(rb * KG) * kGroupBytes;
     struct Stage {
         u32x4 w[2];
         uint32_t s[2];
         Raw<(NX > 1)> x[4];
+        __device__ __forceinline__ void pin() {
+            hold(w[0], w[1]);
+            hold(s[0], s[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                hold(x[2 * i].q[0], x[2 * i + 1].q[0]);
+                if constexpr (NX > 1) hold(x[2 * i].q[1], x[2 * i + 1].q[1]);
+            }
+        }
     } st[2];
     auto load = [&](Stage& d, int kt) __attribute__((always_inline)) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             d.w[m] = load_codes<true>(ref, uint32_t(m ? L.up : L.gate) + wc + uint32_t(kt) * kTileBytes, lane);
-            d.s[m] = load_scale(ref, uint32_t(m ? L.up_s : L.gate_s) + sc, kt, lane);
+            d.s[m] = load_scales(ref, uint32_t(m ? L.up_s : L.gate_s) + sc, kt, lane);
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const int col = kt * kTileCols + q * kBlock + s * 8;
-            d.x[s] = load_raw<(NX > 1)>(a.x, xrow + col, live && col < a.H);
+            d.x[s] = load_row<(NX > 1)>(rows, uint32_t(c * a.H + col), live && col < a.H);
         }
     };
     f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-    auto use = [&](const Stage& d) __attribute__((always_inline)) {
+    auto use = [&](const Stage& d, int kt, int) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const Pieces<NX> xv = pieces<NX>(d.x[s]);
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                const bf16x8 wv = decode8(d.w[m][s], scale_of(d.s[m]));
+                const bf16x8 wv = decode8(d.w[m][s], scale_in(d.s[m], kt));
 #pragma unroll
                 for (int p = 0; p < NX; ++p)
                     acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv.p[p], acc[m], 0, 0, 0);
             }
         }
     };
-    if (wave < KT) load(st[0], wave);
-    for (int kt = wave; kt < KT; kt += 2 * kWaves) {
-        if (kt + kWaves < KT) load(st[1], kt + kWaves);
-        use(st[0]);
-        if (kt + kWaves >= KT) break;
-        if (kt + 2 * kWaves < KT) load(st[0], kt + 2 * kWaves);
-        use(st[1]);
-    }
+    if (wave < KT) pipeline(st, wave, KT, kWaves, load, [](int) {}, use);
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -900,30 +963,40 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
     const Blob L = blob(a.H, a.I);
     const int KT = col_tiles(a.I), KG = col_groups(a.I), NB = row_blocks(a.H), groups = (NB + R - 1) / R;
     const int units = S * KT, chunks = max(1, (units + NW * U - 1) / (NW * U));
-    const int64_t work = int64_t(chunks) * groups;
-    const int lo = int(work * blockIdx.x / gridDim.x), hi = int(work * (blockIdx.x + 1) / gridDim.x);
+    const int lo = share(chunks * groups, blockIdx.x, gridDim.x), hi = share(chunks * groups, blockIdx.x + 1, gridDim.x);
+    if (lo >= hi) return;
     const int c = int(lane & 15), q = int(lane >> 4);
     const int t = PC ? c / NH : c, pc = PC ? c % NH : 0;
     struct Stage {
         u32x4 w[U][R];
         uint32_t s[U][R];
+        int kt[U];
+        __device__ __forceinline__ void pin() {
+#pragma unroll
+            for (int i = 0; i < U * R; ++i) hold(w[i / R][i % R], s[i / R][i % R]);
+        }
     } st[2];
     auto load = [&](Stage& d, int item) __attribute__((always_inline)) {
-        const int chunk = item / groups, grp = item - chunk * groups;
+        const int chunk = __builtin_amdgcn_readfirstlane(item / groups), grp = item - chunk * groups;
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            const int u = (chunk * NW + wave) * U + j;
-            if (u >= units) continue;
-            const int slot = u / KT, kt = u - slot * KT;
+            // beyond the last tile: no loads where there is one item mostly,
+            // else the last one again, which no token adds
+            int u = (chunk * NW + wave) * U + j;
+            if (U > 1 && u >= units) continue;
+            u = min(u, units - 1);
+            const int slot = __builtin_amdgcn_readfirstlane(u / KT), kt = u - slot * KT;
             const BlobRef ref = tab.ref(slot, L);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const uint32_t b = uint32_t(min(grp * R + i, NB - 1));
                 d.w[j][i] = load_codes<true>(ref, uint32_t(L.down) + (b * uint32_t(KT) + uint32_t(kt)) * kTileBytes, lane);
-                d.s[j][i] = load_scale(ref, uint32_t(L.down_s) + b * uint32_t(KG) * kGroupBytes, kt, lane);
+                d.s[j][i] = load_scales(ref, uint32_t(L.down_s) + b * uint32_t(KG) * kGroupBytes, kt, lane);
             }
+            d.kt[j] = kt;
         }
     };
+    const BlobRef rows = rows_ref(a.act, uint32_t(a.T * a.ks * NH) * uint32_t(a.I) * 2u);
     Raw<false> h[U][4][MP];
     bool live[U];
     auto columns = [&](int chunk) __attribute__((always_inline)) {
@@ -932,17 +1005,17 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
             const int u = (chunk * NW + wave) * U + j, slot = u / KT, kt = u - slot * KT;
             const int k = u < units ? tab.k[slot][t] : kNone;
             live[j] = k != kNone;
-            const size_t row = live[j] ? (size_t(t * a.ks + k) * NH + pc) * a.I : 0;
+            const uint32_t row = uint32_t((t * a.ks + k) * NH + pc) * uint32_t(a.I);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const int col = kt * kTileCols + q * kBlock + x * 8;
 #pragma unroll
                 for (int y = 0; y < MP; ++y)
-                    h[j][x][y] = load_raw<false>(a.act, row + size_t(y) * a.I + col, live[j] && col < a.I);
+                    h[j][x][y] = load_row<false>(rows, row + uint32_t(y * a.I + col), live[j] && col < a.I);
             }
         }
     };
-    auto use = [&](const Stage& d, int item, int buf) __attribute__((always_inline)) {
+    auto multiply = [&](const Stage& d, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -951,7 +1024,7 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const bf16x8 wv = decode8(d.w[j][i][x], scale_of(d.s[j][i]));
+                    const bf16x8 wv = decode8(d.w[j][i][x], scale_in(d.s[j][i], d.kt[j]));
 #pragma unroll
                     for (int y = 0; y < MP; ++y)
                         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, as_operand(h[j][x][y].q[0]), acc, 0, 0, 0);
@@ -963,6 +1036,8 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
 #pragma unroll
             for (int r = 0; r < 4; ++r) red[buf][wave][(i * 4 + r) * 64 + lane] = sum[r];
         }
+    };
+    auto finish = [&](int item, int buf) __attribute__((always_inline)) {
         lds_barrier();
 #pragma unroll
         for (int o = tid; o < OUT; o += N) {
@@ -984,16 +1059,33 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
             else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
         }
     };
-    int chunk = -1;
-    if (lo < hi) load(st[0], lo);
-    for (int item = lo; item < hi; item += 2) {
-        if (item / groups != chunk) columns(chunk = item / groups);
-        if (item + 1 < hi) load(st[1], item + 1);
-        use(st[0], item, 0);
-        if (item + 1 >= hi) break;
-        if ((item + 1) / groups != chunk) columns(chunk = (item + 1) / groups);
-        if (item + 2 < hi) load(st[0], item + 2);
-        use(st[1], item + 1, 1);
+    if (units == 0) {
+        // nothing selected: the sums are zero
+#pragma unroll
+        for (int o = tid; o < NW * OUT; o += N) red[0][o / OUT][o % OUT] = 0.f;
+        for (int item = lo; item < hi; ++item) finish(item, 0);
+        return;
+    }
+    const auto use = [&](const Stage& d, int item, int buf) __attribute__((always_inline)) {
+        multiply(d, buf);
+        finish(item, buf);
+    };
+    if constexpr (U > 1) {
+        // one chunk, and one item up to H 4096
+        columns(0);
+        for (int item = lo; item < hi; ++item) {
+            load(st[0], item);
+            use(st[0], item, (item - lo) & 1);
+        }
+    } else {
+        int held = -1;                                      // the chunk whose columns are held
+        pipeline(
+            st, lo, hi, 1, load,
+            [&](int item) __attribute__((always_inline)) {
+                const int chunk = item / groups;
+                if (chunk != held) columns(held = chunk);
+            },
+            use);
     }
 }
 
