@@ -117,21 +117,23 @@ __device__ __forceinline__ int col_blocks(int H) { return (H + 63) / 64; }
 // by less than 2e-6 of itself down to g = -20 and negligible below).
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 
-// The expert of an entry, or -1 where it names none or repeats an earlier
-// entry of its token (the first one counts).
-__device__ __forceinline__ int entry_expert(const MxArgs& a, int t, int k) {
-    if (k >= a.K) return a.E + (k - a.K);
-    const int32_t* row = a.idx + size_t(t) * a.K;
-    const int e = row[k];
-    if (e < 0 || e >= a.E) return -1;
-    for (int j = 0; j < k; ++j)
-        if (row[j] == e) return -1;
-    return e;
+// Which of token t's entries count, as bits (one token per wave): those that name
+// an expert and are the first of the token to name it, and the shared experts'.
+__device__ __forceinline__ uint32_t valid_entries(const MxArgs& a, int t) {
+    const int lane = threadIdx.x & 63;
+    const int e = lane < a.K ? a.idx[size_t(t) * a.K + lane] : -1;
+    bool first = e >= 0 && e < a.E;
+    for (int j = 0; j < a.K; ++j) first &= !((j < lane) & (__builtin_amdgcn_readlane(e, j) == e));
+    return uint32_t(__ballot(first)) | ((1u << a.ns) - 1u) << a.K;
 }
 
 // A barrier for what passes through LDS alone: __syncthreads would also wait
 // for the stores to memory under way (3 us for 1024 scattered ones).
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Nothing that uses the values is moved before this.
+template <class A, class B>
+__device__ __forceinline__ void hold(A& a, B& b) { asm volatile("" : "+v"(a), "+v"(b)); }
 
 // The tiles of at most tm tokens, experts in order (one workgroup; cnt in LDS).
 __device__ __forceinline__ void list_tiles(const MxArgs& a, const int* cnt, int* tile) {
@@ -339,6 +341,14 @@ __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lan
 }
 
 
+// The scales of the group of column tiles that holds this one, and this one's.
+// (As a byte it would be extended where two stages' values meet, and waited
+// for there.)
+__device__ __forceinline__ uint32_t load_scales(BlobRef r, uint32_t at, int tile, uint32_t lane) {
+    return __builtin_amdgcn_raw_buffer_load_b32(r, int(lane * 4u), int(at + uint32_t(tile / kGroupTiles) * kGroupBytes), 0);
+}
+__device__ __forceinline__ float scale_in(uint32_t group, int tile) { return scale_of(group >> 8 * (tile % kGroupTiles) & 0xffu); }
+
 // ---------------------------------------------------------------- prompts
 //
 // A workgroup multiplies 256 weight rows (128 of gate and the same of up, or
@@ -388,24 +398,25 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         src[j] = uint32_t(UP ? e / a.ks : e) * uint32_t(NP * C / 8);
     }
     const int put = tid / CH * CH + (chunk ^ (tid / CH & 15));
-    u32x4 xr[NP][NT], wn[RB];
-    uint32_t sn[RB];
+    struct Stage {
+        u32x4 x[NP][NT], w[RB];
+        uint32_t s[RB];
+    } st[2];
     // Chunks beyond the row's end read its first one: their codes are zero, and
     // if the row holds a NaN or an infinity its results are not finite without
     // it too.
-    auto load = [&](int kt) __attribute__((always_inline)) {
+    auto load = [&](Stage& d, int kt) __attribute__((always_inline)) {
         const int at = kt * kTileCols + chunk * 8;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const uint32_t off = uint32_t(p * C + (at < C ? at : 0)) / 8;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xr[p][j] = cols[size_t(src[j]) + off];
+            for (int j = 0; j < NT; ++j) d.x[p][j] = cols[size_t(src[j]) + off];
         }
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-            wn[i] = load_codes<false>(ref, wc[i] + uint32_t(kt) * kTileBytes, lane);
-            sn[i] = __builtin_amdgcn_raw_buffer_load_b8(
-                ref, int(lane * 4u), int(wsc[i] + uint32_t(kt / kGroupTiles) * kGroupBytes + uint32_t(kt % kGroupTiles)), 0);
+            d.w[i] = load_codes<false>(ref, wc[i] + uint32_t(kt) * kTileBytes, lane);
+            d.s[i] = load_scales(ref, wsc[i], kt, lane);
         }
     };
     f32x4 acc[RB][NT];
@@ -414,27 +425,17 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int c = int(lane & 15), q = int(lane >> 4);
-    // the workgroup's share of the contraction
-    const int first = UP ? 0 : KT * sp / a.tsplits, last = UP ? KT : KT * (sp + 1) / a.tsplits;
-    auto keep = [&](int kt) __attribute__((always_inline)) {
+    auto keep = [&](const Stage& d, int kt) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xs[(kt & 1) * SZ + p * TM * CH + put + j * 16 * CH] = xr[p][j];
+            for (int j = 0; j < NT; ++j) xs[(kt & 1) * SZ + p * TM * CH + put + j * 16 * CH] = d.x[p][j];
     };
-    load(first);
-    keep(first);
-    for (int kt = first; kt < last; ++kt) {
-        u32x4 w[RB];
+    auto multiply = [&](const u32x4 (&w)[RB], const uint32_t (&scales)[RB], int kt) __attribute__((always_inline)) {
+        const u32x4* buf = xs + (kt & 1) * SZ + c * CH;
         float sc[RB];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) {
-            w[i] = wn[i];
-            sc[i] = scale_of(sn[i]);
-        }
-        __syncthreads();
-        if (kt + 1 < last) load(kt + 1);
-        const u32x4* buf = xs + (kt & 1) * SZ + c * CH;
+        for (int i = 0; i < RB; ++i) sc[i] = scale_in(scales[i], kt);
         bf16x8 b[2][NP][NT];
         auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
@@ -459,7 +460,56 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
                     for (int i = 0; i < RB; ++i)
                         acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], b[s & 1][p][n], acc[i][n], 0, 0, 0);
         }
-        if (kt + 1 < last) keep(kt + 1);
+    };
+    // the workgroup's share of the contraction
+    const int first = UP ? 0 : KT * sp / a.tsplits, last = UP ? KT : KT * (sp + 1) / a.tsplits;
+    load(st[0], first);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (NP * NT <= 3) {
+        // few products per tile: bound by the loads, two tiles ahead
+        const auto step = [&](Stage& now, Stage& next, int kt) __attribute__((always_inline)) {
+            lds_barrier();
+            multiply(now.w, now.s, kt);
+            load(now, kt + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            keep(next, kt + 1);
+        };
+        load(st[1], min(first + 1, last - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        keep(st[0], first);
+        int kt = first;
+        for (; kt + 3 < last; kt += 2) {
+            step(st[0], st[1], kt);
+            step(st[1], st[0], kt + 1);
+        }
+        lds_barrier();
+        multiply(st[0].w, st[0].s, kt);
+        if (kt + 2 < last) load(st[0], kt + 2);
+        if (kt + 1 < last) {
+            keep(st[1], kt + 1);
+            lds_barrier();
+            multiply(st[1].w, st[1].s, kt + 1);
+        }
+        if (kt + 2 < last) {
+            keep(st[0], kt + 2);
+            lds_barrier();
+            multiply(st[0].w, st[0].s, kt + 2);
+        }
+    } else {
+        keep(st[0], first);
+        for (int kt = first; kt < last; ++kt) {
+            u32x4 w[RB];
+            uint32_t sc[RB];
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                w[i] = st[0].w[i];
+                sc[i] = st[0].s[i];
+            }
+            lds_barrier();
+            if (kt + 1 < last) load(st[0], kt + 1);
+            multiply(w, sc, kt);
+            if (kt + 1 < last) keep(st[0], kt + 1);
+        }
     }
     // lane: token 16 n + c, rows 4 q .. 4 q + 3 of each block
 #pragma unroll
@@ -555,6 +605,7 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
     constexpr int V = 8;
     const int t = blockIdx.x / nb;
     const int h = ((blockIdx.x - t * nb) * kThreads + threadIdx.x) * V;
+    const uint32_t valid = valid_entries(a, t);
     if (h >= a.H) return;
     float s[V];
 #pragma unroll
@@ -562,20 +613,21 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
     for (int sp = 0; sp < a.tsplits; ++sp) {
 #pragma unroll 4
         for (int k = 0; k < a.ks; ++k) {
-            if (entry_expert(a, t, k) < 0) continue;
+            // the other entries' bits cleared: a branch would keep their loads apart
+            const uint32_t mask = 0u - (valid >> k & 1u);
             const size_t e = (size_t(sp) * a.T + t) * a.ks + k;
             if constexpr (TF) {
-                const float4* p = reinterpret_cast<const float4*>(a.part + e * a.H + h);
-                const float4 u = p[0], v = p[1];
-                s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-                s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+                const u32x4* p = reinterpret_cast<const u32x4*>(a.part + e * a.H + h);
+                const u32x4 u = p[0] & mask, v = p[1] & mask;
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[i] += __uint_as_float(i < 4 ? u[i & 3] : v[i & 3]);
             } else {
                 union {
-                    uint4 q;
+                    u32x4 q;
                     _Float16 f[V];
                 } u;
-                u.q = *reinterpret_cast<const uint4*>(reinterpret_cast<const _Float16*>(a.part) + e * a.H + h);
-                const float sc = a.tscale[e * col_blocks(a.H) + h / 64];
+                u.q = *reinterpret_cast<const u32x4*>(reinterpret_cast<const _Float16*>(a.part) + e * a.H + h) & mask;
+                const float sc = __uint_as_float(__float_as_uint(a.tscale[e * col_blocks(a.H) + h / 64]) & mask);
 #pragma unroll
                 for (int i = 0; i < V; ++i) s[i] += float(u.f[i]) * sc;
             }
@@ -632,10 +684,6 @@ __device__ __forceinline__ Raw<F32> load_row(BlobRef rows, uint32_t at, bool in)
     return r;
 }
 
-// Nothing that uses the values is moved before this.
-template <class A, class B>
-__device__ __forceinline__ void hold(A& a, B& b) { asm volatile("" : "+v"(a), "+v"(b)); }
-
 // Work items lo, lo + step .. below hi (at least one), the next one's loads
 // (into the other of two stages) under way while one is used.  ready(i) comes
 // before the next loads, so that what it loads is waited for without them.
@@ -675,14 +723,6 @@ __device__ __forceinline__ void pipeline(S (&st)[2], int lo, int hi, int step, L
 __device__ __forceinline__ int share(uint32_t items, uint32_t wg, uint32_t n) {
     return __builtin_amdgcn_readfirstlane(int(items * wg / n));
 }
-
-// The scales of the group of column tiles that holds this one, and this one's.
-// (As a byte it would be extended where two stages' values meet, and waited
-// for there.)
-__device__ __forceinline__ uint32_t load_scales(BlobRef r, uint32_t at, int tile, uint32_t lane) {
-    return __builtin_amdgcn_raw_buffer_load_b32(r, int(lane * 4u), int(at + uint32_t(tile / kGroupTiles) * kGroupBytes), 0);
-}
-__device__ __forceinline__ float scale_in(uint32_t group, int tile) { return scale_of(group >> 8 * (tile % kGroupTiles) & 0xffu); }
 
 // The slots of a decode step in LDS: routed experts ascending, then the shared.
 struct SlotTable {
