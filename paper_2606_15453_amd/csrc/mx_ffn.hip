@@ -174,7 +174,9 @@ __global__ __launch_bounds__(kPlanThreads) void mx_tiles_kernel(MxArgs a) {
 // One expert's entries per workgroup, by token: order[g * T ..] and cnt[g].  A
 // thread compares its token's KU entries (FOUR: K is a multiple of four and
 // they are loaded four at a time) and takes the first that names the expert;
-// a wave's place is its lanes' ballot, the waves' places meet in LDS.
+// a wave's place is its lanes' ballot, the waves' places meet in LDS.  Bound by
+// the latency of 1024 tokens' loads and barriers after another: 12.5 us for 4096
+// tokens and 128 experts.
 template <int KU, bool FOUR>
 __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     constexpr int W = kPlanThreads / 64;
@@ -333,8 +335,9 @@ __device__ __forceinline__ BlobRef expert_blob(const MxArgs& a, const Blob& L, i
     return blob_ref(g < a.E ? a.eptr[g] : a.sptr[g - a.E], L);
 }
 
-// ONCE: read by one workgroup only, past the caches (DeepSeek-V2-Lite sizes, 16
-// tokens: gate and up 38 us through them, 33 past them).
+// ONCE: read by one workgroup only, past the caches (gate and up of
+// DeepSeek-V2-Lite sizes, 16 tokens: 33.9 us through them, 29.2 past them; of
+// Mixtral sizes, one token: 25.6 and 23.0).
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lane) {
     return __builtin_amdgcn_raw_buffer_load_b128(r, int(lane * 16u), int(at), ONCE ? 2 : 0);
@@ -358,11 +361,18 @@ __device__ __forceinline__ float scale_in(uint32_t group, int tile) { return sca
 // through LDS, 128 at a time, double-buffered.  A column's 256 bytes lie as 16
 // chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
 // lanes of a read, one chunk of 16 tokens, meet 16 different places.
+// Bound by the matrix instructions for many tokens (Qwen3-30B sizes, 4096 tokens:
+// up 189 us, 1090 TFLOP/s, where the library's 8192^3 product reaches 1213 on the
+// same card; down 138, 750, its six column tiles a workgroup against the time to
+// fetch the first and to store the sums), by the weights' bytes for few (64
+// tokens: 210 MB in 36.5 us, 5.7 TB/s).
+//
 // F32: the activations keep fp32 precision (up), the terms of y are fp32
-// (down); else activations are bf16, and terms fp16 with a power of two per 64:
-// off by 2^-11 of themselves at most, an eighth of what y's own rounding is,
-// and half the bytes that the down launch writes and the sum reads (Qwen3-30B
-// sizes, 4096 tokens: 393 us with fp32 terms, 349 with these).
+// (down); else activations are bf16, and terms fp16 over the power of two at or
+// below the largest of the token's 64: off by 2^-11 of themselves (an eighth of
+// what rounding y costs), or by 2^-25 of that largest if they are smaller than
+// 2^-14 of it, in half the bytes that the down launch writes and the sum reads
+// (4096 tokens: 138 + 24 us for the two launches, 148 + 43 with fp32 terms).
 template <bool UP, int NP, int NT, bool F32>
 __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, int sp, u32x4* xs, int* ent) {
     constexpr int TM = 16 * NT;
@@ -465,8 +475,10 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     const int first = UP ? 0 : KT * sp / a.tsplits, last = UP ? KT : KT * (sp + 1) / a.tsplits;
     load(st[0], first);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (NP * NT <= 3) {
-        // few products per tile: bound by the loads, two tiles ahead
+    if constexpr (NT == 1) {
+        // few products per column tile: bound by the loads, two of them ahead (20
+        // tokens, H 2048, I 1408, 16 experts: 29.6 us a call, 32.6 with one; with
+        // 32 tokens a tile the two are equal)
         const auto step = [&](Stage& now, Stage& next, int kt) __attribute__((always_inline)) {
             lds_barrier();
             multiply(now.w, now.s, kt);
@@ -474,7 +486,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
             __builtin_amdgcn_sched_barrier(0);
             keep(next, kt + 1);
         };
-        load(st[1], min(first + 1, last - 1));
+        load(st[1], min(first + 1, last - 1));              // (not behind a branch, see pipeline)
         __builtin_amdgcn_sched_barrier(0);
         keep(st[0], first);
         int kt = first;
@@ -579,8 +591,10 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     }
 }
 
+// Three waves per SIMD (168 registers); four where they cost no spills in the loop
+// and pay: 1024 tokens of top-4, tiles of 32, 73.0 us a call, 76.3 with three.
 template <bool UP, int NP, int NT, bool F32>
-__global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) {
+__global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_kernel(MxArgs a, int nb) {
     constexpr int TM = 16 * NT;
     __shared__ u32x4 xs[2][NP * TM * kTileCols / 8];
     __shared__ int ent[TM];
@@ -599,7 +613,8 @@ __global__ __launch_bounds__(kThreads, 3) void mx_tile_kernel(MxArgs a, int nb) 
 }
 
 // y[t] = the sum of its entries' terms (TF: fp32, else fp16 with their power of
-// two), in the entries' order, in fp32.
+// two), in the entries' order, in fp32.  Bound by the terms' bytes (4096 tokens of
+// top-8, H 2048: 151 MB in 23.7 us, 6.4 TB/s).
 template <bool TF, bool YF>
 __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
     constexpr int V = 8;
@@ -660,6 +675,12 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
 // takes an equal run of the row blocks to compute, its waves share the
 // contraction and keep their columns in registers, so that the loop loads
 // weights alone, the next row block's while the present one's are used.
+// Measured, Mixtral sizes, one token: up 125 MB in 23.0 us and down 62 MB in
+// 15.0 + 3.9 (join); DeepSeek-V2-Lite sizes, 16 tokens: 161 MB in 29.2, 81 MB in
+// 20.6 + 4.0.  About 6 us of each launch pass before the first weights arrive
+// (selection, pointers, weights, one after the other) and after the last; in
+// between the up launch streams 7 TB/s, the down launch, whose waves' sums meet
+// in LDS for every four row blocks, 5.
 
 // A distinct expert of a decode step and, per token, the entry that selects it.
 struct DecodeSlot {
@@ -1159,7 +1180,10 @@ __global__ __launch_bounds__(1024) void mx_join_kernel(MxArgs a) {
 }
 
 // The down launch's forms: up to 48 column tiles of few columns in one chunk of
-// sixteen waves, else chunks of eight tiles.
+// sixteen waves, whose sums are y (one token, H 2048, I 768, top 8: a call 13.1
+// us, 14.2 with chunks; H 4096, I 1408, top 4, bf16 y: 15.7 and 18.6), else chunks
+// of eight tiles (two row blocks at a time, or four waves: up to 10% slower;
+// sixteen waves: within 3%).
 constexpr int kOneWaves = 16, kOneU = 3, kOneR = 1;
 constexpr int kRunWaves = 8, kRunU = 1, kRunR = 4;
 
@@ -1224,6 +1248,13 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
     return y;
 }
 
+// Row blocks in turn with the columns in registers, for bf16 x of up to 32 column
+// tiles (16 tokens of top-8 of 64, I 1536, whole calls: H 512 31.7 us, 40.1 with
+// mx_up_wide; 1024 44.1 and 49.8; 2048 65.6 and 71.6; 4096 113 and 117; one token
+// the same with both).  Four waves take 1, 2 or 4 tiles each (with 4 throughout H
+// 512 34.6 us, 1024 45.3), eight 4; as many workgroups as stay side by side on the
+// 256 CUs, but up to 1024 row blocks of four waves one each (one token, H 2048, I
+// 1536: 18.0 us, 19.4 on 512).
 template <int NX, int NH>
 void launch_up_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
     const int KT = col_tiles(a.H), NB = row_blocks(a.I);
@@ -1265,6 +1296,9 @@ int launch_decode(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t 
     launch_up_decode<NX, NH>(a, L, s);
     STMOE_LAUNCHED();
     if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
+    // up to five tokens of fp32 y the three pieces of a column are columns of one
+    // instruction (one token, H 2048, I 768, top 8: a call 13.1 us, 14.8 with three
+    // instructions; five tokens 27.8 and 29.9)
     if (YF && a.T * NH <= kMaxB) return launch_down_decode<NH, YF, YF>(a, L, s);
     return launch_down_decode<NH, false, YF>(a, L, s);
 }

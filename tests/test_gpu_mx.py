@@ -196,6 +196,24 @@ def test_ffn_parity(T, H, I, E, K, ns, x_bf16, y_bf16):
     assert err <= _tol(x_bf16, y_bf16)
 
 
+@pytest.mark.parametrize("T,H,I,E,K", [(2000, 264, 4104, 20, 2), (8192, 264, 264, 16, 4)])
+def test_ffn_prompts_in_large_tiles(T, H, I, E, K):
+    """bf16 prompts large enough for tiles of 64 tokens, the down product in parts and whole; a token's bits do not
+    depend on the tokens beside it, whichever kind of tile it falls into."""
+    import torch
+    ex = Experts(E, H, I, T)
+    x, idx, w = _inputs(T, K, E, H, 3, torch.bfloat16)
+    idx[::50] = -1
+    y = _run(ex, E, H, I, x, idx, w, torch.bfloat16)
+    want = mxref.moe_ffn(_f64(x), idx.cpu().numpy(), _f64(w), ex.values)
+    assert _err(y, want) <= _tol(True, True)
+    x2, idx2, w2 = _inputs(T, K, E, H, 4, torch.bfloat16)
+    idx2[:, 0] = 1
+    keep = slice(T // 2, T // 2 + 40)
+    x2[keep], idx2[keep], w2[keep] = x[keep], idx[keep], w[keep]
+    assert torch.equal(_run(ex, E, H, I, x2, idx2, w2, torch.bfloat16)[keep], y[keep])
+
+
 @pytest.mark.parametrize("H,I", [(4096, 14336), (2048, 1408), (16384, 64), (64, 65536)])
 @pytest.mark.parametrize("T", [1, 20])
 def test_ffn_large_experts(H, I, T):
