@@ -20,7 +20,7 @@ using namespace mx;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanEntries = 1024;
+constexpr int kPlanEntries = 256;
 constexpr int kMaxShared = 8;
 constexpr int kMaxT = 65536;
 constexpr int kMaxGroups = kMaxE + kMaxShared;
@@ -175,8 +175,8 @@ __global__ __launch_bounds__(kPlanThreads) void mx_tiles_kernel(MxArgs a) {
 // thread compares its token's KU entries (FOUR: K is a multiple of four and
 // they are loaded four at a time) and takes the first that names the expert;
 // a wave's place is its lanes' ballot, the waves' places meet in LDS.  Bound by
-// the latency of 1024 tokens' loads and barriers after another: 12.5 us for 4096
-// tokens and 128 experts.
+// the latency of its barriers, 1024 tokens after another, the next ones' entries
+// on their way: 5.0 us for 4096 tokens and 128 experts.
 template <int KU, bool FOUR>
 __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     constexpr int W = kPlanThreads / 64;
@@ -188,22 +188,30 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
         if (threadIdx.x == 0) a.cnt[g] = a.T;
         return;
     }
-    int before = 0;
-    for (int t0 = 0, par = 0; t0 < a.T; t0 += kPlanThreads, par ^= 1) {
-        const int t = t0 + threadIdx.x;
+    int before = 0, e[KU];
+    // beyond K the last entry again, which does not count there
+    auto load = [&](int t) __attribute__((always_inline)) {
         const int32_t* row = a.idx + size_t(min(t, a.T - 1)) * a.K;
-        int k = -1;
 #pragma unroll
-        for (int j = KU - (FOUR ? 4 : 1); j >= 0; j -= FOUR ? 4 : 1) {
-            // beyond K the last entry again, which does not count there
+        for (int j = 0; j < KU; j += FOUR ? 4 : 1) {
             if constexpr (FOUR) {
-                const int4 e = *reinterpret_cast<const int4*>(row + min(j, a.K - 4));
-                const int f = e.x == g ? j : e.y == g ? j + 1 : e.z == g ? j + 2 : e.w == g ? j + 3 : -1;
-                k = f >= 0 && j < a.K ? f : k;
+                const int4 v = *reinterpret_cast<const int4*>(row + min(j, a.K - 4));
+                e[j] = v.x;
+                e[j + 1] = v.y;
+                e[j + 2] = v.z;
+                e[j + 3] = v.w;
             } else {
-                k = row[min(j, a.K - 1)] == g && j < a.K ? j : k;
+                e[j] = row[min(j, a.K - 1)];
             }
         }
+    };
+    load(threadIdx.x);
+    for (int t0 = 0, par = 0; t0 < a.T; t0 += kPlanThreads, par ^= 1) {
+        const int t = t0 + threadIdx.x;
+        int k = -1;
+#pragma unroll
+        for (int j = KU - 1; j >= 0; --j) k = (e[j] == g) & (j < a.K) ? j : k;
+        load(t + kPlanThreads);
         if (t >= a.T) k = -1;
         const unsigned long long m = __ballot(k >= 0);
         if (lane == 0) found[par][wave] = __popcll(m);
@@ -220,21 +228,21 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     if (threadIdx.x == 0) a.cnt[g] = before;
 }
 
-// All experts' entries and the tiles by one workgroup, a thread per token.  For
-// at most kPlanEntries entries, where it saves a launch (whole calls, H 512, I
-// 128 to 256, against the two launches above: 20 tokens of top-2 16.6 and 17.6
-// us, 128 of top-8 21.8 both, 256 of top-8 25.2 and 24.3).  An expert's tokens are bits of a mask in LDS, a token's
-// place the number of bits below its own; a bit that its thread finds set is a
-// repeated expert.  The KU entries are handled side by side, without branches,
-// so that their LDS accesses overlap; entries that name no expert meet words of
-// their own.
+// All experts' entries and the tiles by one workgroup, a thread per token, for at
+// most kPlanEntries entries: it saves a launch (whole calls against the two
+// launches above: 20 tokens of top-2 15.9 and 16.9 us, 37 of top-3 26.4 and 27.1;
+// beyond 300 entries it no longer did).  An expert's tokens are bits of a mask in
+// LDS, a token's place the number of bits below its own; a bit that its thread
+// finds set is a repeated expert.  The KU entries are handled side by side,
+// without branches, so that their LDS accesses overlap; entries that name no
+// expert meet words of their own.
 template <int KU>
 __global__ __launch_bounds__(kPlanThreads) void mx_plan_kernel(MxArgs a) {
-    constexpr int W = kPlanThreads / 32;                    // words of a mask
+    constexpr int W = kPlanEntries / 32;                    // words of a mask
     __shared__ uint32_t mask[kMaxE + 2][W];                 // the last two: nobody's
     __shared__ uint16_t below[kMaxE][W];
     __shared__ int cnt[kMaxGroups], tile[kMaxGroups + 1];
-    const int tid = threadIdx.x, t = tid, w = tid >> 5;
+    const int tid = threadIdx.x, t = tid, w = min(tid >> 5, W - 1);
     const bool four = a.K % 4 == 0 && reinterpret_cast<uintptr_t>(a.idx) % 16 == 0;
     const int32_t* row = a.idx + size_t(t < a.T ? t : 0) * a.K;
     int e[KU];
@@ -261,7 +269,7 @@ __global__ __launch_bounds__(kPlanThreads) void mx_plan_kernel(MxArgs a) {
 #pragma unroll
     for (int j = 0; j < KU; ++j) {
         mine[j] = e[j] >= 0 && e[j] < a.E;
-        word[j] = mine[j] ? &mask[e[j]][w] : &mask[kMaxE][tid & 63];
+        word[j] = mine[j] ? &mask[e[j]][w] : &mask[kMaxE][tid % (2 * W)];
     }
     const uint32_t bit = 1u << (tid & 31);
     uint32_t was[KU];
@@ -270,16 +278,16 @@ __global__ __launch_bounds__(kPlanThreads) void mx_plan_kernel(MxArgs a) {
 #pragma unroll
     for (int j = 0; j < KU; ++j) mine[j] &= !(was[j] & bit);
     lds_barrier();
-    // 32 lanes: an expert's words
-    for (int g = w; g < a.E; g += W) {
-        const int l = tid & 31, c = __builtin_popcount(mask[g][l]);
+    // W lanes: an expert's words
+    for (int g = tid / W; g < a.E; g += kPlanThreads / W) {
+        const int l = tid % W, c = __builtin_popcount(mask[g][l]);
         int v = c;
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up(v, d, 32);
+        for (int d = 1; d < W; d <<= 1) {
+            const int o = __shfl_up(v, d, W);
             if (l >= d) v += o;
         }
         below[g][l] = uint16_t(v - c);
-        if (l == 31) cnt[g] = v;
+        if (l == W - 1) cnt[g] = v;
     }
     if (tid < a.ns) cnt[a.E + tid] = a.T;
     lds_barrier();

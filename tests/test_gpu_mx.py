@@ -227,7 +227,7 @@ def test_ffn_large_experts(H, I, T):
 
 @pytest.mark.parametrize("y_bf16", [False, True])
 @pytest.mark.parametrize("T,K,E,off", [
-    (5, 8, 20, 0), (6, 8, 20, 1), (16, 16, 256, 0), (16, 9, 256, 3), (17, 16, 20, 0), (20, 9, 12, 0), (64, 16, 16, 1),
+    (5, 8, 20, 0), (6, 8, 20, 1), (17, 15, 40, 0), (32, 8, 256, 0), (33, 8, 256, 0), (256, 1, 7, 0), (257, 1, 7, 0), (16, 16, 256, 0), (16, 9, 256, 3), (17, 16, 20, 0), (20, 9, 12, 0), (64, 16, 16, 1),
     (65, 16, 20, 0), (100, 8, 16, 1), (120, 9, 11, 0), (130, 16, 20, 0), (130, 16, 20, 1), (300, 8, 16, 2), (1024, 1, 256, 0),
     (1025, 1, 2, 0), (1100, 12, 64, 0)])
 def test_ffn_selections_of_every_width(T, K, E, off, y_bf16):
