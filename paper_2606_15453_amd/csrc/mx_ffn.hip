@@ -47,7 +47,7 @@ struct MxArgs {
     struct DecodeSlot* slots;       // by ascending expert, the shared ones last
     int32_t* nslots;
     int smax;                       // slots at most
-    float* split;                   // [chunk][row block of H][256] sums of the down launch
+    float* split;                   // [chunk][4 row blocks of H][token][row] sums of the down launch
     unsigned long long* n_experts;  // counts distinct routed experts (timed decode layers), or null
 };
 
@@ -350,7 +350,6 @@ template <bool ONCE>
 __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lane) {
     return __builtin_amdgcn_raw_buffer_load_b128(r, int(lane * 16u), int(at), ONCE ? 2 : 0);
 }
-
 
 // The scales of the group of column tiles that holds this one, and this one's.
 // (As a byte it would be extended where two stages' values meet, and waited
@@ -684,8 +683,8 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
 // contraction and keep their columns in registers, so that the loop loads
 // weights alone, the next row block's while the present one's are used.
 // Measured, Mixtral sizes, one token: up 125 MB in 23.0 us and down 62 MB in
-// 15.0 + 3.9 (join); DeepSeek-V2-Lite sizes, 16 tokens: 161 MB in 29.2, 81 MB in
-// 20.6 + 4.0.  About 6 us of each launch pass before the first weights arrive
+// 13.8 + 3.9 (join); DeepSeek-V2-Lite sizes, 16 tokens: 161 MB in 29.2, 81 MB in
+// 21.4 + 3.9.  About 6 us of each launch pass before the first weights arrive
 // (selection, pointers, weights, one after the other) and after the last; in
 // between the up launch streams 7 TB/s, the down launch, whose waves' sums meet
 // in LDS for every four row blocks, 5.
@@ -1013,10 +1012,13 @@ __global__ __launch_bounds__(kThreads) void mx_up_wide(MxArgs a, int nrb) {
 // rows, U per wave, whose activations the wave holds while it goes through the
 // row blocks.  With one chunk the sums are y, else the chunks' sums go to the
 // join launch.  PC: few tokens, whose pieces are columns too.
+// (Four waves per SIMD: with 142 registers for three pieces only one workgroup
+// would fit a CU.)
 template <int NH, bool PC, bool YF, int NW, int U, int R>
-__global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) {
+__global__ __launch_bounds__(64 * NW, 4) void mx_down_decode(MxArgs a, int direct) {
     constexpr int MP = PC ? 1 : NH;                         // instructions per operand
     constexpr int N = 64 * NW, OUT = R * 256;
+    constexpr int PER = ((PC ? kMaxB / NH : kMaxB) * R * kTileRows + N - 1) / N;
     __shared__ SlotTable tab;
     __shared__ float red[2][NW][OUT];
     const uint32_t lane = threadIdx.x & 63;
@@ -1084,6 +1086,10 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
             }
         }
     };
+    // Where a sum is put (chunks): the columns of a row permuted by row and row
+    // block, so that half a wave meets 32 banks both here, where it has two rows of
+    // 16 columns, and in finish, where it has 16 rows of two row blocks.
+    const int put = U > 1 ? int(lane) : int(lane) ^ (int(lane) >> 5) << 1;
     auto multiply = [&](const Stage& d, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -1103,29 +1109,53 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
                 for (int r = 0; r < 4; ++r) sum[r] += live[j] ? acc[r] : 0.f;
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) red[buf][wave][(i * 4 + r) * 64 + lane] = sum[r];
+            for (int r = 0; r < 4; ++r) red[buf][wave][i * 256 + r * 64 + (put ^ (U > 1 ? 0 : r * 4 + (i & 1)))] = sum[r];
         }
     };
+    // the sums of the waves, and of a token's pieces
     auto finish = [&](int item, int buf) __attribute__((always_inline)) {
         lds_barrier();
-#pragma unroll
-        for (int o = tid; o < OUT; o += N) {
+        const auto store = [&](int tok, int row, float v) __attribute__((always_inline)) {
+            if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(tok) * a.H + row] = v;
+            else reinterpret_cast<__bf16*>(a.y)[size_t(tok) * a.H + row] = __bf16(v);
+        };
+        if constexpr (U > 1) {
+            // one row block, a thread per row and column
+            if (tid >= OUT) return;
             float v = 0.f;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) v += red[buf][w][o];
-            if (!direct) {
-                a.split[size_t(item) * OUT + o] = v;
-                continue;
-            }
-            float s = v;
+            for (int w = 0; w < NW; ++w) v += red[buf][w][tid];
             if constexpr (PC) {
-                s += __shfl_down(v, 1, 64);
-                s += __shfl_down(v, 2, 64);
+                static_assert(NH == 3, "a token's pieces are three columns");
+                v += __shfl_down(v, 1, 64) + __shfl_down(v, 2, 64);
             }
-            const int row = (item * R + o / 256) * kTileRows + 4 * q + (o / 64 & 3);
-            if (t >= a.T || pc || row >= a.H) continue;
-            if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = s;
-            else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
+            const int row = item * kTileRows + 4 * q + tid / 64;
+            if (t < a.T && !pc && row < a.H) store(t, row, v);
+            return;
+        }
+        // [token][row block][row]: of the tokens that are there, so that few of them
+        // have few sums to write and to join (Mixtral sizes, one token: the down
+        // launch 15.5 us with all 16 columns' sums, 13.8 with these)
+        float v[PER];
+#pragma unroll
+        for (int z = 0; z < PER; ++z) {
+            const int o = tid + z * N, row = o % kTileRows, i = o / kTileRows % R, tok = o / (R * kTileRows);
+            v[z] = 0.f;
+            if (tok >= a.T) break;
+            const float* p = &red[buf][0][i * 256 + row % 4 * 64 + row / 4 * 16];
+            const int to = row % 4 * 4 + row / 8 * 2 + (i & 1);
+#pragma unroll
+            for (int x = 0; x < (PC ? NH : 1); ++x)
+#pragma unroll
+                for (int w = 0; w < NW; ++w) v[z] += p[w * OUT + ((PC ? NH * tok + x : tok) ^ to)];
+        }
+#pragma unroll
+        for (int z = 0; z < PER; ++z) {
+            const int o = tid + z * N, row = (item * R + o / kTileRows % R) * kTileRows + o % kTileRows;
+            const int tok = o / (R * kTileRows);
+            if (tok >= a.T) break;
+            if (!direct) a.split[size_t(item) * (a.T * R * kTileRows) + o] = v[z];
+            else if (row < a.H) store(tok, row, v[z]);
         }
     };
     if (units == 0) {
@@ -1158,33 +1188,26 @@ __global__ __launch_bounds__(64 * NW) void mx_down_decode(MxArgs a, int direct) 
     }
 }
 
-// y from the chunks' sums, in their order: a row block per workgroup.
-template <int NH, bool PC, bool YF, int TILES, int R>
+// y from the chunks' sums, in their order: 256 of a chunk's sums per workgroup,
+// four threads each.
+template <bool YF, int TILES, int R>
 __global__ __launch_bounds__(1024) void mx_join_kernel(MxArgs a) {
     __shared__ float red[4][256];
-    const int rb = blockIdx.x, tid = threadIdx.x, o = tid & 255, part = tid >> 8;
+    const int tid = threadIdx.x, o = int(blockIdx.x) * 256 + (tid & 255), part = tid >> 8;
     const int groups = (row_blocks(a.H) + R - 1) / R, units = *a.nslots * col_tiles(a.I);
-    const int chunks = max(1, (units + TILES - 1) / TILES);
-    const float* p = a.split + size_t(rb / R) * R * 256 + rb % R * 256 + o;
+    const int chunks = max(1, (units + TILES - 1) / TILES), n = groups * R * kTileRows * a.T;
     float v = 0.f;
+    if (o < n) {
 #pragma unroll 8
-    for (int x = part; x < chunks; x += 4) v += p[size_t(x) * groups * R * 256];
-    red[part][o] = v;
-    __syncthreads();
-    if (tid < 256) red[0][o] = (red[0][o] + red[1][o]) + (red[2][o] + red[3][o]);
-    __syncthreads();
-    for (int i = tid; i < kTileRows * a.T; i += 1024) {
-        const int t = i / kTileRows, rr = i % kTileRows, row = rb * kTileRows + rr;
-        if (row >= a.H) continue;
-        const float* f = &red[0][rr % 4 * 64 + rr / 4 * 16 + (PC ? NH * t : t)];
-        float s = f[0];
-        if constexpr (PC) {
-#pragma unroll
-            for (int c = 1; c < NH; ++c) s += f[c];
-        }
-        if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = s;
-        else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
+        for (int x = part; x < chunks; x += 4) v += a.split[size_t(x) * n + o];
     }
+    red[part][tid & 255] = v;
+    __syncthreads();
+    const int t = o / (R * kTileRows) % a.T, row = (o / (R * kTileRows * a.T) * R + o / kTileRows % R) * kTileRows + o % kTileRows;
+    if (part || o >= n || row >= a.H) return;
+    const float s = (red[0][tid] + red[1][tid]) + (red[2][tid] + red[3][tid]);
+    if constexpr (YF) reinterpret_cast<float*>(a.y)[size_t(t) * a.H + row] = s;
+    else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
 }
 
 // The down launch's forms: up to 48 column tiles of few columns in one chunk of
@@ -1236,7 +1259,7 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
         y.plan = take(size_t(y.slots) * sizeof(DecodeSlot));
         y.nslots = take(sizeof(int32_t));
         const size_t chunks = (size_t(y.units) + kRunWaves * kRunU - 1) / (kRunWaves * kRunU);
-        y.split = take(chunks * ((row_blocks(H) + kRunR - 1) / kRunR * kRunR) * 256 * sizeof(float));
+        y.split = take(chunks * ((row_blocks(H) + kRunR - 1) / kRunR * kRunR) * kTileRows * T * sizeof(float));
     } else {
         y.tm = tile_tokens(T, K, E, ns, I, dtype == STMOE_BF16 && ydtype == STMOE_BF16);
         // a full tile takes tm entries; each expert has at most one that is not full
@@ -1292,7 +1315,8 @@ int launch_down_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
                        dim3(64 * kRunWaves), 0, s, a, chunks == 1);
     STMOE_LAUNCHED();
     if (chunks > 1) {
-        hipLaunchKernelGGL((mx_join_kernel<NH, PC, YF, kRunWaves * kRunU, kRunR>), dim3(unsigned(NB)), dim3(1024), 0, s, a);
+        const int64_t sums = int64_t((NB + kRunR - 1) / kRunR * kRunR) * kTileRows * a.T;
+        hipLaunchKernelGGL((mx_join_kernel<YF, kRunWaves * kRunU, kRunR>), dim3(unsigned((sums + 255) / 256)), dim3(1024), 0, s, a);
         STMOE_LAUNCHED();
     }
     return STMOE_OK;
