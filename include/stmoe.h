@@ -326,7 +326,8 @@ int moe_mx_pack_expert(const uint8_t* gate_codes, const uint8_t* gate_scales, co
  *   y            device out [T][H] ydtype, 16-byte aligned
  *   ws           device workspace of moe_expert_ffn_mx_workspace_bytes(...)
  *                bytes, 256-byte aligned, no initial contents required; calls
- *                sharing it must be ordered on one stream
+ *                sharing it must be ordered on one stream.  Its size does not
+ *                always grow with T: calls of several sizes share the largest
  * dtype and ydtype: STMOE_BF16 or STMOE_F32 each.  Sums are fp32.  fp32 x, and
  * the activations when y is fp32, enter the products as bf16 pieces that hold
  * their 24 bits; with bf16 y the activations are rounded to bf16 (and fp32 x

@@ -459,6 +459,32 @@ def test_ffn_other_stream_and_graph(T):
         assert torch.equal(y, eager), seed
 
 
+@pytest.mark.parametrize("T", [2, 90])
+def test_ffn_graphs_that_share_a_workspace(T):
+    """Two captured calls of different sizes over one workspace, replayed in turn on one stream."""
+    import torch
+    H, I, E, K = 256, 264, 10, 3
+    ex = Experts(E, H, I, 8)
+    s = torch.cuda.Stream()
+    ws = _ws(T + 40, K, E, H, I, 0, torch.bfloat16, torch.float32)
+    graphs = []
+    for n in (T, T + 40):
+        x, idx, w = _inputs(n, K, E, H, n, torch.bfloat16)
+        alone = _run(ex, E, H, I, x, idx, w, torch.float32)
+        y = torch.empty((n, H), device=DEV)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            _run(ex, E, H, I, x, idx, w, torch.float32, y=y, ws=ws, stream=s)
+        graphs.append((g, y, alone, x, idx, w))
+    for i in (0, 1, 1, 0, 1, 0, 0):
+        g, y, alone = graphs[i][:3]
+        y.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, alone)
+
+
 def test_ffn_entries_beyond_32_bit_offsets():
     """65536 tokens whose partial rows pass 4 GiB: tokens of both ends and the middle against 64 bits."""
     import torch
