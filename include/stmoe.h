@@ -331,10 +331,8 @@ int moe_mx_pack_expert(const uint8_t* gate_codes, const uint8_t* gate_scales, co
  * dtype and ydtype: STMOE_BF16 or STMOE_F32 each.  Sums are fp32.  fp32 x, and
  * the activations when y is fp32, enter the products as bf16 pieces that hold
  * their 24 bits; with bf16 y the activations are rounded to bf16 (and fp32 x
- * to 16 bits), and beyond 16 tokens an expert's term of y may be rounded to
- * fp16 over a power of two that 64 columns share (off by 2^-11 of itself, or by
- * 2^-25 of the 64's largest where it is below 2^-14 of that).  An fp32 x that
- * rounds to an infinite bf16 (above 3.39e38) counts as infinite.  T (K +
+ * to 16 bits).  An fp32 x that rounds to an infinite bf16 (above 3.39e38)
+ * counts as infinite.  T (K +
  * n_shared) I elements of activations, 2 bytes each (6 with fp32 y), are at
  * most 64 GiB.  The same inputs give the same bits.  With more than 16 tokens
  * a token's result does not depend on the other tokens' values; up to 16 the

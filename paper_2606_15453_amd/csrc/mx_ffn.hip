@@ -42,7 +42,6 @@ struct MxArgs {
     int32_t* ntiles;
     uint16_t* act;                  // [entry][piece][I] bf16 pieces
     float* part;                    // [part][entry][H] terms of y
-    float* tscale;                  // [entry][64 columns of H] their powers of two, where they are fp16
     // decode steps (T <= 16)
     struct DecodeSlot* slots;       // by ascending expert, the shared ones last
     int32_t* nslots;
@@ -109,8 +108,6 @@ __device__ __forceinline__ Pieces<N> pieces(const Raw<(N > 1)>& r) {
     }
     return o;
 }
-
-__device__ __forceinline__ int col_blocks(int H) { return (H + 63) / 64; }
 
 // g / (1 + exp(-g)) with the hardware's exponential and reciprocal (2^-23 of
 // their values; the exponent's product rounds to 2^-24 of |g|, so silu is off
@@ -373,14 +370,13 @@ __device__ __forceinline__ float scale_in(uint32_t group, int tile) { return sca
 // same card; down 138, 750, its six column tiles a workgroup against the time to
 // fetch the first and to store the sums), by the weights' bytes for few (64
 // tokens: 210 MB in 36.5 us, 5.7 TB/s).
+// The experts' terms of y go to memory in fp32, whatever y's type: they are parts of
+// its sum, and a column of y may be far smaller than the columns beside it (fp16
+// terms over a power of two per 64 columns took 4096 tokens from 424 to 404 us a
+// call and lost every column 2^-25 of its neighbours' size).
 //
-// F32: the activations keep fp32 precision (up), the terms of y are fp32
-// (down); else activations are bf16, and terms fp16 over the power of two at or
-// below the largest of the token's 64: off by 2^-11 of themselves (an eighth of
-// what rounding y costs), or by 2^-25 of that largest if they are smaller than
-// 2^-14 of it, in half the bytes that the down launch writes and the sum reads
-// (4096 tokens: 138 + 24 us for the two launches, 148 + 43 with fp32 terms).
-template <bool UP, int NP, int NT, bool F32>
+// NP: pieces of the columns, NH: of the activations (up).
+template <bool UP, int NP, int NT, int NH>
 __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int bk, int sp, u32x4* xs, int* ent) {
     constexpr int TM = 16 * NT;
     constexpr int RB = 4;                                   // row blocks per wave
@@ -536,7 +532,6 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         if (16 * n + c >= tl.z) continue;
         const int e = ent[16 * n + c];
         if constexpr (UP) {
-            constexpr int NH = kPiecesH<F32>;
 #pragma unroll
             for (int i = 0; i < RB / 2; ++i) {
                 const int row = rb[i] * kTileRows + 4 * q;
@@ -559,40 +554,11 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         } else {
             const int t = e / a.ks, k = e - t * a.ks;
             const float w = k < a.K ? a.w[size_t(t) * a.K + k] : 1.f;
-            f32x4 d[RB];
-#pragma unroll
-            for (int i = 0; i < RB; ++i) d[i] = w * acc[i][n];
-            float back = 1.f;
-            if constexpr (!F32) {
-                // fp16 terms over the power of two below the largest of the
-                // token's 64 (infinities and NaN aside, which fp16 keeps)
-                float top = 0.f;
-#pragma unroll
-                for (int i = 0; i < RB; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) top = fmaxf(top, __builtin_isfinite(d[i][r]) ? fabsf(d[i][r]) : 0.f);
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const uint32_t eb = min(max(__float_as_uint(top) >> 23, 1u), 253u);
-                back = __uint_as_float((254u - eb) << 23);
-                if (q == 0 && rb[0] < NB) a.tscale[size_t(e) * col_blocks(a.H) + rb[0] / RB] = __uint_as_float(eb << 23);
-            }
 #pragma unroll
             for (int i = 0; i < RB; ++i) {
                 const int row = rb[i] * kTileRows + 4 * q;
                 if (row >= a.H) continue;
-                const size_t at = (size_t(sp) * a.T * a.ks + e) * a.H + row;
-                if constexpr (F32) {
-                    *reinterpret_cast<f32x4*>(a.part + at) = d[i];
-                } else {
-                    union {
-                        _Float16 h[4];
-                        uint2 v;
-                    } o;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o.h[r] = _Float16(d[i][r] * back);
-                    *reinterpret_cast<uint2*>(reinterpret_cast<_Float16*>(a.part) + at) = o.v;
-                }
+                *reinterpret_cast<f32x4*>(a.part + (size_t(sp) * a.T * a.ks + e) * a.H + row) = w * acc[i][n];
             }
         }
     }
@@ -600,7 +566,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 
 // Three waves per SIMD (168 registers); four where they cost no spills in the loop
 // and pay: 1024 tokens of top-4, tiles of 32, 73.0 us a call, 76.3 with three.
-template <bool UP, int NP, int NT, bool F32>
+template <bool UP, int NP, int NT, int NH>
 __global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_kernel(MxArgs a, int nb) {
     constexpr int TM = 16 * NT;
     __shared__ u32x4 xs[2][NP * TM * kTileCols / 8];
@@ -614,15 +580,14 @@ __global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_
     const int4 tl = a.tiles[tix];
     if constexpr (NT > 1) {
         // an expert's last tile, if at most half full, in half the instructions
-        if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, F32>(a, tl, bk, sp, xs[0], ent);
+        if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, NH>(a, tl, bk, sp, xs[0], ent);
     }
-    tile_product<UP, NP, NT, F32>(a, tl, bk, sp, xs[0], ent);
+    tile_product<UP, NP, NT, NH>(a, tl, bk, sp, xs[0], ent);
 }
 
-// y[t] = the sum of its entries' terms (TF: fp32, else fp16 with their power of
-// two), in the entries' order, in fp32.  Bound by the terms' bytes (4096 tokens of
-// top-8, H 2048: 151 MB in 23.7 us, 6.4 TB/s).
-template <bool TF, bool YF>
+// y[t] = the sum of its entries' terms, in the entries' order, in fp32.  Bound by
+// the terms' bytes (4096 tokens of top-8, H 2048: 285 MB in 43 us, 6.6 TB/s).
+template <bool YF>
 __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
     constexpr int V = 8;
     const int t = blockIdx.x / nb;
@@ -638,21 +603,10 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
             // the other entries' bits cleared: a branch would keep their loads apart
             const uint32_t mask = 0u - (valid >> k & 1u);
             const size_t e = (size_t(sp) * a.T + t) * a.ks + k;
-            if constexpr (TF) {
-                const u32x4* p = reinterpret_cast<const u32x4*>(a.part + e * a.H + h);
-                const u32x4 u = p[0] & mask, v = p[1] & mask;
+            const u32x4* p = reinterpret_cast<const u32x4*>(a.part + e * a.H + h);
+            const u32x4 u = p[0] & mask, v = p[1] & mask;
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[i] += __uint_as_float(i < 4 ? u[i & 3] : v[i & 3]);
-            } else {
-                union {
-                    u32x4 q;
-                    _Float16 f[V];
-                } u;
-                u.q = *reinterpret_cast<const u32x4*>(reinterpret_cast<const _Float16*>(a.part) + e * a.H + h) & mask;
-                const float sc = __uint_as_float(__float_as_uint(a.tscale[e * col_blocks(a.H) + h / 64]) & mask);
-#pragma unroll
-                for (int i = 0; i < V; ++i) s[i] += float(u.f[i]) * sc;
-            }
+            for (int i = 0; i < V; ++i) s[i] += __uint_as_float(i < 4 ? u[i & 3] : v[i & 3]);
         }
     }
     if constexpr (YF) {
@@ -1220,7 +1174,7 @@ constexpr int kRunWaves = 8, kRunU = 1, kRunR = 4;
 
 struct MxLayout {
     int tm, max_tiles, tsplits, slots, units;
-    size_t order, cnt, tiles, ntiles, act, part, tscale, xs, plan, nslots, split, total;
+    size_t order, cnt, tiles, ntiles, act, part, xs, plan, nslots, split, total;
 };
 
 // Tokens per tile: 64 where an expert gets more than 32 on average, both x and
@@ -1270,9 +1224,7 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
         y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
         y.ntiles = take(sizeof(int32_t));
         y.tsplits = tile_splits(y.tm, n, E, ns, H, I);
-        const bool tf = ydtype == STMOE_F32 || y.tsplits > 1;
-        y.part = take(n * y.tsplits * H * (tf ? sizeof(float) : sizeof(uint16_t)));
-        if (!tf) y.tscale = take(n * ((H + 63) / 64) * sizeof(float));
+        y.part = take(n * y.tsplits * H * sizeof(float));
         if (dtype == STMOE_F32) y.xs = take(size_t(T) * H * (ydtype == STMOE_F32 ? 3 : 2) * sizeof(uint16_t));
     }
     y.total = off;
@@ -1342,18 +1294,13 @@ int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t e
     const int ub = (a.I + 127) / 128, db = (a.H + 255) / 256 * L.tsplits;
     const int sb = (a.H + kThreads * 8 - 1) / (kThreads * 8);
     const dim3 sgrid(unsigned(a.T) * unsigned(sb)), block(kThreads);
-    hipLaunchKernelGGL((mx_tile_kernel<true, kPiecesX<XF, YF>, NT, YF>), grid(ub), block, 0, s, a, ub);
+    constexpr int NH = kPiecesH<YF>;
+    hipLaunchKernelGGL((mx_tile_kernel<true, kPiecesX<XF, YF>, NT, NH>), grid(ub), block, 0, s, a, ub);
     STMOE_LAUNCHED();
     if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
-    if (YF || L.tsplits > 1) {
-        hipLaunchKernelGGL((mx_tile_kernel<false, kPiecesH<YF>, NT, true>), grid(db), block, 0, s, a, db);
-        STMOE_LAUNCHED();
-        hipLaunchKernelGGL((mx_sum_kernel<true, YF>), sgrid, block, 0, s, a, sb);
-    } else {
-        hipLaunchKernelGGL((mx_tile_kernel<false, 1, NT, false>), grid(db), block, 0, s, a, db);
-        STMOE_LAUNCHED();
-        hipLaunchKernelGGL((mx_sum_kernel<false, false>), sgrid, block, 0, s, a, sb);
-    }
+    hipLaunchKernelGGL((mx_tile_kernel<false, NH, NT, NH>), grid(db), block, 0, s, a, db);
+    STMOE_LAUNCHED();
+    hipLaunchKernelGGL((mx_sum_kernel<YF>), sgrid, block, 0, s, a, sb);
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
@@ -1430,7 +1377,6 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
     a.smax = L.slots;
     a.split = reinterpret_cast<float*>(base + L.split);
     a.part = reinterpret_cast<float*>(base + L.part);
-    a.tscale = reinterpret_cast<float*>(base + L.tscale);
     a.n_experts = n_experts;
     const bool xf = dtype == STMOE_F32, yf = ydtype == STMOE_F32;
     if (T <= kMaxB) {
