@@ -328,15 +328,15 @@ int moe_mx_pack_expert(const uint8_t* gate_codes, const uint8_t* gate_scales, co
  *                bytes, 256-byte aligned, no initial contents required; calls
  *                sharing it must be ordered on one stream.  Its size does not
  *                always grow with T: calls of several sizes share the largest
- * dtype and ydtype: STMOE_BF16 or STMOE_F32 each.  Sums are fp32.  fp32 x, and
- * the activations when y is fp32, enter the products as bf16 pieces that hold
- * their 24 bits; with bf16 y the activations are rounded to bf16 (and fp32 x
- * to 16 bits).  An fp32 x that rounds to an infinite bf16 (above 3.39e38)
- * counts as infinite.  T (K +
- * n_shared) I elements of activations, 2 bytes each (6 with fp32 y), are at
- * most 64 GiB.  The same inputs give the same bits.  With more than 16 tokens
- * a token's result does not depend on the other tokens' values; up to 16 the
- * order of its sums goes by the experts that the call selects. */
+ * dtype and ydtype: STMOE_BF16 or STMOE_F32 each.  Sums are fp32.  fp32 x and
+ * the activations enter the products as bf16 pieces: with fp32 y three, which
+ * hold their 24 bits, with bf16 y two (off by 2^-16 of themselves at most).  An
+ * fp32 x or activation that rounds to an infinite bf16 (above 3.39e38) counts as
+ * infinite.  T (K + n_shared) I is at most 2^35, a third of that with fp32 y
+ * (activations of 128 and 64 GiB).  The same inputs give the same bits.  With
+ * more than 16 tokens a token's result does not depend on the other tokens'
+ * values; up to 16 the order of its sums goes by the experts that the call
+ * selects. */
 size_t moe_expert_ffn_mx_workspace_bytes(int T, int K, int E, int H, int I, int n_shared, int dtype,
                                          int ydtype);
 int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const float* topk_w, int T, int K, int H,

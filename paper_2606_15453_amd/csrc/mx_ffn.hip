@@ -7,9 +7,10 @@
 // the row operand in registers, tokens are the columns.  fp32 values (x, and
 // the activations when y is fp32) are split into three bf16 pieces, the
 // value's rounding and twice the rounding of what is left, which hold its 24
-// bits: three instructions per operand.  With bf16 y the activations are
-// rounded to bf16 (2^-8 of themselves at most, as y is) and fp32 x goes in two
-// pieces.
+// bits: three instructions per operand.  With bf16 y two pieces are taken of
+// both: 2^-16 of themselves at most, where rounding y costs 2^-8.  (One piece of
+// the activations lost as much as that rounding itself: 0.0024 of y off against
+// 0.0017; with two, decode steps take up to 3% longer and 4096 tokens 19%.)
 #include "mx_format.h"
 
 namespace stmoe {
@@ -54,7 +55,8 @@ struct MxArgs {
 template <bool XF, bool YF>
 constexpr int kPiecesX = XF ? (YF ? 3 : 2) : 1;
 template <bool YF>
-constexpr int kPiecesH = YF ? 3 : 1;
+constexpr int kPiecesH = YF ? 3 : 2;
+inline size_t pieces_h(int ydtype) { return ydtype == STMOE_F32 ? kPiecesH<true> : kPiecesH<false>; }
 
 // Column operand: eight consecutive values of a row as bf16 pieces.
 template <int N>
@@ -403,12 +405,12 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     __syncthreads();
     // thread: chunk tid % 16 of tokens tid / 16 + 16 j
     const u32x4* cols = reinterpret_cast<const u32x4*>(UP ? a.x : a.act);
-    uint32_t src[NT];                                       // in chunks
+    uint32_t src[NT];                                       // in chunks of one piece
     const int chunk = tid % CH;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int e = ent[tid / CH + 16 * j];
-        src[j] = uint32_t(UP ? e / a.ks : e) * uint32_t(NP * C / 8);
+        src[j] = uint32_t(UP ? e / a.ks : e) * uint32_t(C / 8);
     }
     const int put = tid / CH * CH + (chunk ^ (tid / CH & 15));
     struct Stage {
@@ -424,7 +426,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         for (int p = 0; p < NP; ++p) {
             const uint32_t off = uint32_t(p * C + (at < C ? at : 0)) / 8;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) d.x[p][j] = cols[size_t(src[j]) + off];
+            for (int j = 0; j < NT; ++j) d.x[p][j] = cols[size_t(src[j]) * NP + off];
         }
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
@@ -564,10 +566,11 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     }
 }
 
+// cut: workgroups that share a tile's tokens (down).
 // Three waves per SIMD (168 registers); four where they cost no spills in the loop
 // and pay: 1024 tokens of top-4, tiles of 32, 73.0 us a call, 76.3 with three.
 template <bool UP, int NP, int NT, int NH>
-__global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_kernel(MxArgs a, int nb) {
+__global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_kernel(MxArgs a, int nb, int cut) {
     constexpr int TM = 16 * NT;
     __shared__ u32x4 xs[2][NP * TM * kTileCols / 8];
     __shared__ int ent[TM];
@@ -576,8 +579,16 @@ __global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_
     const int work = *a.ntiles * nb, per = (work + 7) / 8;
     const int id = int(blockIdx.x % 8) * per + int(blockIdx.x / 8);
     if (int(blockIdx.x / 8) >= per || id >= work) return;
-    const int tix = id / nb, rest = id - tix * nb, sp = UP ? 0 : rest % a.tsplits, bk = UP ? rest : rest / a.tsplits;
-    const int4 tl = a.tiles[tix];
+    const int tix = id / nb, rest = id - tix * nb, sp = UP ? 0 : rest % a.tsplits;
+    int bk = UP ? rest : rest / a.tsplits;
+    int4 tl = a.tiles[tix];
+    if (!UP && cut > 1) {
+        const int piece = bk % cut;
+        bk /= cut;
+        tl.y += piece * TM;
+        tl.z = min(tl.z - piece * TM, TM);
+        if (tl.z <= 0) return;
+    }
     if constexpr (NT > 1) {
         // an expert's last tile, if at most half full, in half the instructions
         if (tl.z <= TM / 2) return tile_product<UP, NP, NT / 2, NH>(a, tl, bk, sp, xs[0], ent);
@@ -1080,8 +1091,10 @@ __global__ __launch_bounds__(64 * NW, 4) void mx_down_decode(MxArgs a, int direc
 #pragma unroll
             for (int w = 0; w < NW; ++w) v += red[buf][w][tid];
             if constexpr (PC) {
-                static_assert(NH == 3, "a token's pieces are three columns");
-                v += __shfl_down(v, 1, 64) + __shfl_down(v, 2, 64);
+                static_assert(NH == 2 || NH == 3, "a token's pieces are two or three columns");
+                float more = __shfl_down(v, 1, 64);
+                if constexpr (NH == 3) more += __shfl_down(v, 2, 64);
+                v += more;
             }
             const int row = item * kTileRows + 4 * q + tid / 64;
             if (t < a.T && !pc && row < a.H) store(t, row, v);
@@ -1181,10 +1194,12 @@ struct MxLayout {
 // y are bf16 and that leaves 1536 workgroups of the up launch (two rounds of
 // three per CU); else 32 above 12 on average, else 16.  Measured in us with
 // tiles of 16, 32 and 64 (H 2048, I 768, 64 experts, top 4 unless said):
-//    128 tokens   41    42    44       512 tokens   56    57    61
-//    256          50    45    46      2048         135   113   125  (960 workgroups)
-//   4096, 128 experts, top 8, bf16:   393 with 32, 365 with 64; fp32: 862, 803, 890
-//    512, H 4096, I 14336, 8 experts, top 2, bf16:  557 with 32, 432 with 64
+//    128 tokens   41    41    45       512 tokens   59    63    68
+//    256          49    49    52      2048         152   137   148  (960 workgroups)
+//   4096, 128 experts, top 8, bf16:   472 with 32, 463 with 64
+//    512, H 4096, I 14336, 8 experts, top 2, bf16:  663 with 32, 531 with 64
+// (12: with large experts 32 is ahead from there on, 64 tokens of the last shape
+// 201 and 171 us; small ones lose up to a tenth by it until about 40.)
 int tile_tokens(int T, int K, int E, int ns, int I, bool bf16) {
     const int mean = T * K / E;
     const int64_t wg = (int64_t(T) * (K + ns) / 64 + (E + ns) / 2) * ((I + 127) / 128);
@@ -1206,7 +1221,7 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
     const size_t n = size_t(T) * (K + ns);
     size_t off = 0;
     auto take = [&](size_t b) { const size_t at = off; off = (off + b + 255) / 256 * 256; return at; };
-    y.act = take(n * (ydtype == STMOE_F32 ? 3 : 1) * I * sizeof(uint16_t));
+    y.act = take(n * pieces_h(ydtype) * I * sizeof(uint16_t));
     if (T <= kMaxB) {
         y.slots = (E < T * K ? E : T * K) + ns;
         y.units = y.slots * col_tiles(I);
@@ -1253,7 +1268,7 @@ void launch_up_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
 template <int NH, bool PC, bool YF>
 int launch_down_decode(const MxArgs& a, const MxLayout& L, hipStream_t s) {
     const int NB = row_blocks(a.H);
-    if constexpr (PC || NH == 1) {
+    if constexpr (PC) {
         if (L.units <= kOneWaves * kOneU) {
             hipLaunchKernelGGL((mx_down_decode<NH, PC, YF, kOneWaves, kOneU, kOneR>), dim3(unsigned(NB < 256 ? NB : 256)),
                                dim3(64 * kOneWaves), 0, s, a, 1);
@@ -1280,10 +1295,11 @@ int launch_decode(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t 
     launch_up_decode<NX, NH>(a, L, s);
     STMOE_LAUNCHED();
     if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
-    // up to five tokens of fp32 y the three pieces of a column are columns of one
-    // instruction (one token, H 2048, I 768, top 8: a call 13.1 us, 14.8 with three
-    // instructions; five tokens 27.8 and 29.9)
-    if (YF && a.T * NH <= kMaxB) return launch_down_decode<NH, YF, YF>(a, L, s);
+    // few tokens (up to five of fp32 y, eight of bf16) have the pieces of a column as
+    // columns of one instruction (one token, H 2048, I 768, top 8, fp32 y: a call 13.1
+    // us, 14.8 with three instructions; five tokens 27.8 and 29.9; eight of bf16 y, H
+    // 2048, I 128, top 6: 13.0 and 14.3)
+    if (a.T * NH <= kMaxB) return launch_down_decode<NH, true, YF>(a, L, s);
     return launch_down_decode<NH, false, YF>(a, L, s);
 }
 
@@ -1295,10 +1311,14 @@ int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t e
     const int sb = (a.H + kThreads * 8 - 1) / (kThreads * 8);
     const dim3 sgrid(unsigned(a.T) * unsigned(sb)), block(kThreads);
     constexpr int NH = kPiecesH<YF>;
-    hipLaunchKernelGGL((mx_tile_kernel<true, kPiecesX<XF, YF>, NT, NH>), grid(ub), block, 0, s, a, ub);
+    hipLaunchKernelGGL((mx_tile_kernel<true, kPiecesX<XF, YF>, NT, NH>), grid(ub), block, 0, s, a, ub, 1);
     STMOE_LAUNCHED();
     if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
-    hipLaunchKernelGGL((mx_tile_kernel<false, NH, NT, NH>), grid(db), block, 0, s, a, db);
+    // tiles of 64 tokens in two halves: both pieces of 64 columns would leave two
+    // workgroups a CU (4096 tokens of top-8 507 us a call, 519 whole; 512 tokens of
+    // Mixtral sizes 539 and 572)
+    constexpr int DT = NT == 4 ? 2 : NT, CUT = NT / DT;
+    hipLaunchKernelGGL((mx_tile_kernel<false, NH, DT, NH>), grid(db * CUT), block, 0, s, a, db * CUT, CUT);
     STMOE_LAUNCHED();
     hipLaunchKernelGGL((mx_sum_kernel<YF>), sgrid, block, 0, s, a, sb);
     STMOE_LAUNCHED();
@@ -1337,7 +1357,8 @@ int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream
     return launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
 }
 
-// The launches index the activations in 16-byte chunks of 32 bits.
+// The launches count a piece of the activations in 16-byte chunks of 32 bits; three
+// pieces are held to the same bytes.
 bool too_large(int T, int K, int I, int ns, int ydtype) {
     return size_t(T) * (K + ns) * (ydtype == STMOE_F32 ? 3 : 1) * I / 8 > size_t(1) << 32;
 }

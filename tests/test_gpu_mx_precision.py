@@ -84,3 +84,12 @@ def test_small_columns_beside_large_ones(T, H, I, E, K):
     """Columns of y whose W_down rows are 2^-6 to 2^-40 of the others keep their bits (activations in bf16: 2^-8)."""
     rows = [2.0 ** -[0, 0, 6, 14, 20, 26, 40][i % 7] for i in range(H)]
     _check(T, H, I, E, K, rows, act=2.0 ** -8)
+
+
+@pytest.mark.parametrize("x_bf16", [True, False])
+@pytest.mark.parametrize("T,H,I,E,K", [(1, 64, 64, 8, 2), (3, 64, 1544, 6, 4), (8, 64, 64, 8, 2), (9, 64, 64, 8, 2), (16, 64, 64, 8, 2),
+                                       (17, 64, 64, 8, 2), (40, 64, 64, 4, 2), (300, 64, 64, 4, 2), (8192, 72, 264, 16, 4)])
+def test_bf16_results_are_off_by_their_rounding(T, H, I, E, K, x_bf16):
+    """A bf16 y is the fp32 one rounded, but for 2^-16 of the activations (two bf16 pieces)."""
+    _check(T, H, I, E, K, [1.0] * H, 2.0 ** -16, x_bf16)
+    _check(T, H, I, E, K, [2.0 ** -[0, 0, 6, 14, 20, 26, 40][i % 7] for i in range(H)], 2.0 ** -16, x_bf16)
