@@ -278,6 +278,15 @@ def _dense(name, t, shape, dtypes, dev):
     raise ValueError(f"{name} must be a contiguous {list(shape)} tensor, not {list(t.shape)}")
 
 
+def _workspace(ws, dev):
+    """Pointer and bytes of a workspace: contiguous device memory (alignment and size are the library's to check)."""
+    if ws is None or ws.get_device() != dev:
+        raise ValueError("ws must be on the current CUDA device")
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    return ws.data_ptr(), ws.nbytes
+
+
 def _rows(name, t):
     """(rows, columns, row stride) of a matrix whose rows are contiguous and do not overlap."""
     if t.dim() != 2:
@@ -316,7 +325,7 @@ def route_balance(logits, K, idx, w, counts, n_tokens, loss, ws, renorm=False, m
         _dense("mask", mask, (T,), (torch.uint8, torch.bool), dev)
     _call("moe_route_balance", logits.data_ptr(), T, ld, E, K, _dt("logits", logits), int(renorm), _p(mask),
           idx.data_ptr(), w.data_ptr(), counts.data_ptr(), n_tokens.data_ptr(), _p(prob_sum), loss.data_ptr(),
-          ws.data_ptr(), ws.nbytes, _s(stream))
+          *_workspace(ws, dev), _s(stream))
 
 
 def route_balance_backward(logits, idx, counts, n_tokens, d_loss, d_logits, d_w=None, renorm=False, stream=None):
@@ -479,7 +488,7 @@ def expert_ffn_mx(x, idx, w, H, I, E, expert_ptrs, y, ws, shared_ptrs=None, n_sh
     if n_shared:
         _dense("shared_ptrs", shared_ptrs, (n_shared,), (torch.int64,), dev)
     _call("moe_expert_ffn_mx", x.data_ptr(), idx.data_ptr(), w.data_ptr(), T, K, H, I, E, _DTYPES[x.dtype],
-          _DTYPES[y.dtype], expert_ptrs.data_ptr(), _p(shared_ptrs), n_shared, y.data_ptr(), ws.data_ptr(), ws.nbytes,
+          _DTYPES[y.dtype], expert_ptrs.data_ptr(), _p(shared_ptrs), n_shared, y.data_ptr(), *_workspace(ws, dev),
           _s(stream))
 
 

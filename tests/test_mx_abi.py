@@ -148,3 +148,59 @@ def test_plain_losses_by_hand():
     f = mxref.balance(z, 1)
     assert f["counts"].tolist() == [2, 0] and f["n"] == 2
     assert np.allclose(f["loss"], [1.5, np.log(4) ** 2], rtol=1e-14)
+
+
+class _OnCard:
+    """A tensor as the binding sees it: what its checks ask for, and an address."""
+
+    def __init__(self, shape, dtype, device=0, step=1):
+        import torch
+        self.shape, self.dtype, self.device, self.step = torch.Size(shape), dtype, device, step
+        self.nbytes = torch.empty(0, dtype=dtype).element_size() * self.shape.numel()
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return self.step == 1
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return tuple(self.shape[i + 1:].numel() * self.step for i in range(len(self.shape)))
+
+    def data_ptr(self):
+        return 4096
+
+    def numel(self):
+        return self.shape.numel()
+
+
+@pytest.mark.parametrize("ws", [dict(device=-1), dict(device=1), dict(step=2), None])
+def test_binding_refuses_workspaces_it_would_misread(monkeypatch, ws):
+    """A workspace in host memory, on another GPU, with gaps between its elements, or none: no call goes to the library."""
+    import torch
+    calls = []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(S, "_call", lambda name, *a: calls.append(name))
+    monkeypatch.setattr(S, "_s", lambda stream: None)
+    f, i, b = torch.float32, torch.int32, torch.bfloat16
+    T, E, K, H, I = 4, 8, 2, 64, 64
+
+    def run(w):
+        S.route_balance(_OnCard((T, E), f), K, _OnCard((T, K), i), _OnCard((T, K), f), _OnCard((E,), i), _OnCard((1,), i),
+                        _OnCard((2,), f), w)
+
+    def ffn(w):
+        S.expert_ffn_mx(_OnCard((T, H), b), _OnCard((T, K), i), _OnCard((T, K), f), H, I, E, _OnCard((E,), torch.int64),
+                        _OnCard((T, H), f), w)
+
+    good = _OnCard((1 << 20,), torch.uint8)
+    run(good), ffn(good)
+    assert calls == ["moe_route_balance", "moe_expert_ffn_mx"]
+    bad = None if ws is None else _OnCard((1 << 20,), torch.uint8, **ws)
+    for call in (run, ffn):
+        with pytest.raises(ValueError):
+            call(bad)
+    assert len(calls) == 2
