@@ -417,9 +417,8 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         u32x4 x[NP][NT], w[RB];
         uint32_t s[RB];
     } st[2];
-    // Chunks beyond the row's end read its first one: their codes are zero, and
-    // if the row holds a NaN or an infinity its results are not finite without
-    // it too.
+    // Chunks beyond the row's end read its first one and are kept as zeros: their
+    // codes are zero, but that times an infinity is NaN.
     auto load = [&](Stage& d, int kt) __attribute__((always_inline)) {
         const int at = kt * kTileCols + chunk * 8;
 #pragma unroll
@@ -441,10 +440,11 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
         for (int n = 0; n < NT; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int c = int(lane & 15), q = int(lane >> 4);
     auto keep = [&](const Stage& d, int kt) __attribute__((always_inline)) {
+        const uint32_t in = kt * kTileCols + chunk * 8 < C ? ~0u : 0u;
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xs[(kt & 1) * SZ + p * TM * CH + put + j * 16 * CH] = d.x[p][j];
+            for (int j = 0; j < NT; ++j) xs[(kt & 1) * SZ + p * TM * CH + put + j * 16 * CH] = d.x[p][j] & in;
     };
     auto multiply = [&](const u32x4 (&w)[RB], const uint32_t (&scales)[RB], int kt) __attribute__((always_inline)) {
         const u32x4* buf = xs + (kt & 1) * SZ + c * CH;

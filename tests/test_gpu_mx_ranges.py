@@ -1,0 +1,57 @@
+"""GPU: the 4-bit expert FFN at the ends of its ranges: infinite results, the widths of hidden states that its
+decode kernels divide among waves, offsets beyond 32 bits.  Tolerances as in test_gpu_mx."""
+import numpy as np
+import pytest
+
+from test_gpu_mx import DEV, _run
+
+pytestmark = pytest.mark.gpu
+
+
+def _pack(H, I, gate, up, down):
+    """A blob of matrices of the values 0, 1 and -1 (scale 1)."""
+    import torch
+    from paper_2606_15453_amd import stmoe as S
+    mats = []
+    for m in (gate, up, down):
+        c = torch.where(m == 0, 0, torch.where(m > 0, 2, 10)).to(torch.uint8)
+        codes = (c[:, 0::2] | (c[:, 1::2] << 4)).contiguous().to(DEV)
+        mats.append((codes, torch.full((m.shape[0], (m.shape[1] + 31) // 32), 127, dtype=torch.uint8, device=DEV)))
+    blob = torch.empty(S.blob_bytes(H, I, S.MXFP4), dtype=torch.uint8, device=DEV)
+    S.mx_pack_expert(*mats, H, I, blob)
+    return blob
+
+
+@pytest.mark.parametrize("x_bf16,y_bf16", [(True, False), (True, True), (False, False), (False, True)])
+@pytest.mark.parametrize("T,E,K", [(1, 4, 2), (5, 4, 2), (16, 4, 2), (17, 4, 2), (40, 4, 2), (300, 4, 2), (8192, 16, 4)])
+@pytest.mark.parametrize("H,I", [(72, 264), (136, 328)])
+def test_infinite_results(H, I, T, E, K, x_bf16, y_bf16):
+    """An infinity among the first hidden states or activations times weights that are not zero there is an infinite
+    result, whatever lies behind the last column."""
+    import torch
+
+    class Same:
+        pass
+
+    xd, yd = (torch.bfloat16 if b else torch.float32 for b in (x_bf16, y_bf16))
+    rng = np.random.default_rng(T)
+    idx = torch.from_numpy(np.stack([rng.choice(E, K, replace=False) for _ in range(T)]).astype(np.int32)).to(DEV)
+    w = torch.full((T, K), 0.5, device=DEV)
+    sign = torch.from_numpy(rng.choice([-1, 1], H))
+    # x[0] infinite: all gate and up sums are plus infinity, and so is every activation
+    gate = torch.zeros((I, H), dtype=torch.int64)
+    gate[:, 0] = 1
+    down = sign[:, None].expand(H, I)
+    # x[0] = 2^65: activation 0 is 2^130, beyond fp32, the others are 0
+    one = torch.zeros((I, H), dtype=torch.int64)
+    one[0, 0] = 1
+    first = torch.zeros((H, I), dtype=torch.int64)
+    first[:, 0] = sign
+    for x0, mats in ((float("inf"), (gate, gate, down)), (2.0 ** 65, (one, one, first))):
+        ex = Same()
+        blob = _pack(H, I, *mats)
+        ex.ptrs = torch.full((E,), blob.data_ptr(), dtype=torch.int64, device=DEV)
+        x = torch.ones((T, H), device=DEV)
+        x[:, 0] = x0
+        y = _run(ex, E, H, I, x.to(xd), idx, w, yd)
+        assert torch.equal(y.float(), (sign * float("inf")).float().to(DEV).expand(T, H)), x0
