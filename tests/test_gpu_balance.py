@@ -271,3 +271,20 @@ def test_layer_of_a_training_batch():
     d_w = d_w.astype(np.float32).astype(np.float64)
     got = _check_backward(z, f, d_w, [0.01, 0.001], True)
     assert not got[140:].any()
+
+
+@pytest.mark.parametrize("T,E,dtype", [(2 ** 26, 3, "bfloat16"), (2 ** 24, 61, "bfloat16"), (2 ** 24, 61, "float32"),
+                                       (2 ** 24, 124, "bfloat16"), (2 ** 24, 200, "bfloat16")])
+def test_sums_of_the_largest_batches(T, E, dtype):
+    """Rows of equal logits, as a fresh router gives them, whose rounding errors do not cancel.  In half steps of 2^-24:
+    a row's probability is off by two, a chain of 32 rows, four rows side by side and 16 waves by 49 more, a product
+    and the last rounding by two; the logarithm's square by eight."""
+    import torch
+    K = 2
+    z = torch.zeros((T, E), dtype=getattr(torch, dtype), device=DEV)
+    o = _forward(z, K)
+    u = 2.0 ** -24
+    np.testing.assert_allclose(_f64(o["prob_sum"]), np.full(E, T / E), rtol=53 * u)
+    loss = _f64(o["loss"])
+    assert abs(loss[0] - 1) <= 53 * u and abs(loss[1] / np.log(E) ** 2 - 1) <= 59 * u
+    assert o["counts"].tolist() == [T, T] + [0] * (E - 2) and int(o["n"]) == T
