@@ -326,8 +326,8 @@ int moe_mx_pack_expert(const uint8_t* gate_codes, const uint8_t* gate_scales, co
  *   y            device out [T][H] ydtype, 16-byte aligned
  *   ws           device workspace of moe_expert_ffn_mx_workspace_bytes(...)
  *                bytes, 256-byte aligned, no initial contents required; calls
- *                sharing it must be ordered on one stream.  Its size does not
- *                always grow with T: calls of several sizes share the largest
+ *                sharing it must be ordered on one stream.  Its size never
+ *                falls as T grows: one for many tokens serves fewer
  * dtype and ydtype: STMOE_BF16 or STMOE_F32 each.  Sums are fp32.  fp32 x and
  * the activations enter the products as bf16 pieces: with fp32 y three, which
  * hold their 24 bits, with bf16 y two (off by 2^-16 of themselves at most).  An

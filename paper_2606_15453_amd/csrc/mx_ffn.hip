@@ -1210,12 +1210,26 @@ int tile_tokens(int T, int K, int E, int ns, int I, bool bf16) {
 // CU) if half of the experts' last tiles are filled, of four column tiles at
 // least (32 tokens, H 1024, I 8192, 8 experts: 84 us unsplit, 48 split; 20
 // tokens, H 2048, I 1408, 16 experts: 37 and 34).
+constexpr size_t kDownWgs = 768;
+int most_splits(int I) { return col_tiles(I) < 8 ? 1 : col_tiles(I) / 4; }
 int tile_splits(int tm, size_t n, int E, int ns, int H, int I) {
     const size_t wg = (n / tm + (E + ns) / 2 + 1) * size_t((H + 255) / 256);
-    const int want = wg >= 768 ? 1 : int(768 / wg), most = col_tiles(I) / 4;
-    return want < 1 ? 1 : most < 1 ? 1 : want < most ? want : most;
+    const int want = wg >= kDownWgs ? 1 : int(kDownWgs / wg), most = most_splits(I);
+    return want < most ? want : most;
 }
 
+// Rows of terms for n entries: n times tile_splits, or what fewer entries in more
+// parts need.  With floor(n / tm) >= (n + 1) / tm - 1 the parts are at most
+// 768 tm / ((n + 1 + (E + ns) / 2 tm) H / 256), and that times n grows with n.
+size_t term_rows(int tm, size_t n, int E, int ns, int H, int I) {
+    const size_t den = (n + 1 + size_t((E + ns) / 2) * tm) * size_t((H + 255) / 256);
+    const size_t parts = (kDownWgs * tm * n + den - 1) / den, most = n * most_splits(I);
+    return parts < n ? n : parts < most ? parts : most;
+}
+
+// Its bytes grow with T (a workspace for many tokens serves fewer): a prompt's are
+// those of 16 tokens at least, and its parts are sized for the largest number of
+// tokens up to T that needs most.
 MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydtype) {
     MxLayout y{};
     const size_t n = size_t(T) * (K + ns);
@@ -1236,13 +1250,15 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
         y.max_tiles = int(most < n ? most : n);
         y.order = take(size_t(E + ns) * T * sizeof(int32_t));
         y.cnt = take(size_t(E + ns) * sizeof(int32_t));
-        y.tiles = take(size_t(y.max_tiles) * sizeof(int4));
+        const size_t small = n / 16 + E + ns;               // tiles of 16 tokens
+        y.tiles = take((small < n ? small : n) * sizeof(int4));
         y.ntiles = take(sizeof(int32_t));
         y.tsplits = tile_splits(y.tm, n, E, ns, H, I);
-        y.part = take(n * y.tsplits * H * sizeof(float));
+        y.part = take(term_rows(y.tm, n, E, ns, H, I) * H * sizeof(float));
         if (dtype == STMOE_F32) y.xs = take(size_t(T) * H * (ydtype == STMOE_F32 ? 3 : 2) * sizeof(uint16_t));
     }
-    y.total = off;
+    const size_t step = T <= kMaxB ? 0 : mx_layout(kMaxB, K, E, H, I, ns, dtype, ydtype).total;
+    y.total = off > step ? off : step;
     return y;
 }
 

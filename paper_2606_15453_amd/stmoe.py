@@ -472,7 +472,7 @@ def mx_pack_expert(gate, up, down, H, I, blob, stream=None):
 
 
 def ffn_mx_workspace_bytes(T, K, E, H, I, n_shared=0, dtype=torch.bfloat16, y_dtype=torch.float32):
-    """Workspace bytes for expert_ffn_mx (256-byte aligned; not always more for a larger T); 0 for an invalid shape."""
+    """Workspace bytes for expert_ffn_mx (256-byte aligned; never less for a larger T); 0 for an invalid shape."""
     return _lib.moe_expert_ffn_mx_workspace_bytes(T, K, E, H, I, n_shared, _DTYPES[dtype], _DTYPES[y_dtype])
 
 

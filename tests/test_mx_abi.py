@@ -204,3 +204,23 @@ def test_binding_refuses_workspaces_it_would_misread(monkeypatch, ws):
         with pytest.raises(ValueError):
             call(bad)
     assert len(calls) == 2
+
+
+@pytest.mark.parametrize("xd", [S.BF16, S.F32])
+@pytest.mark.parametrize("yd", [S.BF16, S.F32])
+@pytest.mark.parametrize("K,E,H,I,ns", [(2, 8, 4096, 14336, 0), (8, 128, 2048, 768, 0), (6, 64, 2048, 1408, 2), (3, 13, 1000, 520, 1),
+                                        (1, 1, 8, 8, 0), (16, 16, 16384, 64, 8), (1, 256, 256, 65536, 0), (2, 4, 64, 8192, 0)])
+def test_a_workspace_for_many_tokens_serves_fewer(K, E, H, I, ns, xd, yd):
+    n = L.moe_expert_ffn_mx_workspace_bytes
+    rng = np.random.default_rng(K * E)
+    sizes = sorted(set(range(0, 1100)) | set(rng.integers(1100, 65537, 3000).tolist()) | {65536})
+    last = 0
+    for T in sizes:
+        b = n(T, K, E, H, I, ns, xd, yd)
+        if b == 0:      # beyond the bound on the activations, which only larger batches are
+            assert T * (K + ns) * I > 2 ** 35 // 3
+            break
+        assert b >= last, T
+        last = b
+    # not by far more than what the call writes: activations, terms in up to 64 parts of the contraction, x in pieces
+    assert n(64, 2, 8, 4096, 14336, 0, xd, yd) <= 64 << 20
