@@ -3,7 +3,8 @@ decode kernels divide among waves, offsets beyond 32 bits.  Tolerances as in tes
 import numpy as np
 import pytest
 
-from test_gpu_mx import DEV, _run
+import mxref
+from test_gpu_mx import DEV, Experts, _err, _f64, _inputs, _run, _tol
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +56,29 @@ def test_infinite_results(H, I, T, E, K, x_bf16, y_bf16):
         x[:, 0] = x0
         y = _run(ex, E, H, I, x.to(xd), idx, w, yd)
         assert torch.equal(y.float(), (sign * float("inf")).float().to(DEV).expand(T, H)), x0
+
+
+def _parity(T, H, I, E, K, x_bf16, y_bf16, pick=None, seed=0):
+    import torch
+    xd, yd = (torch.bfloat16 if b else torch.float32 for b in (x_bf16, y_bf16))
+    ex = Experts(E, H, I, T + H)
+    x, idx, w = _inputs(T, K, E, H, seed, xd)
+    y = _run(ex, E, H, I, x, idx, w, yd)
+    pick = np.arange(T) if pick is None else pick
+    want = mxref.moe_ffn(_f64(x[pick]), idx.cpu().numpy()[pick], _f64(w[pick]), ex.values)
+    assert _err(y[pick], want) <= _tol(x_bf16, y_bf16)
+    assert bool(y.isfinite().all())
+
+
+@pytest.mark.parametrize("y_bf16", [False, True])
+@pytest.mark.parametrize("H,I", [(4096, 64), (64, 4096)])
+def test_terms_and_activations_beyond_32_bit_offsets(H, I, y_bf16):
+    """More than 2^31 terms (H) or activations (I), which pass 4 GiB in two bytes each: tokens of both ends and around
+    the offsets 2^31 and 2^32."""
+    T, E, K = 65536, 9, 9
+    n = T * K * max(H, I)
+    assert n > 2 ** 31 and 2 * n > 2 ** 32
+    edge = [(1 << b) // (K * max(H, I) * size) for b in (31, 32, 33) for size in (1, 2, 4)]
+    pick = np.unique(np.concatenate([np.arange(16), np.arange(T - 16, T)] +
+                                    [np.arange(max(0, e - 4), min(T, e + 4)) for e in edge]))
+    _parity(T, H, I, E, K, True, y_bf16, pick=pick)
