@@ -71,6 +71,22 @@ def _parity(T, H, I, E, K, x_bf16, y_bf16, pick=None, seed=0):
 
 
 @pytest.mark.parametrize("y_bf16", [False, True])
+@pytest.mark.parametrize("H", [2048, 2056, 3000, 3584, 4096])
+@pytest.mark.parametrize("T", [2, 7, 16])
+def test_decode_steps_of_wide_hidden_states(T, H, y_bf16):
+    """bf16 hidden states of 17 to 32 column tiles (and 16, where the waves are half as many), whose last waves have few
+    columns or none: H 2056 leaves three waves of eight without, 3000 two, 3584 one."""
+    _parity(T, H, 136, 9, 3, True, y_bf16, seed=H)
+
+
+@pytest.mark.parametrize("x_bf16,y_bf16", [(True, False), (True, True), (False, False), (False, True)])
+@pytest.mark.parametrize("T,H", [(16, 4104), (16, 7168), (7, 5120), (2, 16384)])
+def test_decode_steps_of_more_column_tiles(T, H, x_bf16, y_bf16):
+    """Hidden states beyond 32 column tiles, and fp32 ones."""
+    _parity(T, H, 136, 9, 3, x_bf16, y_bf16, seed=H)
+
+
+@pytest.mark.parametrize("y_bf16", [False, True])
 @pytest.mark.parametrize("H,I", [(4096, 64), (64, 4096)])
 def test_terms_and_activations_beyond_32_bit_offsets(H, I, y_bf16):
     """More than 2^31 terms (H) or activations (I), which pass 4 GiB in two bytes each: tokens of both ends and around
