@@ -139,11 +139,10 @@ __device__ __forceinline__ void list_tiles(const MxArgs& a, const int* cnt, int*
     const int tid = threadIdx.x, G = a.E + a.ns;
     if (tid < 64) {
         // running sums of the tile counts, 64 experts at a time
-        int before = 0, used = 0;
+        int before = 0;
         for (int g0 = 0; g0 < G; g0 += 64) {
             const int g = g0 + tid, c = g < G ? cnt[g] : 0;
             int v = (c + a.tm - 1) / a.tm;
-            used += __popcll(__ballot(c > 0 && g < a.E));
             for (int d = 1; d < 64; d <<= 1) {
                 const int o = __shfl_up(v, d, 64);
                 if (tid >= d) v += o;
@@ -154,7 +153,6 @@ __device__ __forceinline__ void list_tiles(const MxArgs& a, const int* cnt, int*
         if (tid == 0) {
             tile[0] = 0;
             *a.ntiles = before;
-            if (a.n_experts) *a.n_experts += (unsigned long long)(used);
         }
     }
     __syncthreads();
@@ -1086,16 +1084,14 @@ __global__ __launch_bounds__(64 * NW, 4) void mx_down_decode(MxArgs a, int direc
         };
         if constexpr (U > 1) {
             // one row block, a thread per row and column
+            static_assert(PC && (NH == 2 || NH == 3), "a token's pieces are two or three columns");
             if (tid >= OUT) return;
             float v = 0.f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) v += red[buf][w][tid];
-            if constexpr (PC) {
-                static_assert(NH == 2 || NH == 3, "a token's pieces are two or three columns");
-                float more = __shfl_down(v, 1, 64);
-                if constexpr (NH == 3) more += __shfl_down(v, 2, 64);
-                v += more;
-            }
+            float more = __shfl_down(v, 1, 64);
+            if constexpr (NH == 3) more += __shfl_down(v, 2, 64);
+            v += more;
             const int row = item * kTileRows + 4 * q + tid / 64;
             if (t < a.T && !pc && row < a.H) store(t, row, v);
             return;
@@ -1320,7 +1316,7 @@ int launch_decode(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t 
 }
 
 template <bool XF, bool YF, int NT>
-int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t ev_mid) {
+int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s) {
     // rounded up to the eight XCDs
     const auto grid = [&](int nb) { return dim3(unsigned((int64_t(L.max_tiles) * nb + 7) / 8 * 8)); };
     const int ub = (a.I + 127) / 128, db = (a.H + 255) / 256 * L.tsplits;
@@ -1329,7 +1325,6 @@ int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t e
     constexpr int NH = kPiecesH<YF>;
     hipLaunchKernelGGL((mx_tile_kernel<true, kPiecesX<XF, YF>, NT, NH>), grid(ub), block, 0, s, a, ub, 1);
     STMOE_LAUNCHED();
-    if (ev_mid) STMOE_HIP(hipEventRecord(ev_mid, s));
     // tiles of 64 tokens in two halves: both pieces of 64 columns would leave two
     // workgroups a CU (4096 tokens of top-8 507 us a call, 519 whole; 512 tokens of
     // Mixtral sizes 539 and 572)
@@ -1342,7 +1337,7 @@ int launch_tiles(const MxArgs& a, const MxLayout& L, hipStream_t s, hipEvent_t e
 }
 
 template <bool XF, bool YF>
-int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream_t s, hipEvent_t ev_mid) {
+int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream_t s) {
     MxArgs a = args;
     const dim3 block(kPlanThreads);
     if (a.T * a.K <= kPlanEntries) {
@@ -1367,10 +1362,10 @@ int launch_prompt(const MxArgs& args, const MxLayout& L, uint16_t* xs, hipStream
         a.x = xs;
     }
     if constexpr (!XF && !YF) {
-        if (L.tm == 64) return launch_tiles<XF, YF, 4>(a, L, s, ev_mid);
+        if (L.tm == 64) return launch_tiles<XF, YF, 4>(a, L, s);
     }
-    if (L.tm == 32) return launch_tiles<XF, YF, 2>(a, L, s, ev_mid);
-    return launch_tiles<XF, YF, 1>(a, L, s, ev_mid);
+    if (L.tm == 32) return launch_tiles<XF, YF, 2>(a, L, s);
+    return launch_tiles<XF, YF, 1>(a, L, s);
 }
 
 // The launches count a piece of the activations in 16-byte chunks of 32 bits; three
@@ -1382,7 +1377,8 @@ bool too_large(int T, int K, int I, int ns, int ydtype) {
 }  // namespace
 
 // Internal entry of the decode-layer orchestration too (no argument checks).
-// `ev_mid` is recorded between the gate/up and the down work.
+// `n_experts` and `ev_mid` (recorded between the gate/up and the down work) are for
+// decode steps, T <= kMaxB; a prompt ignores them.
 int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int K, int H, int I, int E, int dtype,
                   int ydtype, const void* const* eptr, const void* const* sptr, int n_shared, void* y, void* ws,
                   hipStream_t s, unsigned long long* n_experts, hipEvent_t ev_mid) {
@@ -1421,8 +1417,8 @@ int mx_ffn_launch(const void* x, const int32_t* idx, const float* w, int T, int 
         return yf ? launch_decode<false, true>(a, L, s, ev_mid) : launch_decode<false, false>(a, L, s, ev_mid);
     }
     uint16_t* xs = reinterpret_cast<uint16_t*>(base + L.xs);
-    if (xf) return yf ? launch_prompt<true, true>(a, L, xs, s, ev_mid) : launch_prompt<true, false>(a, L, xs, s, ev_mid);
-    return yf ? launch_prompt<false, true>(a, L, xs, s, ev_mid) : launch_prompt<false, false>(a, L, xs, s, ev_mid);
+    if (xf) return yf ? launch_prompt<true, true>(a, L, xs, s) : launch_prompt<true, false>(a, L, xs, s);
+    return yf ? launch_prompt<false, true>(a, L, xs, s) : launch_prompt<false, false>(a, L, xs, s);
 }
 
 }  // namespace stmoe
