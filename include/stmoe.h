@@ -186,7 +186,7 @@ int stmoe_stats(stmoe_predictor* p, int64_t* out);
  * not zero and that have a logit above minus infinity.  A logit of minus
  * infinity is no candidate and has probability 0; the type's lowest value is
  * a number like others.  A NaN ranks below every number and makes its row's
- * weights and the losses NaN.
+ * weights and the losses NaN, as plus infinity does.
  *
  *   logits   device [T] rows of E values, row stride ld elements, dtype
  *   mask     device [T] uint8, or NULL: every token counts
@@ -213,7 +213,10 @@ int moe_route_balance(const void* logits, int64_t T, int64_t ld, int E, int K, i
  * topk_idx, counts and n_tokens as moe_route_balance took and gave them (the
  * counts and n_tokens may be summed over ranks); rows whose first topk_idx is
  * negative get zeros.
- *   d_w      device [T][K] fp32, or NULL (zeros)
+ *   d_w      device [T][K] fp32, or NULL (zeros).  For experts' outputs weighted
+ *            and summed to y it is dy[t] . (output of expert topk_idx[t][k]);
+ *            moe_expert_ffn_mx over column k of the selection with weights of
+ *            one gives those outputs
  *   d_loss   device [2] fp32
  *   d_logits device out [T] rows of E values, row stride ld_d, dtype; may be
  *            logits itself when ld_d = ld */
@@ -295,7 +298,8 @@ int moe_expert_ffn_noalloc(const void* x, const int32_t* topk_idx, const float* 
  * magnitude, divided by 4 (at least 2^-127), and rounds every value / scale to
  * the nearest magnitude, ties to the even code, at most 6.  A block that holds
  * an infinity or a NaN gets the scale byte 255 and codes 0: its values read
- * back as NaN.  Every value read back is exact in both dtypes.
+ * back as NaN.  Every value read back is exact in both dtypes (infinite where a
+ * scale byte of 253 or 254, which quantising does not give, takes it beyond them).
  *   x, y   device, dtype, row stride ld elements (>= cols)
  *   rows   0 <= rows <= 2^31 (0: nothing is done); 1 <= cols <= 2^30
  * ---------------------------------------------------------------------- */

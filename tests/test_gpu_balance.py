@@ -288,3 +288,38 @@ def test_sums_of_the_largest_batches(T, E, dtype):
     loss = _f64(o["loss"])
     assert abs(loss[0] - 1) <= 53 * u and abs(loss[1] / np.log(E) ** 2 - 1) <= 59 * u
     assert o["counts"].tolist() == [T, T] + [0] * (E - 2) and int(o["n"]) == T
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("T", [12, 150])
+def test_router_gradient_from_the_experts_own_outputs(T, renorm):
+    """A gate weight's gradient is dy . (its expert's own output), and expert_ffn_mx over one column of the selection
+    with weights of one gives those outputs: the router's gradient from the library's own calls alone, against 64 bits.
+    A column's outputs are off by 2e-5 of their norm and the fp32 product of H terms by H 2^-24 of theirs; a row of the
+    gradient takes at most twice the largest of its K errors."""
+    import torch
+    from test_gpu_mx import Experts, _run
+    H, I, E, K = 256, 136, 12, 3
+    ex = Experts(E, H, I, 1)
+    g = torch.Generator(device=DEV).manual_seed(T)
+    x = torch.randn((T, H), generator=g, device=DEV).to(torch.bfloat16)
+    z = x.float() @ torch.randn((H, E), generator=g, device=DEV) * H ** -0.5
+    r = torch.randn((T, H), generator=g, device=DEV)
+    mask = torch.ones(T, dtype=torch.uint8, device=DEV)
+    mask[-2:] = 0
+    o, f = _check_forward(z, K, renorm, mask)
+    ones = torch.ones((T, 1), device=DEV)
+    d_w = torch.stack([(_run(ex, E, H, I, x, o["idx"][:, k:k + 1].contiguous(), ones, torch.float32) * r).sum(dim=1)
+                       for k in range(K)], dim=1)
+    want_w, off = np.zeros((T, K)), np.zeros((T, K))
+    for k in range(K):
+        out = mxref.moe_ffn(_f64(x), f["idx"][:, k:k + 1], np.ones((T, 1)), ex.values)
+        want_w[:, k] = (out * _f64(r)).sum(axis=1)
+        off[:, k] = (2e-5 + H * 2.0 ** -24) * np.linalg.norm(out, axis=1) * np.linalg.norm(_f64(r), axis=1)
+    assert (np.abs(_f64(d_w) - want_w) <= off).all()
+    d_loss = [0.01, 0.001]
+    got = _f64(_backward(z, f, _f64(d_w), d_loss, renorm))
+    want = mxref.balance_grad(_f64(z), f["idx"], f["counts"], f["n"], want_w, np.float32(d_loss).astype(np.float64), renorm)
+    big = np.abs(want_w).max(axis=1) + d_loss[0] * E + 2 * d_loss[1] * np.abs(f["lse"])
+    assert (np.abs(got - want) <= (2 * off.max(axis=1) + 1e-5 * 2 * big)[:, None]).all()
+    assert not got[-2:].any() and np.abs(got).max() > 1e-3
