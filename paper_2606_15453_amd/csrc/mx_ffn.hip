@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kPlanThreads) void mx_tiles_kernel(MxArgs a) {
 // they are loaded four at a time) and takes the first that names the expert;
 // a wave's place is its lanes' ballot, the waves' places meet in LDS.  Bound by
 // the latency of its barriers, 1024 tokens after another, the next ones' entries
-// on their way: 5.0 us for 4096 tokens and 128 experts.
+// on their way: 5.4 us for 4096 tokens and 128 experts.
 template <int KU, bool FOUR>
 __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
     constexpr int W = kPlanThreads / 64;
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kPlanThreads) void mx_order_kernel(MxArgs a) {
 
 // All experts' entries and the tiles by one workgroup, a thread per token, for at
 // most kPlanEntries entries: it saves a launch (whole calls against the two
-// launches above: 20 tokens of top-2 15.9 and 16.9 us, 37 of top-3 26.4 and 27.1;
+// launches above: 20 tokens of top-2 16.2 and 16.8 us, 37 of top-3 27.4 and 28.0;
 // beyond 300 entries it no longer did).  An expert's tokens are bits of a mask in
 // LDS, a token's place the number of bits below its own; a bit that its thread
 // finds set is a repeated expert.  The KU entries are handled side by side,
@@ -341,8 +341,8 @@ __device__ __forceinline__ BlobRef expert_blob(const MxArgs& a, const Blob& L, i
 }
 
 // ONCE: read by one workgroup only, past the caches (gate and up of
-// DeepSeek-V2-Lite sizes, 16 tokens: 33.9 us through them, 29.2 past them; of
-// Mixtral sizes, one token: 25.6 and 23.0).
+// DeepSeek-V2-Lite sizes, 16 tokens: 40.0 us through them, 34.0 past them; of
+// Mixtral sizes, one token: 26.2 and 23.5).
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load_codes(BlobRef r, uint32_t at, uint32_t lane) {
     return __builtin_amdgcn_raw_buffer_load_b128(r, int(lane * 16u), int(at), ONCE ? 2 : 0);
@@ -365,11 +365,11 @@ __device__ __forceinline__ float scale_in(uint32_t group, int tile) { return sca
 // through LDS, 128 at a time, double-buffered.  A column's 256 bytes lie as 16
 // chunks of eight values, chunk i in place i ^ (token % 16), so that the 16
 // lanes of a read, one chunk of 16 tokens, meet 16 different places.
-// Bound by the matrix instructions for many tokens (Qwen3-30B sizes, 4096 tokens:
-// up 189 us, 1090 TFLOP/s, where the library's 8192^3 product reaches 1213 on the
-// same card; down 138, 750, its six column tiles a workgroup against the time to
-// fetch the first and to store the sums), by the weights' bytes for few (64
-// tokens: 210 MB in 36.5 us, 5.7 TB/s).
+// Bound by the matrix instructions for many tokens (Qwen3-30B sizes, 4096 tokens,
+// bf16 y, medians of a trace: up 213 us, 970 TFLOP/s, where the library's 8192^3
+// product reaches 1213 on the same card; down, two pieces, 211 us, 980 TFLOP/s of
+// instructions), by the weights' bytes for few (64 tokens: 210 MB in 39.5 us, 5.3
+// TB/s).
 // The experts' terms of y go to memory in fp32, whatever y's type: they are parts of
 // its sum, and a column of y may be far smaller than the columns beside it (fp16
 // terms over a power of two per 64 columns took 4096 tokens from 424 to 404 us a
@@ -480,7 +480,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (NT == 1) {
         // few products per column tile: bound by the loads, two of them ahead (20
-        // tokens, H 2048, I 1408, 16 experts: 29.6 us a call, 32.6 with one; with
+        // tokens, H 2048, I 1408, 16 experts: 29.4 us a call, 31.8 with one; with
         // 32 tokens a tile the two are equal)
         const auto step = [&](Stage& now, Stage& next, int kt) __attribute__((always_inline)) {
             lds_barrier();
@@ -566,7 +566,7 @@ __device__ __forceinline__ void tile_product(const MxArgs& a, const int4 tl, int
 
 // cut: workgroups that share a tile's tokens (down).
 // Three waves per SIMD (168 registers); four where they cost no spills in the loop
-// and pay: 1024 tokens of top-4, tiles of 32, 73.0 us a call, 76.3 with three.
+// and pay: 1024 tokens of top-4, tiles of 32, 85.6 us a call, 89.6 with three.
 template <bool UP, int NP, int NT, int NH>
 __global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_kernel(MxArgs a, int nb, int cut) {
     constexpr int TM = 16 * NT;
@@ -595,7 +595,7 @@ __global__ __launch_bounds__(kThreads, NP == 1 && NT == 2 ? 4 : 3) void mx_tile_
 }
 
 // y[t] = the sum of its entries' terms, in the entries' order, in fp32.  Bound by
-// the terms' bytes (4096 tokens of top-8, H 2048: 285 MB in 43 us, 6.6 TB/s).
+// the terms' bytes (4096 tokens of top-8, H 2048: 285 MB in 44.9 us, 6.3 TB/s).
 template <bool YF>
 __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
     constexpr int V = 8;
@@ -645,9 +645,9 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
 // takes an equal run of the row blocks to compute, its waves share the
 // contraction and keep their columns in registers, so that the loop loads
 // weights alone, the next row block's while the present one's are used.
-// Measured, Mixtral sizes, one token: up 125 MB in 23.0 us and down 62 MB in
-// 13.8 + 3.9 (join); DeepSeek-V2-Lite sizes, 16 tokens: 161 MB in 29.2, 81 MB in
-// 21.4 + 3.9.  About 6 us of each launch pass before the first weights arrive
+// Medians of a trace, Mixtral sizes, one token: up 125 MB in 23.4 us and down 62 MB
+// in 14.0 + 4.6 (join); DeepSeek-V2-Lite sizes, 16 tokens: 161 MB in 34.2, 81 MB in
+// 26.0 + 4.9 (29.4, 21.5 and 4.4 the shortest).  About 6 us of each launch pass before the first weights arrive
 // (selection, pointers, weights, one after the other) and after the last; in
 // between the up launch streams 7 TB/s, the down launch, whose waves' sums meet
 // in LDS for every four row blocks, 5.
@@ -1098,7 +1098,7 @@ __global__ __launch_bounds__(64 * NW, 4) void mx_down_decode(MxArgs a, int direc
         }
         // [token][row block][row]: of the tokens that are there, so that few of them
         // have few sums to write and to join (Mixtral sizes, one token: the down
-        // launch 15.5 us with all 16 columns' sums, 13.8 with these)
+        // launch at its shortest 15.5 us with all 16 columns' sums, 13.8 with these)
         float v[PER];
 #pragma unroll
         for (int z = 0; z < PER; ++z) {
@@ -1173,11 +1173,11 @@ __global__ __launch_bounds__(1024) void mx_join_kernel(MxArgs a) {
     else reinterpret_cast<__bf16*>(a.y)[size_t(t) * a.H + row] = __bf16(s);
 }
 
-// The down launch's forms: up to 48 column tiles of few columns in one chunk of
-// sixteen waves, whose sums are y (one token, H 2048, I 768, top 8: a call 13.1
-// us, 14.2 with chunks; H 4096, I 1408, top 4, bf16 y: 15.7 and 18.6), else chunks
-// of eight tiles (two row blocks at a time, or four waves: up to 10% slower;
-// sixteen waves: within 3%).
+// The down launch's forms: pieces as columns and up to 48 column tiles, which is
+// what sixteen waves hold in registers, in one chunk, whose sums are y (at that
+// border, one token, H 2048, I 768, top 8: a call 12.9 us, 13.7 with chunks; H
+// 4096, I 1408, top 4, bf16 y: 16.8 and 18.3), else chunks of eight tiles (two row
+// blocks at a time, or four waves: up to 10% slower; sixteen waves: within 3%).
 constexpr int kOneWaves = 16, kOneU = 3, kOneR = 1;
 constexpr int kRunWaves = 8, kRunU = 1, kRunR = 4;
 
@@ -1204,8 +1204,8 @@ int tile_tokens(int T, int K, int E, int ns, int I, bool bf16) {
 
 // Parts of the down launch's contraction: enough for 768 workgroups (three per
 // CU) if half of the experts' last tiles are filled, of four column tiles at
-// least (32 tokens, H 1024, I 8192, 8 experts: 84 us unsplit, 48 split; 20
-// tokens, H 2048, I 1408, 16 experts: 37 and 34).
+// least (32 tokens, H 1024, I 8192, 8 experts: 74 us unsplit, 44 split; 20
+// tokens, H 2048, I 1408, 16 experts: 32 and 29).
 constexpr size_t kDownWgs = 768;
 int most_splits(int I) { return col_tiles(I) < 8 ? 1 : col_tiles(I) / 4; }
 int tile_splits(int tm, size_t n, int E, int ns, int H, int I) {
@@ -1259,7 +1259,7 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
 }
 
 // Row blocks in turn with the columns in registers, for bf16 x of up to 32 column
-// tiles (16 tokens of top-8 of 64, I 1536, whole calls: H 512 31.7 us, 40.1 with
+// tiles, which is what eight waves of four hold (16 tokens of top-8 of 64, I 1536, whole calls: H 512 31.7 us, 40.1 with
 // mx_up_wide; 1024 44.1 and 49.8; 2048 65.6 and 71.6; 4096 113 and 117; one token
 // the same with both).  Four waves take 1, 2 or 4 tiles each (with 4 throughout H
 // 512 34.6 us, 1024 45.3), eight 4; as many workgroups as stay side by side on the

@@ -4,8 +4,8 @@
 // Quantising is one pass: a lane takes eight columns (16 bytes of bf16), the
 // four lanes of a block share the largest magnitude by two lane exchanges, and
 // the hardware conversion divides by the scale and rounds.  The bound is the
-// bytes, esz and 17/32 per element: 14336 x 4096 bf16 takes 24.8 us one way (6.0
-// TB/s) and 21.9 back (6.8).
+// bytes, esz and 17/32 per element: 14336 x 4096 bf16 takes 26.7 us one way (5.6
+// TB/s) and 22.6 back (6.6), medians of a trace.
 #include "mx_format.h"
 
 namespace stmoe {
@@ -19,7 +19,7 @@ constexpr int kUnitsPerBlock = kBlock / kUnit;  // lanes per block
 
 // Rows start at any element: the loads and stores below are whole vectors of
 // their type's own alignment, which the memory pipeline takes at any address.
-// x is read once, past the caches (14336 x 4096 bf16: 28.7 us through them, 24.8
+// x is read once, past the caches (14336 x 4096 bf16: 29.9 us through them, 26.7
 // past them).
 template <class V, class E>
 __device__ __forceinline__ V load_once(const E* p) {
@@ -63,8 +63,8 @@ __device__ __forceinline__ void load_unit(const void* x, int64_t at, int n, floa
 }
 
 // A unit's row and column.  FLAT: whole blocks in contiguous rows, where the
-// matrix is one long row (14336 x 4096 bf16: 24.8 us, 29.4 without; reading back
-// 21.9 and 23.0); else a division, of 32 bits where the units allow it.
+// matrix is one long row (14336 x 4096 bf16: 26.7 us, 30.2 without; reading back
+// 22.6 and 24.0); else a division, of 32 bits where the units allow it.
 template <bool FLAT, int W>
 __device__ __forceinline__ void place(int64_t u, int upr, int64_t& row, int& col) {
     if (FLAT) return;

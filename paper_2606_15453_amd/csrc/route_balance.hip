@@ -16,11 +16,12 @@
 // registers.  The K winners are taken one by one (largest key, lowest index).
 //
 // The forward pass is bound by its instructions, those of the K selections above
-// all (about 50 each for eight logits a lane): 32768 x 128 fp32, top 8, 15 us
+// all (89 each for eight logits a lane, of which 65 are the vector unit's and 16
+// waits between them): 32768 x 128 fp32, top 8, 16.8 us, the median of a trace,
 // for 16.8 MB, and as long in bf16.  Its workgroups' sums go to a second launch
-// of one workgroup (4-5 us; the last workgroup to arrive doing that in the first
-// launch took as long).  The gradient is bound by its bytes: 36 MB in 9.8 us,
-// 3.6 TB/s.
+// of one workgroup (5.6 us; the last workgroup to arrive doing that in the first
+// launch took as long).  The gradient is bound by its bytes and by the load of a
+// selected logit, which waits for the selection: 36 MB in 11.2 us, 3.2 TB/s.
 #include <type_traits>
 
 #include "common.h"
@@ -34,7 +35,7 @@ constexpr int kRowLanes = 16;
 constexpr int kRows = 64 / kRowLanes;      // rows a wave works on
 constexpr int kMaxWg = 256;                // workgroups of the forward pass, each with a row of partial sums
 // Rows that a lane adds up, in 32 bits, before the sums in 64: beyond 2^19 tokens
-// there are more workgroups instead.  Equal rows' rounding errors do not cancel
+// there are more than kMaxWg workgroups instead.  Equal rows' rounding errors do not cancel
 // (4096 of them are up to 4e-5 off, 32 at most 2e-6).  2^24 x 128 bf16, top 8, takes
 // 5.46 ms, 5.26 in 256 workgroups; 2^26 x 8 3.7 and 5.1.
 constexpr int kChain = 32;
@@ -455,8 +456,8 @@ BalanceLayout balance_layout(int64_t T, int E) {
 }
 
 // Calls f(bf16, logits per lane, VEC) for E experts.  VEC: bf16 rows of whole
-// groups of four, aligned to them (32768 x 128: 14.5 us with, 15.7 without, the
-// gradient 9.8 and 11.2; fp32 15.4 and 15.5, 10.3 and 9.8).
+// groups of four, aligned to them (32768 x 128, shortest launches: 14.5 us with,
+// 15.7 without, the gradient 9.8 and 11.2; fp32 15.4 and 15.5, 10.3 and 9.8).
 template <class F>
 void with_row(int dtype, int E, bool fours, F f) {
     const auto lanes = [&](auto bf, auto vec) {
@@ -569,7 +570,8 @@ extern "C" int moe_route_balance_backward(const void* logits, int64_t T, int64_t
     a.d_w = d_w;
     a.d_loss = d_loss;
     a.d_logits = d_logits;
-    // 1024 workgroups at most (32768 x 128 fp32: 16.0 us with 256, 10.3, 11.1 with 4096)
+    // 1024 workgroups at most (32768 x 128 fp32, shortest launches: 16.0 us with 256,
+    // 10.3, 11.1 with 4096)
     const int64_t per = kGradThreads / 64 * kRows, wg = (T + per - 1) / per;
     const dim3 grid(unsigned(wg < 1024 ? wg : 1024));
     with_row(dtype, E, rows_of_four(logits, ld, E) && rows_of_four(d_logits, ld_d, E), [&](auto bf, auto v, auto vec) {
