@@ -49,6 +49,25 @@ def log(msg):
     print(f"[bench] {msg}", file=sys.stderr, flush=True)
 
 
+#: what a capped run keeps in the line on stdout; --record takes all of it
+RUN_KEYS = ("tokens_per_s", "stall_ms_per_token", "h2d_copies", "h2d_gbps")
+
+
+def stdout_line(out):
+    """The one JSON line: the record with its capped runs cut to RUN_KEYS and without what follows from those, short
+    enough (below 7000 characters) to be read whole from the end of a captured output."""
+    def short(runs):
+        return {k: {n: v[n] for n in RUN_KEYS} if isinstance(v, dict) and "tokens_per_s" in v else v
+                for k, v in runs.items() if not k.startswith("stall_reduction")}
+
+    line = dict(out)
+    if "offload" in line:
+        line["offload"] = short(line["offload"])
+    if "capped" in line.get("largest_config", {}):
+        line["largest_config"] = dict(line["largest_config"], capped=short(line["largest_config"]["capped"]))
+    return json.dumps(line, separators=(",", ":"))
+
+
 def parse():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -100,6 +119,8 @@ def parse():
                          "line's 'largest_config' (0 skips)")
     ap.add_argument("--largest-capped-tokens", type=int, default=3,
                     help="tokens of the largest workload's capped-cache runs in 'largest_config' (0 skips)")
+    ap.add_argument("--record", metavar="FILE",
+                    help="write the whole record there too (every capped run with its settings, counters and stages)")
     ap.add_argument("--read-floor", action="store_true",
                     help="time one streaming-read launch per size, bytes in no cache (markdown table) and exit")
     ap.add_argument("--reread-probe", action="store_true",
@@ -2151,7 +2172,10 @@ def main():
                                                args.pinned_gb)
         log(f"largest config {out['largest_config']['workload']}: {out['largest_config']['tokens_per_s']} tok/s "
             f"({time.time() - t0:.1f}s wall)")
-    print(json.dumps(out), flush=True)
+    if args.record:
+        with open(args.record, "w") as f:
+            json.dump(out, f, indent=1)
+    print(stdout_line(out), flush=True)
 
 
 if __name__ == "__main__":

@@ -124,3 +124,43 @@ def test_timing_cadence():
         c = bench.timing_cadence(steps)
         timed = len(range(0, steps, c))
         assert 1 <= c <= bench.TIMING_EVERY and (timed >= 2 or steps == 1)
+
+
+def test_line_on_stdout_is_short_and_keeps_the_contract():
+    """The default run's record, with every capped run of both workloads: one line below 7000 characters with the
+    record's own values; the record itself is left whole."""
+    import json
+    from paper_2606_15453_amd import workload as W
+    run = dict(tokens=16, seconds=1.0259, prefetch_min_score=2, staged_per_layer=2, staged_head_bytes=2961408,
+               graph_replay=False, prefetch_max_per_layer=3, online_update=True, prefetch_after_demand=True,
+               device_decisions=False, eviction="least recently used", tokens_per_s=15.599, ms_per_token=3560.331,
+               stall_ms_per_token=3516.494, h2d_copies=15703, h2d_gbps=52.47,
+               cache=dict(hits=10121, demand=2569, overflow=9799, prefetch=3472, useful=2623, wasted=848),
+               stages_us_per_layer=dict(route_and_predict=47.1, record_wait_and_missed_loads=12046.7, ffn=25776.5),
+               recall_layers_ge1=0.7127, recall_layer0=0.5391, precision=0.183, mean_predicted_per_row=31.078)
+
+    def capped(names):
+        return dict({n: dict(run) for n in names}, stall_reduction={n: 0.0283 for n in names},
+                    stall_reduction_vs_same_policy_on_demand={n: dict(against="on_demand_device", reduction=-0.0122) for n in names},
+                    cache_slots_per_layer=45, pool_tier="host",
+                    host_pool=dict(distinct_blobs=1483, experts=12032, slot_of_expert="(l*E + e) mod distinct_blobs"),
+                    h2d_link="PCIe, pinned host memory, hipMemcpyAsync on demand/side streams")
+
+    out = {k: 1234.567 for k in ("value", "ms_per_step", "ffn_hbm_gbps", "step_hbm_gbps", "layer_us", "host_issue_us_per_layer")}
+    out.update(metric="MoE decode tokens/s; expert-weight HBM GB/s vs peak; prefetch hit rate", unit="tokens/s", n_gpus=1,
+               steps=20, warmup=5, higher_is_better=True, scaling="weak", vs_baseline=None, dtype="bf16", data="x" * 80,
+               config=dict(workload="x" * 60, mode="x" * 160, launch="x" * 120, layers=32), roofline=dict(note="x" * 420),
+               prediction=dict(note="x" * 80), stages_us_per_layer=dict(note="x" * 120), repeats=dict(note="x" * 120),
+               cpu_baseline=dict(note="x" * 620), achievable_read_gbps=dict(note="x" * 60), ffn_down=dict(note="x" * 80))
+    out["offload"] = capped([v["name"] for v in bench.offload_variants(W.CONFIGS["mixtral"])])
+    out["largest_config"] = dict(tokens_per_s=367.72, note="x" * 700,
+                                 capped=capped(["on_demand", "on_demand_device", "st_moe_device", "st_moe_staged_device"]))
+    whole = json.dumps(out)
+    line = bench.stdout_line(out)
+    assert "\n" not in line and len(line) < 7000 < len(whole)
+    assert json.dumps(out) == whole
+    back = json.loads(line)
+    assert {k: v for k, v in back.items() if k not in ("offload", "largest_config")} == \
+        {k: v for k, v in out.items() if k not in ("offload", "largest_config")}
+    assert back["offload"]["on_demand_freq"] == dict(tokens_per_s=15.599, stall_ms_per_token=3516.494, h2d_copies=15703, h2d_gbps=52.47)
+    assert back["largest_config"]["tokens_per_s"] == 367.72 and back["largest_config"]["capped"]["cache_slots_per_layer"] == 45
