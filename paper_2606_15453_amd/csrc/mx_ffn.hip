@@ -647,10 +647,10 @@ __global__ __launch_bounds__(kThreads) void mx_sum_kernel(MxArgs a, int nb) {
 // weights alone, the next row block's while the present one's are used.
 // Medians of a trace, Mixtral sizes, one token: up 125 MB in 23.4 us and down 62 MB
 // in 14.0 + 4.6 (join); DeepSeek-V2-Lite sizes, 16 tokens: 161 MB in 34.2, 81 MB in
-// 26.0 + 4.9 (29.4, 21.5 and 4.4 the shortest).  About 6 us of each launch pass before the first weights arrive
-// (selection, pointers, weights, one after the other) and after the last; in
-// between the up launch streams 7 TB/s, the down launch, whose waves' sums meet
-// in LDS for every four row blocks, 5.
+// 26.0 + 4.9 (29.4, 21.5 and 4.4 the shortest).  About 6 us of each launch pass
+// before the first weights arrive (selection, pointers, weights, one after the
+// other) and after the last; in between the up launch streams 7 TB/s, the down
+// launch, whose waves' sums meet in LDS for every four row blocks, 5.
 
 // A distinct expert of a decode step and, per token, the entry that selects it.
 struct DecodeSlot {
@@ -1192,10 +1192,11 @@ struct MxLayout {
 // tiles of 16, 32 and 64 (H 2048, I 768, 64 experts, top 4 unless said):
 //    128 tokens   41    41    45       512 tokens   59    63    68
 //    256          49    49    52      2048         152   137   148  (960 workgroups)
-//   4096, 128 experts, top 8, bf16:   472 with 32, 463 with 64
+//   4096, 128 experts, top 8, bf16:   472 with 32, 463 with 64; fp32: 862, 803, 890
 //    512, H 4096, I 14336, 8 experts, top 2, bf16:  663 with 32, 531 with 64
-// (12: with large experts 32 is ahead from there on, 64 tokens of the last shape
-// 201 and 171 us; small ones lose up to a tenth by it until about 40.)
+// 12 is where 32 gets ahead with large experts (64 tokens of the last shape 201 and
+// 171 us); with small ones 16 stays ahead until about 40 (160 fp32 tokens, H 1000, I
+// 520, top 3 of 13: 30 and 40 us).
 int tile_tokens(int T, int K, int E, int ns, int I, bool bf16) {
     const int mean = T * K / E;
     const int64_t wg = (int64_t(T) * (K + ns) / 64 + (E + ns) / 2) * ((I + 127) / 128);
