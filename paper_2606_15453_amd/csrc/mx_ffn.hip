@@ -1260,9 +1260,9 @@ MxLayout mx_layout(int T, int K, int E, int H, int I, int ns, int dtype, int ydt
 }
 
 // Row blocks in turn with the columns in registers, for bf16 x of up to 32 column
-// tiles, which is what eight waves of four hold (16 tokens of top-8 of 64, I 1536, whole calls: H 512 31.7 us, 40.1 with
-// mx_up_wide; 1024 44.1 and 49.8; 2048 65.6 and 71.6; 4096 113 and 117; one token
-// the same with both).  Four waves take 1, 2 or 4 tiles each (with 4 throughout H
+// tiles, which is what eight waves of four hold (16 tokens of top-8 of 64, I 1536,
+// whole calls: H 512 31.7 us, 40.1 with mx_up_wide; 1024 44.1 and 49.8; 2048 65.6
+// and 71.6; 4096 113 and 117; one token the same with both).  Four waves take 1, 2 or 4 tiles each (with 4 throughout H
 // 512 34.6 us, 1024 45.3), eight 4; as many workgroups as stay side by side on the
 // 256 CUs, but up to 1024 row blocks of four waves one each (one token, H 2048, I
 // 1536: 18.0 us, 19.4 on 512).
