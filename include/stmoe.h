@@ -226,6 +226,54 @@ int moe_route_balance_backward(const void* logits, int64_t T, int64_t ld, int E,
                                void* d_logits, int64_t ld_d, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Routing by scores: s = softmax(logits[t]) or the sigmoid of every logit.  A
+ * bias (for balance) takes part in the choice c = s + bias and not in the
+ * weights; the experts may be in n_groups groups of consecutive ones, of which
+ * a token's best top_groups are searched, a group being as good as the sum of
+ * its best group_top choices (1 or 2); the best K experts there are selected,
+ * with the weights scale * s, or, with renorm = 1, scale * s divided by the
+ * sum of the selected s.  Choices are compared in 64 bits (without a bias by
+ * the logits themselves); equal ones go to the lower index, of experts and of
+ * groups.  A logit or a bias of minus infinity is no candidate; the type's
+ * lowest value is a number like others.  A choice that is NaN ranks below
+ * every number; a softmax over a NaN or plus infinity is NaN throughout.
+ *
+ *   logits   device [T] rows of E values, row stride ld elements, dtype
+ *   score    STMOE_SOFTMAX or STMOE_SIGMOID
+ *   bias     device [E] fp32, or NULL
+ *   mask     device [T] uint8, or NULL: every token counts
+ *   topk_idx device out [T][K] int32, best choice first; -1 (and weight 0)
+ *            where a row has fewer than K candidates, and throughout a row
+ *            whose mask is 0
+ *   topk_w   device out [T][K] fp32
+ *   counts   device [E] int32, or NULL: the number of selections of every
+ *            expert is added to it
+ *   0 <= T <= 2^26 (0: nothing is done); n_groups divides E; K at most 16 and
+ *   the experts of top_groups groups.  One launch, no workspace.  The same
+ *   inputs give the same bits.
+ * ---------------------------------------------------------------------- */
+enum { STMOE_SOFTMAX = 0, STMOE_SIGMOID = 1 };
+int moe_route_scored(const void* logits, int64_t T, int64_t ld, int E, int K, int dtype, int score,
+                     const float* bias, int n_groups, int top_groups, int group_top, int renorm,
+                     float scale, const uint8_t* mask, int32_t* topk_idx, float* topk_w,
+                     int32_t* counts, void* stream);
+/* Its gradient: d_logits from the gradients d_w (device [T][K] fp32) of the
+ * weights, with the selection topk_idx as a constant; entries outside [0, E)
+ * have no part, an expert named twice counts twice.
+ *   d_logits device out [T] rows of E values, row stride ld_d, dtype; may be
+ *            logits itself when ld_d = ld */
+int moe_route_scored_backward(const void* logits, int64_t T, int64_t ld, int E, int K, int dtype, int score,
+                              int renorm, float scale, const int32_t* topk_idx, const float* d_w,
+                              void* d_logits, int64_t ld_d, void* stream);
+/* One step of the balance biases of L layers: an expert with fewer selections
+ * than its layer's mean gains rate, one with more loses it.
+ *   counts   device [L][E] int32 (may be summed over batches and ranks)
+ *   bias     device [L][E] fp32; bias_out device out [L][E] fp32, may be bias
+ *   reset    1: counts are set to 0 for the next step */
+int moe_route_bias_step(int32_t* counts, int L, int E, const float* bias, float rate, float* bias_out,
+                        int reset, void* stream);
+
+/* ------------------------------------------------------------------------
  * Expert packing.  A packed expert ("blob") is one contiguous buffer:
  * W_gate [I][H], then W_up [I][H], then W_down [H][I], each row-major in
  * the storage dtype; 3*H*I elements.  One blob moves with one copy.

@@ -97,6 +97,9 @@ _SIGS = {
     "moe_route_balance_workspace_bytes": (sz, [i64, i32]),
     "moe_route_balance": (i32, [vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
     "moe_route_balance_backward": (i32, [vp, i64, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp]),
+    "moe_route_scored": (i32, [vp, i64, i64, i32, i32, i32, i32, vp, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp, vp]),
+    "moe_route_scored_backward": (i32, [vp, i64, i64, i32, i32, i32, i32, i32, C.c_float, vp, vp, vp, i64, vp]),
+    "moe_route_bias_step": (i32, [vp, i32, i32, vp, C.c_float, vp, i32, vp]),
     "moe_mx_quantize": (i32, [vp, i64, i32, i64, i32, vp, vp, vp]),
     "moe_mx_dequantize": (i32, [vp, vp, i64, i32, vp, i64, i32, vp]),
     "moe_mx_pack_expert": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]),
@@ -344,6 +347,66 @@ def route_balance_backward(logits, idx, counts, n_tokens, d_loss, d_logits, d_w=
         _dense("d_w", d_w, (T, K), _F32, dev)
     _call("moe_route_balance_backward", logits.data_ptr(), T, ld, E, K, _dt("logits", logits), int(renorm),
           idx.data_ptr(), counts.data_ptr(), n_tokens.data_ptr(), _p(d_w), d_loss.data_ptr(), d_logits.data_ptr(), ld_d,
+          _s(stream))
+
+
+# ------------------------------------------------------------- routing by scores
+SOFTMAX, SIGMOID = 0, 1
+_SCORES = {"softmax": SOFTMAX, "sigmoid": SIGMOID, SOFTMAX: SOFTMAX, SIGMOID: SIGMOID}
+
+
+def _score(score):
+    if score not in _SCORES:
+        raise ValueError(f"score must be 'softmax' or 'sigmoid', not {score!r}")
+    return _SCORES[score]
+
+
+def route_scored(logits, K, idx, w, score="sigmoid", bias=None, n_groups=1, top_groups=None, group_top=2, renorm=False,
+                 scale=1.0, mask=None, counts=None, stream=None):
+    """The best K experts of the best top_groups (None: all) groups by score + bias, and their weights, for logits
+    [T][E] (rows may be strided); the selections per expert are added to counts."""
+    T, E, ld = _rows("logits", logits)
+    dev = _device("logits", logits)
+    _dense("idx", idx, (T, K), _I32, dev)
+    _dense("w", w, (T, K), _F32, dev)
+    if bias is not None:
+        _dense("bias", bias, (E,), _F32, dev)
+    if mask is not None:
+        _dense("mask", mask, (T,), (torch.uint8, torch.bool), dev)
+    if counts is not None:
+        _dense("counts", counts, (E,), _I32, dev)
+    _call("moe_route_scored", logits.data_ptr(), T, ld, E, K, _dt("logits", logits), _score(score), _p(bias), n_groups,
+          n_groups if top_groups is None else top_groups, group_top, int(renorm), scale, _p(mask), idx.data_ptr(),
+          w.data_ptr(), _p(counts), _s(stream))
+
+
+def route_scored_backward(logits, idx, d_w, d_logits, score="sigmoid", renorm=False, scale=1.0, stream=None):
+    """d_logits of route_scored, from the gradients of the weights."""
+    T, E, ld = _rows("logits", logits)
+    Td, Ed, ld_d = _rows("d_logits", d_logits)
+    dev = _device("logits", logits)
+    if idx.dim() != 2:
+        raise ValueError("idx must be a matrix")
+    K = idx.shape[1]
+    if (Td, Ed) != (T, E) or d_logits.dtype != logits.dtype or d_logits.get_device() != dev:
+        raise ValueError("d_logits must have the shape, dtype and device of logits")
+    _dense("idx", idx, (T, K), _I32, dev)
+    _dense("d_w", d_w, (T, K), _F32, dev)
+    _call("moe_route_scored_backward", logits.data_ptr(), T, ld, E, K, _dt("logits", logits), _score(score), int(renorm),
+          scale, idx.data_ptr(), d_w.data_ptr(), d_logits.data_ptr(), ld_d, _s(stream))
+
+
+def route_bias_step(counts, bias, rate, out=None, reset=False, stream=None):
+    """One step of the balance biases, [E] or [L][E], into out (None: bias itself); reset: counts become 0."""
+    dev = _device("counts", counts)
+    if counts.dim() not in (1, 2):
+        raise ValueError("counts must be [E] or [L][E]")
+    out = bias if out is None else out
+    _dense("counts", counts, counts.shape, _I32, dev)
+    _dense("bias", bias, counts.shape, _F32, dev)
+    _dense("out", out, counts.shape, _F32, dev)
+    L = counts.shape[0] if counts.dim() == 2 else 1
+    _call("moe_route_bias_step", counts.data_ptr(), L, counts.shape[-1], bias.data_ptr(), rate, out.data_ptr(), int(reset),
           _s(stream))
 
 
