@@ -397,6 +397,65 @@ int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const float* topk_
                       void* stream);
 
 /* ------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection (the router's
+ * logits, the expert block's result, or a projection of the caller's): for
+ * token t with adapter a = adapter[t] of rank r,
+ *   y[t] = base[t] + scale_a * (x[t] A_a^T) B_a
+ * with A_a [r][Hin] and B_a [r][Hout] row-major (the up-projection is held by
+ * its ranks, the transpose of [Hout][r]); a token whose adapter is not in
+ * [0, n_adapters) gets base[t].
+ *
+ * moe_lora_plan sorts a batch's tokens by adapter, once for every projection
+ * of every layer that the batch passes.  plan: device, 256-byte aligned,
+ * moe_lora_plan_bytes(T, n_adapters) bytes, read by the calls that take it
+ * with the same T and n_adapters (with others they write nothing).
+ *   adapter  device [T] int32
+ *   0 <= T <= 65536, 1 <= n_adapters <= 4096
+ * ---------------------------------------------------------------------- */
+size_t moe_lora_plan_bytes(int T, int n_adapters);
+int moe_lora_plan(const int32_t* adapter, int T, int n_adapters, void* plan, size_t plan_bytes, void* stream);
+/*   x        device [T] rows of Hin values, row stride ldx elements, dtype
+ *   a_ptrs   device array [n_adapters] of device pointers to A, dtype, 16-byte
+ *            aligned; b_ptrs so to B.  Only the batch's adapters' are read
+ *   R        1 <= R <= 128, the largest rank
+ *   ranks    device [n_adapters] int32 (0 to R), or NULL: all R
+ *   scales   device [n_adapters] fp32, or NULL: all 1
+ *   base     device [T] rows of Hout values, row stride ld_base, ydtype, or
+ *            NULL: zeros; may be y when ld_base = ldy
+ *   y        device out [T] rows of Hout values, row stride ldy, ydtype
+ *   v        device out [T][R] fp32, 16-byte aligned, or NULL: x[t] A_a^T, for
+ *            moe_lora_backward (0 beyond the adapter's rank; rows without an
+ *            adapter are left as they are)
+ *   ws       device workspace of moe_lora_workspace_bytes(...) bytes, 256-byte
+ *            aligned, no initial contents required; calls sharing it must be
+ *            ordered on one stream.  Its size never falls as T grows
+ * dtype and ydtype: STMOE_BF16 or STMOE_F32 each; Hin, Hout 1 to 65536 (bf16:
+ * multiples of 8 in 16-byte aligned rows are faster).  Sums are fp32, and x A^T
+ * is held in 32 bits.  The same inputs give the same bits. */
+size_t moe_lora_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype);
+int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapters, int R, int dtype, int ydtype,
+             const void* plan, const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks,
+             const float* scales, const void* base, int64_t ld_base, void* y, int64_t ldy, float* v, void* ws,
+             size_t ws_bytes, void* stream);
+/* Its gradient, for T >= 1: from dy (device [T] rows of Hout values, row stride
+ * ld_dy, dtype), x and v as moe_lora took and gave them,
+ *   dx[t] = base[t] + scale_a * (dy[t] B_a^T) A_a      (base NULL: zeros; dx
+ *           NULL: not computed; base may be dx when ld_base = ld_dx)
+ *   dA_a  = scale_a * sum over a's tokens of (dy[t] B_a^T)^T x[t]
+ *   dB_a  = scale_a * sum over a's tokens of v[t]^T dy[t]
+ *   base, dx   device [T] rows of Hin values, dtype
+ *   da_ptrs    device array [n_adapters] of device pointers to fp32 [r][Hin],
+ *              16-byte aligned; db_ptrs so to fp32 [r][Hout].  Overwritten,
+ *              with zeros for an adapter without tokens; no two may overlap
+ *   ws         moe_lora_backward_workspace_bytes(...) bytes, as above */
+size_t moe_lora_backward_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype);
+int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int64_t ld_dy, const float* v, int T, int Hin,
+                      int Hout, int n_adapters, int R, int dtype, const void* plan, const void* const* a_ptrs,
+                      const void* const* b_ptrs, const int32_t* ranks, const float* scales, float* const* da_ptrs,
+                      float* const* db_ptrs, const void* base, int64_t ld_base, void* dx, int64_t ld_dx, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Expert cache policy (host only, no HIP calls): per-layer partition of C
  * slots, least recently used with protection of the current set.
  *   prefetch(layer, ranked, n, stamp): for each of the first min(n, C)

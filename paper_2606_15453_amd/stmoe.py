@@ -100,6 +100,13 @@ _SIGS = {
     "moe_route_scored": (i32, [vp, i64, i64, i32, i32, i32, i32, vp, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp, vp]),
     "moe_route_scored_backward": (i32, [vp, i64, i64, i32, i32, i32, i32, i32, C.c_float, vp, vp, vp, i64, vp]),
     "moe_route_bias_step": (i32, [vp, i32, i32, vp, C.c_float, vp, i32, vp]),
+    "moe_lora_plan_bytes": (sz, [i32, i32]),
+    "moe_lora_plan": (i32, [vp, i32, i32, vp, sz, vp]),
+    "moe_lora_workspace_bytes": (sz, [i32] * 6),
+    "moe_lora": (i32, [vp, i64, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, sz, vp]),
+    "moe_lora_backward_workspace_bytes": (sz, [i32] * 6),
+    "moe_lora_backward": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64,
+                                vp, i64, vp, sz, vp]),
     "moe_mx_quantize": (i32, [vp, i64, i32, i64, i32, vp, vp, vp]),
     "moe_mx_dequantize": (i32, [vp, vp, i64, i32, vp, i64, i32, vp]),
     "moe_mx_pack_expert": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]),
@@ -553,6 +560,114 @@ def expert_ffn_mx(x, idx, w, H, I, E, expert_ptrs, y, ws, shared_ptrs=None, n_sh
     _call("moe_expert_ffn_mx", x.data_ptr(), idx.data_ptr(), w.data_ptr(), T, K, H, I, E, _DTYPES[x.dtype],
           _DTYPES[y.dtype], expert_ptrs.data_ptr(), _p(shared_ptrs), n_shared, y.data_ptr(), *_workspace(ws, dev),
           _s(stream))
+
+
+# ------------------------------------------------------------- low-rank adapters
+def lora_plan_bytes(T, n):
+    """Bytes of the plan of T tokens and n adapters (256-byte aligned); 0 for an invalid shape."""
+    return _lib.moe_lora_plan_bytes(T, n)
+
+
+def lora_plan(adapter, n, plan, stream=None):
+    """Sort a batch by its tokens' adapters [T] (outside [0, n): none), for every lora and lora_backward call on it."""
+    dev = _device("adapter", adapter)
+    _dense("adapter", adapter, (adapter.numel(),), _I32, dev)
+    _call("moe_lora_plan", adapter.data_ptr(), adapter.numel(), n, *_plan(plan, dev), _s(stream))
+
+
+def _plan(plan, dev):
+    if plan is None or plan.get_device() != dev:
+        raise ValueError("plan must be on the current CUDA device")
+    if not plan.is_contiguous():
+        raise ValueError("plan must be contiguous")
+    return plan.data_ptr(), plan.nbytes
+
+
+def _adapters(T, plan, a_ptrs, b_ptrs, ranks, scales, dev):
+    """(number of adapters, plan pointer) after the checks that lora and lora_backward share."""
+    n = a_ptrs.numel()
+    at, nbytes = _plan(plan, dev)
+    if nbytes < lora_plan_bytes(T, n):
+        raise ValueError(f"plan is not that of {T} tokens and {n} adapters")
+    for name, t in (("a_ptrs", a_ptrs), ("b_ptrs", b_ptrs)):
+        _dense(name, t, (n,), (torch.int64,), dev)
+    if ranks is not None:
+        _dense("ranks", ranks, (n,), _I32, dev)
+    if scales is not None:
+        _dense("scales", scales, (n,), _F32, dev)
+    return n, at
+
+
+def _rows_of(name, t, rows, dev, dtypes):
+    """(columns, row stride) of a matrix with that many rows."""
+    r, c, ld = _rows(name, t)
+    if r != rows:
+        raise ValueError(f"{name} must have {rows} rows, not {r}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the current CUDA device")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}")
+    return c, ld
+
+
+def lora_workspace_bytes(T, Hin, Hout, n, R, dtype=torch.bfloat16):
+    """Workspace bytes for lora (256-byte aligned; never less for a larger T); 0 for an invalid shape."""
+    return _lib.moe_lora_workspace_bytes(T, Hin, Hout, n, R, _DTYPES[dtype])
+
+
+def lora_backward_workspace_bytes(T, Hin, Hout, n, R, dtype=torch.bfloat16):
+    """Workspace bytes for lora_backward, likewise."""
+    return _lib.moe_lora_backward_workspace_bytes(T, Hin, Hout, n, R, _DTYPES[dtype])
+
+
+def lora(x, plan, a_ptrs, b_ptrs, R, y, ws, base=None, ranks=None, scales=None, v=None, stream=None):
+    """y = base + scale (x A^T) B of every token's adapter: x [T][Hin], base and y [T][Hout] (rows may be strided), A
+    [r][Hin] and B [r][Hout] in x's dtype; base None: zeros, base y: in place.  v [T][R]: x A^T, for lora_backward."""
+    T, Hin, ldx = _rows("x", x)
+    dev = _device("x", x)
+    dt = _dt("x", x)
+    Hout, ldy = _rows_of("y", y, T, dev, _DTYPES)
+    ld_base = 0
+    if base is not None:
+        cols, ld_base = _rows_of("base", base, T, dev, (y.dtype,))
+        if cols != Hout:
+            raise ValueError(f"base must have {Hout} columns, not {cols}")
+    n, at = _adapters(T, plan, a_ptrs, b_ptrs, ranks, scales, dev)
+    if v is not None:
+        _dense("v", v, (T, R), _F32, dev)
+    _call("moe_lora", x.data_ptr(), ldx, T, Hin, Hout, n, R, dt, _DTYPES[y.dtype], at, a_ptrs.data_ptr(),
+          b_ptrs.data_ptr(), _p(ranks), _p(scales), _p(base), ld_base, y.data_ptr(), ldy, _p(v), *_workspace(ws, dev),
+          _s(stream))
+
+
+def lora_backward(x, dy, v, plan, a_ptrs, b_ptrs, R, da_ptrs, db_ptrs, ws, dx=None, base=None, ranks=None, scales=None,
+                  stream=None):
+    """Gradients of lora: dA [r][Hin] and dB [r][Hout] fp32 behind da_ptrs and db_ptrs, and dx = base + scale (dy B^T) A
+    where it is given (base None: zeros, base dx: in place)."""
+    T, Hin, ldx = _rows("x", x)
+    dev = _device("x", x)
+    dt = _dt("x", x)
+    Hout, ld_dy = _rows_of("dy", dy, T, dev, (x.dtype,))
+    ld_dx = ld_base = 0
+    if base is not None and dx is None:
+        raise ValueError("base without dx")
+    for name, t in (("dx", dx), ("base", base)):
+        if t is None:
+            continue
+        cols, ld = _rows_of(name, t, T, dev, (x.dtype,))
+        if cols != Hin:
+            raise ValueError(f"{name} must have {Hin} columns, not {cols}")
+        if name == "dx":
+            ld_dx = ld
+        else:
+            ld_base = ld
+    n, at = _adapters(T, plan, a_ptrs, b_ptrs, ranks, scales, dev)
+    for name, t in (("da_ptrs", da_ptrs), ("db_ptrs", db_ptrs)):
+        _dense(name, t, (n,), (torch.int64,), dev)
+    _dense("v", v, (T, R), _F32, dev)
+    _call("moe_lora_backward", x.data_ptr(), ldx, dy.data_ptr(), ld_dy, v.data_ptr(), T, Hin, Hout, n, R, dt, at,
+          a_ptrs.data_ptr(), b_ptrs.data_ptr(), _p(ranks), _p(scales), da_ptrs.data_ptr(), db_ptrs.data_ptr(), _p(base),
+          ld_base, _p(dx), ld_dx, *_workspace(ws, dev), _s(stream))
 
 
 # ------------------------------------------------------------- cache policy

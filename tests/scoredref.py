@@ -81,3 +81,26 @@ def route_grad(z, idx, d_w, score, renorm, scale):
 def bias_step(counts, bias, rate):
     counts = np.asarray(counts, np.int64)
     return bias + rate * np.sign(counts.sum(axis=-1, keepdims=True) - counts * counts.shape[-1])
+
+
+def lora(x, adapter, A, B, scales, base):
+    """(y [T][Hout], {token: v}) of lists of A [r][Hin] and B [r][Hout]; adapters outside the list: base alone."""
+    y, v = np.array(base, np.float64), {}
+    for a in range(len(A)):
+        rows = np.flatnonzero(adapter == a)
+        va = x[rows] @ A[a].T
+        y[rows] += scales[a] * (va @ B[a])
+        v.update(zip(rows, va))
+    return y, v
+
+
+def lora_grad(x, dy, adapter, A, B, scales, base):
+    """(dx [T][Hin], [dA], [dB])"""
+    dx, dA, dB = np.array(base, np.float64), [], []
+    for a in range(len(A)):
+        rows = np.flatnonzero(adapter == a)
+        u = scales[a] * (dy[rows] @ B[a].T)
+        dx[rows] += u @ A[a]
+        dA.append(u.T @ x[rows])
+        dB.append(scales[a] * ((x[rows] @ A[a].T).T @ dy[rows]))
+    return dx, dA, dB
