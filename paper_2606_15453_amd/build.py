@@ -18,7 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["util.cpp", "route_topk.hip", "predictor.hip", "expert_ffn.hip", "expert_cache.cpp",
            "cache_device.hip", "decode_layer.hip", "calib.hip", "mx_quant.hip", "mx_ffn.hip",
-           "route_balance.hip", "route_scored.hip", "lora_plan.hip", "lora.hip"]
+           "route_balance.hip", "route_scored.hip", "lora_plan.hip", "lora.hip", "lora_bf16.hip"]
 LIB = os.path.join(HERE, "libstmoe.so")
 ARCH = "gfx950"
 

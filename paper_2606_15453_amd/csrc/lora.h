@@ -1,0 +1,58 @@
+// Low-rank adapters: what the general kernels (lora.hip) and those for bf16 rows in
+// whole 16-byte chunks (lora_bf16.hip) share.
+#pragma once
+
+#include "lora_plan.h"
+
+namespace stmoe {
+namespace lora {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct Args {
+    Plan plan;
+    int T, n, R;
+    const int32_t* ranks;          // [n] or null: all R
+    const float* scales;           // [n] or null: 1
+};
+
+__device__ __forceinline__ bool planned(const Args& g) { return g.plan.head->T == g.T && g.plan.head->n == g.n; }
+__device__ __forceinline__ int rank_of(const Args& g, int a) {
+    const int r = g.ranks ? g.ranks[a] : g.R;
+    return r < 0 ? 0 : r < g.R ? r : g.R;
+}
+
+struct ShrinkArgs {
+    Args g;
+    const void* x;                 // [T] rows of C values, row stride ld
+    int64_t ld;
+    int C;
+    const void* const* m;          // [n] matrices [r][C]
+    int scaled;                    // by the adapter's scale
+    float* v;                      // [T][R]; columns beyond the rank get 0
+    int parts;                     // of the columns: v is [parts][T][R] then
+};
+
+struct ExpandArgs {
+    Args g;
+    const float* v;                // [parts][T][R], to be summed
+    int parts;
+    float* v_out;                  // [T][R] the sum, or null
+    const void* const* m;          // [n] matrices [r][C]
+    int C, scaled;
+    const void* base;              // [T] rows of C values, row stride ld_base, or null: 0
+    int64_t ld_base;
+    void* y;                       // out, row stride ld
+    int64_t ld;
+};
+
+// lora_bf16.hip
+int shrink_bf16(const ShrinkArgs& a, int table, hipStream_t s);
+int expand_bf16(const ExpandArgs& a, int table, bool ybf, hipStream_t s);
+
+inline bool chunks16(const void* p, int64_t ld, int C, int esz) {
+    return C % (16 / esz) == 0 && ld * esz % 16 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
+
+}  // namespace lora
+}  // namespace stmoe

@@ -12,13 +12,11 @@
 // of each operand at a time, so any layout of rows and columns does.
 #include <type_traits>
 
-#include "lora_plan.h"
+#include "lora.h"
 
 namespace stmoe {
 namespace lora {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
@@ -39,29 +37,6 @@ __device__ __forceinline__ void put(void* p, int64_t i, float v) {
     if (BF) reinterpret_cast<__bf16*>(p)[i] = __bf16(v);
     else reinterpret_cast<float*>(p)[i] = v;
 }
-
-struct Args {
-    Plan plan;
-    int T, n, R;
-    const int32_t* ranks;          // [n] or null: all R
-    const float* scales;           // [n] or null: 1
-};
-
-__device__ __forceinline__ bool planned(const Args& g) { return g.plan.head->T == g.T && g.plan.head->n == g.n; }
-__device__ __forceinline__ int rank_of(const Args& g, int a) {
-    const int r = g.ranks ? g.ranks[a] : g.R;
-    return r < 0 ? 0 : r < g.R ? r : g.R;
-}
-
-struct ShrinkArgs {
-    Args g;
-    const void* x;                 // [T] rows of C values, row stride ld
-    int64_t ld;
-    int C;
-    const void* const* m;          // [n] matrices [r][C]
-    int scaled;                    // by the adapter's scale
-    float* v;                      // [T][R]; columns beyond the rank get 0
-};
 
 // One tile of 16 tokens a workgroup, its waves a part of the columns each.
 template <bool BF, int RT>
@@ -110,23 +85,19 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs a) {
     }
 }
 
-struct ExpandArgs {
-    Args g;
-    const float* v;                // [T][R]
-    const void* const* m;          // [n] matrices [r][C]
-    int C, scaled;
-    const void* base;              // [T] rows of C values, row stride ld_base, or null: 0
-    int64_t ld_base;
-    void* y;                       // out, row stride ld
-    int64_t ld;
-};
-
 // One tile of 16 tokens and 256 columns a workgroup, 64 columns a wave: the lane
 // (c, q) feeds columns 4 c + j of row 4 q + i and gets columns 16 q .. + 15 of token c.
 template <bool BF, bool YBF>
 __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
     if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[0]) return;
     const Tile tile = a.g.plan.tiles[0][blockIdx.x];
+    if (a.v_out && a.parts > 1 && blockIdx.y == 0 && tile.adapter >= 0)
+        for (int i = threadIdx.x; i < tile.count * a.g.R; i += kThreads) {
+            const int64_t at = int64_t(a.g.plan.order[tile.first + i / a.g.R]) * a.g.R + i % a.g.R;
+            float sum = 0.f;
+            for (int p = 0; p < a.parts; ++p) sum += a.v[int64_t(p) * a.g.T * a.g.R + at];
+            a.v_out[at] = sum;
+        }
     if (tile.adapter < 0 && a.base == a.y) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int o0 = (blockIdx.y * kWaves + wave) * 64;
@@ -142,7 +113,9 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
         if (a.scaled && a.g.scales) s = a.g.scales[tile.adapter];
         for (int r0 = 0; r0 < rank; r0 += 4) {
             const int r = r0 + q;
-            const float vv = in && r < rank ? a.v[int64_t(t) * a.g.R + r] : 0.f;
+            float vv = 0.f;
+            if (in && r < rank)
+                for (int p = 0; p < a.parts; ++p) vv += a.v[(int64_t(p) * a.g.T + t) * a.g.R + r];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int o = o0 + 4 * c + j;
@@ -224,6 +197,21 @@ __global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs a) {
     }
 }
 
+// Tiles of 64 tokens where adapters have that many on average.
+bool large_tiles(int T, int n) { return T >= 64 * n && T > 64; }
+
+// Parts of a token's columns, a workgroup each, where there are few tiles.
+int column_parts(int T, int n, int C) {
+    const int tiles = large_tiles(T, n) ? T / 64 + n : T / 16 + (T < n ? T : n);
+    int p = 1;
+    while (p < 8 && tiles * p < 256 && C / (2 * p) >= 512) p *= 2;
+    return p;
+}
+
+// Rows of all parts of T tokens at most (parts times tokens, by column_parts), which
+// never falls as T grows.
+int part_rows(int T) { return T < 4096 ? 8 * T : T < 32768 ? 32768 : T; }
+
 // Calls f(16-row tiles of the rank).
 template <class F>
 void with_rank(int R, F f) {
@@ -262,6 +250,27 @@ int outer(const OuterArgs& a, bool bf, hipStream_t s) {
     return STMOE_OK;
 }
 
+// The two products over a token's columns and over the rank, one after the other,
+// by the kernels that their rows allow.
+int shrink_expand(ShrinkArgs sh, ExpandArgs ex, int dtype, int ydtype, hipStream_t s) {
+    const PlanLayout y = plan_layout(sh.g.T, sh.g.n);
+    const bool bf = dtype == STMOE_BF16, ybf = ydtype == STMOE_BF16;
+    const int esz = bf ? 2 : 4, ysz = ybf ? 2 : 4;
+    const bool fast_shrink = bf && chunks16(sh.x, sh.ld, sh.C, esz);
+    const bool fast_expand = bf && ex.C % 8 == 0 && chunks16(ex.y, ex.ld, ex.C, ysz) &&
+                             (!ex.base || chunks16(ex.base, ex.ld_base, ex.C, ysz));
+    const int table = large_tiles(sh.g.T, sh.g.n) ? 1 : 0;
+    if (!fast_shrink || sh.parts == 1) {
+        // one part: where the caller wants it
+        sh.parts = ex.parts = 1;
+        if (ex.v_out) sh.v = ex.v_out;
+        ex.v = sh.v;
+    }
+    if (int rc = fast_shrink ? shrink_bf16(sh, table, s) : shrink(sh, y.max_tiles[0], bf, s)) return rc;
+    if (!ex.y) return STMOE_OK;
+    return fast_expand ? expand_bf16(ex, table, ybf, s) : expand(ex, y.max_tiles[0], bf, ybf, s);
+}
+
 size_t rows_bytes(int T, int R) { return (size_t(T) * R * sizeof(float) + 255) / 256 * 256; }
 
 bool bad_shape(int T, int Hin, int Hout, int n, int R, int dtype) {
@@ -293,7 +302,7 @@ using namespace stmoe;
 using namespace stmoe::lora;
 
 extern "C" size_t moe_lora_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype) {
-    return bad_shape(T, Hin, Hout, n_adapters, R, dtype) ? 0 : rows_bytes(T, R) + 256;
+    return bad_shape(T, Hin, Hout, n_adapters, R, dtype) ? 0 : rows_bytes(part_rows(T), R) + 256;
 }
 
 extern "C" int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapters, int R, int dtype, int ydtype,
@@ -314,16 +323,15 @@ extern "C" int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, in
                 "ws and plan must be 256-byte aligned");
     STMOE_CHECK(reinterpret_cast<uintptr_t>(v) % 16 == 0, "v must be 16-byte aligned");
     const Args g{plan_of(plan, T, n_adapters), T, n_adapters, R, ranks, scales};
-    const int tiles = plan_layout(T, n_adapters).max_tiles[0];
-    if (!v) v = reinterpret_cast<float*>(ws);
-    hipStream_t s = as_stream(stream);
-    const bool bf = dtype == STMOE_BF16;
-    if (int rc = shrink(ShrinkArgs{g, x, ldx, Hin, a_ptrs, 0, v}, tiles, bf, s)) return rc;
-    return expand(ExpandArgs{g, v, b_ptrs, Hout, 1, base, ld_base, y, ldy}, tiles, bf, ydtype == STMOE_BF16, s);
+    const int parts = column_parts(T, n_adapters, Hin);
+    float* mine = reinterpret_cast<float*>(ws);
+    return shrink_expand(ShrinkArgs{g, x, ldx, Hin, a_ptrs, 0, mine, parts},
+                         ExpandArgs{g, mine, parts, v, b_ptrs, Hout, 1, base, ld_base, y, ldy}, dtype, ydtype,
+                         as_stream(stream));
 }
 
 extern "C" size_t moe_lora_backward_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype) {
-    return bad_shape(T, Hin, Hout, n_adapters, R, dtype) ? 0 : rows_bytes(T, R) + 256;
+    return bad_shape(T, Hin, Hout, n_adapters, R, dtype) ? 0 : rows_bytes(T, R) + rows_bytes(part_rows(T), R) + 256;
 }
 
 extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int64_t ld_dy, const float* v, int T, int Hin,
@@ -347,13 +355,15 @@ extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int
                 "ws and plan must be 256-byte aligned");
     STMOE_CHECK(reinterpret_cast<uintptr_t>(v) % 16 == 0, "v must be 16-byte aligned");
     const Args g{plan_of(plan, T, n_adapters), T, n_adapters, R, ranks, scales};
-    const int tiles = plan_layout(T, n_adapters).max_tiles[0];
     float* u = reinterpret_cast<float*>(ws);
     hipStream_t s = as_stream(stream);
     const bool bf = dtype == STMOE_BF16;
-    if (int rc = shrink(ShrinkArgs{g, dy, ld_dy, Hout, b_ptrs, 1, u}, tiles, bf, s)) return rc;
+    // where dx is wanted, its launch adds the parts of u up
+    const int parts = dx ? column_parts(T, n_adapters, Hout) : 1;
+    float* mine = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + rows_bytes(T, R));
+    if (int rc = shrink_expand(ShrinkArgs{g, dy, ld_dy, Hout, b_ptrs, 1, mine, parts},
+                               ExpandArgs{g, mine, parts, u, a_ptrs, Hin, 0, base, ld_base, dx, ld_dx}, dtype, dtype, s))
+        return rc;
     if (int rc = outer(OuterArgs{g, dy, ld_dy, Hout, v, 1, db_ptrs}, bf, s)) return rc;
-    if (int rc = outer(OuterArgs{g, x, ldx, Hin, u, 0, da_ptrs}, bf, s)) return rc;
-    if (!dx) return STMOE_OK;
-    return expand(ExpandArgs{g, u, a_ptrs, Hin, 0, base, ld_base, dx, ld_dx}, tiles, bf, bf, s);
+    return outer(OuterArgs{g, x, ldx, Hin, u, 0, da_ptrs}, bf, s);
 }
