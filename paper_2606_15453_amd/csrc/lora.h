@@ -46,7 +46,24 @@ struct ExpandArgs {
     int64_t ld;
 };
 
+struct OuterArgs {
+    Args g;
+    const void* x;                 // [T] rows of C values, row stride ld
+    int64_t ld;
+    int C;
+    const float* u;                // [T][R]
+    int scaled;
+    float* const* d;               // [n] gradients [r][C], out
+    float* part;                   // [outer_slots][R][C] sums of tiles of adapters with several
+};
+
+// A tile's place among the sums of adapters with several tiles: two of their tiles
+// start within `size` tokens only if the first is an adapter's last.
+__host__ __device__ inline int outer_slot(int first, int size, bool last) { return 2 * (first / size) + last; }
+inline size_t outer_slots(int T, int size) { return 2 * (size_t(T) / size + 1); }
+
 // lora_bf16.hip
+int outer_bf16(const OuterArgs (&a)[2], int table, hipStream_t s);
 int shrink_bf16(const ShrinkArgs& a, int table, hipStream_t s);
 int expand_bf16(const ExpandArgs& a, int table, bool ybf, hipStream_t s);
 

@@ -136,16 +136,6 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
         }
 }
 
-struct OuterArgs {
-    Args g;
-    const void* x;                 // [T] rows of C values, row stride ld
-    int64_t ld;
-    int C;
-    const float* u;                // [T][R]
-    int scaled;
-    float* const* d;               // [n] gradients [r][C], out
-};
-
 // One adapter and 64 columns a workgroup, its waves a part of the tokens each.
 template <bool BF, int RT>
 __global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs a) {
@@ -211,6 +201,13 @@ int column_parts(int T, int n, int C) {
 // Rows of all parts of T tokens at most (parts times tokens, by column_parts), which
 // never falls as T grows.
 int part_rows(int T) { return T < 4096 ? 8 * T : T < 32768 ? 32768 : T; }
+
+// Tokens per tile of the sums over tokens: 256, and 1024 for ranks above 16, whose sums
+// (R x C fp32 a tile) would be as many bytes as the rows.
+int outer_table(int, int, int R) { return R <= 16 ? 2 : 3; }
+size_t outer_bytes(int T, int Hin, int Hout, int R) {
+    return outer_slots(T, tile_tokens(outer_table(T, 1, R))) * R * (size_t(Hin) + Hout) * sizeof(float);
+}
 
 // Calls f(16-row tiles of the rank).
 template <class F>
@@ -331,7 +328,8 @@ extern "C" int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, in
 }
 
 extern "C" size_t moe_lora_backward_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype) {
-    return bad_shape(T, Hin, Hout, n_adapters, R, dtype) ? 0 : rows_bytes(T, R) + rows_bytes(part_rows(T), R) + 256;
+    return bad_shape(T, Hin, Hout, n_adapters, R, dtype) ? 0
+               : rows_bytes(T, R) + rows_bytes(part_rows(T), R) + outer_bytes(T, Hin, Hout, R) + 256;
 }
 
 extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int64_t ld_dy, const float* v, int T, int Hin,
@@ -364,6 +362,11 @@ extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int
     if (int rc = shrink_expand(ShrinkArgs{g, dy, ld_dy, Hout, b_ptrs, 1, mine, parts},
                                ExpandArgs{g, mine, parts, u, a_ptrs, Hin, 0, base, ld_base, dx, ld_dx}, dtype, dtype, s))
         return rc;
-    if (int rc = outer(OuterArgs{g, dy, ld_dy, Hout, v, 1, db_ptrs}, bf, s)) return rc;
-    return outer(OuterArgs{g, x, ldx, Hin, u, 0, da_ptrs}, bf, s);
+    const int table = outer_table(T, n_adapters, R);
+    float* sums = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + rows_bytes(T, R) + rows_bytes(part_rows(T), R));
+    const OuterArgs o[2] = {{g, x, ldx, Hin, u, 0, da_ptrs, sums},
+                            {g, dy, ld_dy, Hout, v, 1, db_ptrs, sums + outer_slots(T, tile_tokens(table)) * R * Hin}};
+    if (bf && chunks16(x, ldx, Hin, 2) && chunks16(dy, ld_dy, Hout, 2)) return outer_bf16(o, table, s);
+    if (int rc = outer(o[1], bf, s)) return rc;
+    return outer(o[0], bf, s);
 }

@@ -271,7 +271,143 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
     }
 }
 
+// d = u^T x of a tile of tokens (a gradient, or its sum of an adapter with several
+// tiles).  512 columns and up to 64 ranks a workgroup, 128 columns a wave, 32 tokens at
+// a time: the lane (c, q) loads columns 8 c .. + 7 of tokens 8 q .. + 7, the row operand
+// of instruction j being columns 8 c + j; u's three pieces are made once for the
+// workgroup, in LDS.
+template <int RT>
+__global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox, OuterArgs oy, int table) {
+    constexpr int P = 3;
+    __shared__ u32x4 uf[2][RT][P][64];
+    const OuterArgs& a = blockIdx.z & 1 ? oy : ox;
+    const int rt0 = (blockIdx.z >> 1) * 64;
+    if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[table]) return;
+    const Tile tile = a.g.plan.tiles[table][blockIdx.x];
+    if (tile.adapter < 0 || int(blockIdx.y) * 128 * kWaves >= a.C) return;
+    const int R = a.g.R, rank = rank_of(a.g, tile.adapter);
+    if (rt0 >= rank) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
+    const int h0 = (blockIdx.y * kWaves + wave) * 128, h = h0 + 8 * c;
+    const bool cols = h < a.C;
+    const char* x = reinterpret_cast<const char*>(a.x) + 2 * h;
+    const int32_t* order = a.g.plan.order + tile.first;
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    f32x4 acc[RT][8];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // thread: rank ur, tokens 8 uq .. + 7 of u
+    auto load_u = [&](int k0, float (&u)[8], int i) {
+        const int at = threadIdx.x + i * kThreads, ur = rt0 + (at / 64) * 16 + (at & 15), uq = (at >> 4) & 3;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int p = k0 + 8 * uq + k;
+            u[k] = p < tile.count && ur < rank && at < 64 * RT ? a.u[int64_t(order[p]) * R + ur] : 0.f;
+        }
+    };
+    auto load_x = [&](int k0, u32x4 (&rows)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int p = k0 + 8 * q + k;
+            rows[k] = cols && p < tile.count ? *reinterpret_cast<const u32x4*>(x + 2 * (int64_t(order[p]) * a.ld)) : zero;
+        }
+    };
+    constexpr int UN = (64 * RT + kThreads - 1) / kThreads;
+    float u[UN][8];
+    u32x4 rows[8];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) load_u(0, u[i], i);
+    load_x(0, rows);
+    int buf = 0;
+    for (int k0 = 0; k0 < tile.count; k0 += 32, buf ^= 1) {
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int at = threadIdx.x + i * kThreads;
+            if (at >= 64 * RT) continue;
+            bf16x8 p[P];
+            split(u[i], p);
+#pragma unroll
+            for (int j = 0; j < P; ++j) *reinterpret_cast<bf16x8*>(&uf[buf][at / 64][j][at & 63]) = p[j];
+        }
+        bf16x8 xf[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) xf[j] = column(rows, j);
+        // the next tokens are on their way while these are used
+        if (k0 + 32 < tile.count) {
+#pragma unroll
+            for (int i = 0; i < UN; ++i) load_u(k0 + 32, u[i], i);
+            load_x(k0 + 32, rows);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p) {
+                const bf16x8 b = operand(uf[buf][i][p][lane]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[i][j] = mfma(xf[j], b, acc[i][j]);
+            }
+    }
+    const int tiles = a.g.plan.base[table][tile.adapter + 1] - a.g.plan.base[table][tile.adapter];
+    const float s = a.scaled && a.g.scales ? a.g.scales[tile.adapter] : 1.f;
+    float* d = tiles == 1 ? a.d[tile.adapter]
+                          : a.part + int64_t(outer_slot(tile.first, tile_tokens(table), tile.piece == tiles - 1)) * R * a.C;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int r = rt0 + 16 * i + c;
+        if (r >= rank) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int o = h0 + 32 * q + 8 * k;
+            if (o >= a.C) continue;
+            f32x4* out = reinterpret_cast<f32x4*>(d + int64_t(r) * a.C + o);
+            out[0] = f32x4{s * acc[i][0][k], s * acc[i][1][k], s * acc[i][2][k], s * acc[i][3][k]};
+            out[1] = f32x4{s * acc[i][4][k], s * acc[i][5][k], s * acc[i][6][k], s * acc[i][7][k]};
+        }
+    }
+}
+
+// The gradients of adapters with several tiles, their sums in order, and of those
+// without a token: zeros.
+__global__ __launch_bounds__(kThreads) void lora_join_kernel(OuterArgs ox, OuterArgs oy, int table) {
+    const OuterArgs& a = blockIdx.z ? oy : ox;
+    if (!planned(a.g)) return;
+    const int ad = blockIdx.x, size = tile_tokens(table);
+    const int tiles = a.g.plan.base[table][ad + 1] - a.g.plan.base[table][ad];
+    if (tiles == 1) return;
+    const int first = a.g.plan.seg[ad];
+    const int64_t all = int64_t(rank_of(a.g, ad)) * a.C, part = int64_t(a.g.R) * a.C;
+    float* d = a.d[ad];
+    for (int64_t i = 4 * (int64_t(blockIdx.y) * kThreads + threadIdx.x); i < all; i += 4 * int64_t(gridDim.y) * kThreads) {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int k = 0; k < tiles; ++k)
+            sum += *reinterpret_cast<const f32x4*>(a.part + outer_slot(first + k * size, size, k == tiles - 1) * part + i);
+        *reinterpret_cast<f32x4*>(d + i) = sum;
+    }
+}
+
 }  // namespace
+
+int outer_bf16(const OuterArgs (&a)[2], int table, hipStream_t s) {
+    const int R = a[0].g.R, C = a[0].C > a[1].C ? a[0].C : a[1].C, n = a[0].g.n;
+    const dim3 grid(unsigned(plan_layout(a[0].g.T, n).max_tiles[table]), unsigned((C + 128 * kWaves - 1) / (128 * kWaves)),
+                    R > 64 ? 4 : 2);
+    const auto go = [&](auto rt) {
+        hipLaunchKernelGGL((lora_outer_bf16_kernel<rt()>), grid, dim3(kThreads), 0, s, a[0], a[1], table);
+    };
+    if (R <= 16) go(std::integral_constant<int, 1>());
+    else if (R <= 32) go(std::integral_constant<int, 2>());
+    else go(std::integral_constant<int, 4>());
+    STMOE_LAUNCHED();
+    const int64_t chunks = (int64_t(R) * C / 4 + kThreads - 1) / kThreads, most = n < 64 ? 512 / n : 8;
+    hipLaunchKernelGGL(lora_join_kernel, dim3(unsigned(n), unsigned(chunks < most ? chunks : most), 2), dim3(kThreads), 0, s,
+                       a[0], a[1], table);
+    STMOE_LAUNCHED();
+    return STMOE_OK;
+}
 
 int shrink_bf16(const ShrinkArgs& a, int table, hipStream_t s) {
     const int tiles = plan_layout(a.g.T, a.g.n).max_tiles[table];

@@ -13,9 +13,10 @@ constexpr int kMaxRank = 128;
 constexpr int kMaxCols = 65536;
 constexpr int kPlanThreads = 1024;         // tokens that one workgroup sorts
 
-// tokens per tile of the three tables
-constexpr int kTables = 3;
-__host__ __device__ constexpr int tile_tokens(int s) { return s == 0 ? 16 : s == 1 ? 64 : 256; }
+// tokens per tile of the tables: two for the products of single tokens, two for sums
+// over tokens
+constexpr int kTables = 4;
+__host__ __device__ constexpr int tile_tokens(int s) { return 16 << (2 * s); }
 
 struct Tile {
     int32_t adapter;               // -1: tokens without one
