@@ -115,26 +115,42 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
         for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const u32x4 zero = {0u, 0u, 0u, 0u};
     const int step = 64 * kWaves * int(gridDim.y);
-    if (rank > 0)
-#pragma unroll 2
-        for (int h0 = 64 * (blockIdx.y * kWaves + wave); h0 < a.C; h0 += step) {
-            u32x4 xv[NT][2], mv[RT][2];
+    struct Chunk {
+        u32x4 x[NT][2], m[RT][2];
+    };
+    auto load = [&](int h0, Chunk& v) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int h = h0 + 16 * q + 8 * u;
-                const bool in = h < a.C;       // C is a multiple of 8
+        for (int u = 0; u < 2; ++u) {
+            const int h = h0 + 16 * q + 8 * u;
+            const bool in = h < a.C;       // C is a multiple of 8
 #pragma unroll
-                for (int i = 0; i < NT; ++i) xv[i][u] = in ? *reinterpret_cast<const u32x4*>(xr[i] + 2 * h) : zero;
+            for (int i = 0; i < NT; ++i) v.x[i][u] = in ? *reinterpret_cast<const u32x4*>(xr[i] + 2 * int64_t(h)) : zero;
 #pragma unroll
-                for (int i = 0; i < RT; ++i) mv[i][u] = in ? *reinterpret_cast<const u32x4*>(mr[i] + 2 * h) : zero;
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int j = 0; j < RT; ++j)
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) acc[i][j] = mfma(operand(mv[j][u]), operand(xv[i][u]), acc[i][j]);
+            for (int i = 0; i < RT; ++i) v.m[i][u] = in ? *reinterpret_cast<const u32x4*>(mr[i] + 2 * int64_t(h)) : zero;
         }
+    };
+    auto use = [&](const Chunk& v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < RT; ++j)
+#pragma unroll
+                for (int i = 0; i < NT; ++i) acc[i][j] = mfma(operand(v.m[j][u]), operand(v.x[i][u]), acc[i][j]);
+    };
+    // the next columns are on their way while these are used
+    int h0 = 64 * (blockIdx.y * kWaves + wave);
+    if (rank > 0 && h0 < a.C) {
+        Chunk v0, v1;
+        load(h0, v0);
+        for (;;) {
+            load(h0 + step, v1);
+            use(v0);
+            if ((h0 += step) >= a.C) break;
+            load(h0 + step, v0);
+            use(v1);
+            if ((h0 += step) >= a.C) break;
+        }
+    }
     // the waves' sums, two and two
     auto at = [&](int b, int i, int j) { return reinterpret_cast<f32x4*>(&red[b][16 * i + c][16 * j + 4 * q]); };
     if (wave >= 2)
@@ -158,91 +174,100 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
     }
 }
 
-// y = base + s v B.  A tile of tokens and 512 columns a workgroup, 128 a wave, whose
-// lane (c, q) holds columns 8 c .. + 7 of ranks 8 q .. + 7 (of every 32) as the row
-// operand, rows (columns of B) being 8 c + j for instruction j: it gets columns
-// 32 q .. + 31 of token c.  With a rank of 16 at most the lanes q = 2, 3 hold the same
-// ranks as q = 0, 1, against the second piece of v.
-template <int KS, bool PACK, bool YBF>
+// y = base + s v B.  A tile of up to 16 NS tokens and 512 columns a workgroup, 128 a
+// wave, whose lane (c, q) holds columns 8 c .. + 7 of ranks 8 q .. + 7 (of every 32) as
+// the row operand, rows (columns of B) being 8 c + j for instruction j: it gets columns
+// 32 q .. + 31 of token c.  v's pieces are made once for the workgroup, in LDS.  With a
+// rank of 16 at most the lanes q = 2, 3 hold the same ranks as q = 0, 1, against the
+// second piece of v.
+template <int KS, bool PACK, bool YBF, int NS>
 __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a, int table) {
-    constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P;
+    constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P, W = YBF ? 1 : 2;
+    __shared__ u32x4 vf[NS][NM][64];
     if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[table]) return;
     const Tile tile = a.g.plan.tiles[table][blockIdx.x];
     const int R = a.g.R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int64_t part = int64_t(a.g.T) * R;
+    const int32_t* order = a.g.plan.order + tile.first;
     if (a.v_out && a.parts > 1 && blockIdx.y == 0 && tile.adapter >= 0)
         for (int i = threadIdx.x; i < tile.count * R; i += kThreads) {
-            const int64_t at = int64_t(a.g.plan.order[tile.first + i / R]) * R + i % R;
+            const int64_t at = int64_t(order[i / R]) * R + i % R;
             float sum = 0.f;
             for (int p = 0; p < a.parts; ++p) sum += a.v[p * part + at];
             a.v_out[at] = sum;
         }
     if (tile.adapter < 0 && a.base == a.y) return;
     const int o0 = (blockIdx.y * kWaves + wave) * 128;
-    if (o0 >= a.C) return;
     const u32x4 zero = {0u, 0u, 0u, 0u};
+    int32_t t[NS];
+#pragma unroll
+    for (int k = 0; k < NS; ++k) t[k] = order[16 * k + c < tile.count ? 16 * k + c : 0];
+    // base: four chunks of eight columns
+    auto load_base = [&](int k, u32x4 (&b)[4][W]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int o = o0 + 32 * q + 8 * i;
+            const bool in = a.base && 16 * k + c < tile.count && o < a.C;
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                b[i][w] = in ? reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.base) +
+                                                              (YBF ? 2 : 4) * (t[k] * a.ld_base + o))[w]
+                             : zero;
+        }
+    };
     bf16x8 mf[KS][8];
+    u32x4 b0[4][W], b1[4][W];
     float s = 0.f;
     if (tile.adapter >= 0) {
         const int rank = rank_of(a.g, tile.adapter);
         const char* m = reinterpret_cast<const char*>(a.m[tile.adapter]);
         s = a.scaled && a.g.scales ? a.g.scales[tile.adapter] : 1.f;
+        u32x4 rows[KS][8];
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            u32x4 rows[8];
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r = 32 * k + 8 * (PACK ? q & 1 : q) + i, o = o0 + 8 * c;
-                rows[i] = r < rank && o < a.C ? *reinterpret_cast<const u32x4*>(m + 2 * (int64_t(r) * a.C + o)) : zero;
+                rows[k][i] = r < rank && o < a.C ? *reinterpret_cast<const u32x4*>(m + 2 * (int64_t(r) * a.C + o)) : zero;
             }
+        load_base(0, b0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) mf[k][j] = column(rows, j);
+        for (int i = threadIdx.x; i < 64 * NS * KS; i += kThreads) {
+            const int l = i & 63, k = (i >> 6) % KS, n = (i >> 6) / KS, lq = l >> 4, lt = 16 * n + (l & 15);
+            if (16 * n >= tile.count) break;
+            float v[8];
+            load8(a.v + int64_t(order[lt < tile.count ? lt : 0]) * R, part, a.parts, 32 * k + 8 * (PACK ? lq & 1 : lq), R, v);
+            bf16x8 p[P];
+            split(v, p);
+            if constexpr (PACK) {
+                *reinterpret_cast<bf16x8*>(&vf[n][0][l]) = lq < 2 ? p[0] : p[1];
+                if constexpr (P == 3) *reinterpret_cast<bf16x8*>(&vf[n][1][l]) = lq < 2 ? p[2] : operand(zero);
+            } else {
+#pragma unroll
+                for (int j = 0; j < P; ++j) *reinterpret_cast<bf16x8*>(&vf[n][P * k + j][l]) = p[j];
+            }
         }
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mf[k][j] = column(rows[k], j);
+    } else {
+        load_base(0, b0);
     }
-    for (int k0 = 0; k0 < tile.count; k0 += 16) {
-        const bool in = k0 + c < tile.count;
-        const int64_t t = a.g.plan.order[tile.first + (in ? k0 + c : 0)];
-        // base: four chunks of eight columns
-        constexpr int W = YBF ? 1 : 2;
-        u32x4 b[4][W];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const int o = o0 + 32 * q + 8 * i;
-                b[i][w] = a.base && in && o < a.C
-                              ? reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.base) +
-                                                               (YBF ? 2 : 4) * (t * a.ld_base + o))[w]
-                              : zero;
-            }
+    __syncthreads();
+    auto finish = [&](int k, const u32x4 (&b)[4][W]) __attribute__((always_inline)) {
         f32x4 acc[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (tile.adapter >= 0) {
-            bf16x8 vf[NM];
-            float v[8];
-            if constexpr (PACK) {
-                load8(a.v + t * R, part, a.parts, 8 * (q & 1), R, v);
-                bf16x8 p[P];
-                split(v, p);
-                vf[0] = q < 2 ? p[0] : p[1];
-                if constexpr (P == 3) vf[1] = q < 2 ? p[2] : operand(zero);
-            } else {
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    load8(a.v + t * R, part, a.parts, 32 * k + 8 * q, R, v);
-                    bf16x8 p[P];
-                    split(v, p);
+            for (int i = NM - 1; i >= 0; --i) {
+                const bf16x8 v = operand(vf[k][i][lane]);
 #pragma unroll
-                    for (int i = 0; i < P; ++i) vf[P * k + i] = p[i];
-                }
+                for (int j = 0; j < 8; ++j) acc[j] = mfma(mf[PACK ? 0 : i / P][j], v, acc[j]);
             }
-#pragma unroll
-            for (int i = NM - 1; i >= 0; --i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] = mfma(mf[PACK ? 0 : i / P][j], vf[i], acc[j]);
         }
-        if (!in) continue;
+        if (16 * k + c >= tile.count) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int o = o0 + 32 * q + 8 * i;
@@ -251,10 +276,10 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float f = YBF ? (j % 2 ? bf16_hi(b[i][0][j / 2]) : bf16_lo(b[i][0][j / 2]))
-                                    : __uint_as_float(b[i][W - 1 ? j / 4 : 0][j % 4]);
+                                    : __uint_as_float(b[i][W == 2 ? j / 4 : 0][j % 4]);
                 y[j] = tile.adapter >= 0 ? f + s * acc[j][i] : f;
             }
-            char* out = reinterpret_cast<char*>(a.y) + (YBF ? 2 : 4) * (t * a.ld + o);
+            char* out = reinterpret_cast<char*>(a.y) + (YBF ? 2 : 4) * (t[k] * a.ld + o);
             if constexpr (YBF) {
                 union {
                     __bf16 h[8];
@@ -268,18 +293,30 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
                 reinterpret_cast<f32x4*>(out)[1] = f32x4{y[4], y[5], y[6], y[7]};
             }
         }
+    };
+    // the next tokens' base is on its way while these are finished
+#pragma unroll
+    for (int k = 0; k < NS; k += 2) {
+        if (16 * k >= tile.count) break;
+        if (k + 1 < NS) load_base(k + 1, b1);
+        finish(k, b0);
+        if (k + 1 >= NS || 16 * (k + 1) >= tile.count) break;
+        if (k + 2 < NS) load_base(k + 2, b0);
+        finish(k + 1, b1);
     }
 }
 
 // d = u^T x of a tile of tokens (a gradient, or its sum of an adapter with several
 // tiles).  512 columns and up to 64 ranks a workgroup, 128 columns a wave, 32 tokens at
 // a time: the lane (c, q) loads columns 8 c .. + 7 of tokens 8 q .. + 7, the row operand
-// of instruction j being columns 8 c + j; u's three pieces are made once for the
-// workgroup, in LDS.
+// of instruction j being columns 8 c + j.  u's three pieces are made once for the
+// workgroup, in LDS, 128 tokens at a time.
+constexpr int kStage = 4;          // times 32 tokens
 template <int RT>
 __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox, OuterArgs oy, int table) {
     constexpr int P = 3;
-    __shared__ u32x4 uf[2][RT][P][64];
+    __shared__ u32x4 uf[kStage][RT][P][64];
+    __shared__ int32_t order[tile_tokens(kTables - 1)];
     const OuterArgs& a = blockIdx.z & 1 ? oy : ox;
     const int rt0 = (blockIdx.z >> 1) * 64;
     if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[table]) return;
@@ -287,68 +324,68 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
     if (tile.adapter < 0 || int(blockIdx.y) * 128 * kWaves >= a.C) return;
     const int R = a.g.R, rank = rank_of(a.g, tile.adapter);
     if (rt0 >= rank) return;
+    for (int i = threadIdx.x; i < tile.count; i += kThreads) order[i] = a.g.plan.order[tile.first + i];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int h0 = (blockIdx.y * kWaves + wave) * 128, h = h0 + 8 * c;
     const bool cols = h < a.C;
-    const char* x = reinterpret_cast<const char*>(a.x) + 2 * h;
-    const int32_t* order = a.g.plan.order + tile.first;
+    const char* x = reinterpret_cast<const char*>(a.x) + 2 * int64_t(h);
     const u32x4 zero = {0u, 0u, 0u, 0u};
     f32x4 acc[RT][8];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // thread: rank ur, tokens 8 uq .. + 7 of u
-    auto load_u = [&](int k0, float (&u)[8], int i) {
-        const int at = threadIdx.x + i * kThreads, ur = rt0 + (at / 64) * 16 + (at & 15), uq = (at >> 4) & 3;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int p = k0 + 8 * uq + k;
-            u[k] = p < tile.count && ur < rank && at < 64 * RT ? a.u[int64_t(order[p]) * R + ur] : 0.f;
-        }
-    };
-    auto load_x = [&](int k0, u32x4 (&rows)[8]) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int p = k0 + 8 * q + k;
-            rows[k] = cols && p < tile.count ? *reinterpret_cast<const u32x4*>(x + 2 * (int64_t(order[p]) * a.ld)) : zero;
-        }
-    };
-    constexpr int UN = (64 * RT + kThreads - 1) / kThreads;
-    float u[UN][8];
-    u32x4 rows[8];
-#pragma unroll
-    for (int i = 0; i < UN; ++i) load_u(0, u[i], i);
-    load_x(0, rows);
-    int buf = 0;
-    for (int k0 = 0; k0 < tile.count; k0 += 32, buf ^= 1) {
-#pragma unroll
-        for (int i = 0; i < UN; ++i) {
-            const int at = threadIdx.x + i * kThreads;
-            if (at >= 64 * RT) continue;
-            bf16x8 p[P];
-            split(u[i], p);
-#pragma unroll
-            for (int j = 0; j < P; ++j) *reinterpret_cast<bf16x8*>(&uf[buf][at / 64][j][at & 63]) = p[j];
-        }
-        bf16x8 xf[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) xf[j] = column(rows, j);
-        // the next tokens are on their way while these are used
-        if (k0 + 32 < tile.count) {
-#pragma unroll
-            for (int i = 0; i < UN; ++i) load_u(k0 + 32, u[i], i);
-            load_x(k0 + 32, rows);
-        }
-        __syncthreads();
+    // thread: rank c of tile i, tokens 8 q .. + 7 of the wave's 32
+    float u[RT][8];
+    auto load_u = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
-            for (int p = P - 1; p >= 0; --p) {
-                const bf16x8 b = operand(uf[buf][i][p][lane]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] = mfma(xf[j], b, acc[i][j]);
+            for (int k = 0; k < 8; ++k) {
+                const int p = k0 + 32 * wave + 8 * q + k, r = rt0 + 16 * i + c;
+                u[i][k] = p < tile.count && r < rank ? a.u[int64_t(order[p]) * R + r] : 0.f;
             }
+    };
+    auto load_x = [&](int k0, u32x4 (&rows)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int p = k0 + 8 * q + k;
+            rows[k] = cols && p < tile.count ? *reinterpret_cast<const u32x4*>(x + 2 * (order[p] * a.ld)) : zero;
+        }
+    };
+    u32x4 rows[2][8];
+    __syncthreads();
+    load_u(0);
+    load_x(0, rows[0]);
+    load_x(32, rows[1]);
+    for (int k0 = 0; k0 < tile.count; k0 += 32 * kStage) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            bf16x8 p[P];
+            split(u[i], p);
+#pragma unroll
+            for (int j = 0; j < P; ++j) *reinterpret_cast<bf16x8*>(&uf[wave][i][j][lane]) = p[j];
+        }
+        load_u(k0 + 32 * kStage);
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kStage; ++n) {
+            if (k0 + 32 * n >= tile.count) break;
+            bf16x8 xf[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) xf[j] = column(rows[n & 1], j);
+            // two loads of 32 tokens are on their way while these are used
+            load_x(k0 + 32 * (n + 2), rows[n & 1]);
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int p = P - 1; p >= 0; --p) {
+                    const bf16x8 b = operand(uf[n][i][p][lane]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[i][j] = mfma(xf[j], b, acc[i][j]);
+                }
+        }
     }
     const int tiles = a.g.plan.base[table][tile.adapter + 1] - a.g.plan.base[table][tile.adapter];
     const float s = a.scaled && a.g.scales ? a.g.scales[tile.adapter] : 1.f;
@@ -373,13 +410,12 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
 // without a token: zeros.
 __global__ __launch_bounds__(kThreads) void lora_join_kernel(OuterArgs ox, OuterArgs oy, int table) {
     const OuterArgs& a = blockIdx.z ? oy : ox;
-    if (!planned(a.g)) return;
     const int ad = blockIdx.x, size = tile_tokens(table);
-    const int tiles = a.g.plan.base[table][ad + 1] - a.g.plan.base[table][ad];
-    if (tiles == 1) return;
-    const int first = a.g.plan.seg[ad];
+    // side by side
+    const int tiles = a.g.plan.base[table][ad + 1] - a.g.plan.base[table][ad], first = a.g.plan.seg[ad];
     const int64_t all = int64_t(rank_of(a.g, ad)) * a.C, part = int64_t(a.g.R) * a.C;
     float* d = a.d[ad];
+    if (!planned(a.g) || tiles == 1) return;
     for (int64_t i = 4 * (int64_t(blockIdx.y) * kThreads + threadIdx.x); i < all; i += 4 * int64_t(gridDim.y) * kThreads) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
@@ -430,9 +466,13 @@ int shrink_bf16(const ShrinkArgs& a, int table, hipStream_t s) {
 
 int expand_bf16(const ExpandArgs& a, int table, bool ybf, hipStream_t s) {
     const dim3 grid(unsigned(plan_layout(a.g.T, a.g.n).max_tiles[table]), unsigned((a.C + 128 * kWaves - 1) / (128 * kWaves)));
+    const auto with = [&](auto ks, auto pack, auto ns) {
+        if (ybf) hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), true, ns()>), grid, dim3(kThreads), 0, s, a, table);
+        else hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), false, ns()>), grid, dim3(kThreads), 0, s, a, table);
+    };
     const auto go = [&](auto ks, auto pack) {
-        if (ybf) hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), true>), grid, dim3(kThreads), 0, s, a, table);
-        else hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), false>), grid, dim3(kThreads), 0, s, a, table);
+        if (table == 0) with(ks, pack, std::integral_constant<int, 1>());
+        else with(ks, pack, std::integral_constant<int, 4>());
     };
     const int R = a.g.R;
     if (R <= 16) go(std::integral_constant<int, 1>(), std::true_type());
