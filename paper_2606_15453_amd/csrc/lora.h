@@ -11,12 +11,20 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct Args {
     Plan plan;
+    const void* plan_at;           // the whole plan (host)
     int T, n, R;
     const int32_t* ranks;          // [n] or null: all R
     const float* scales;           // [n] or null: 1
 };
 
 __device__ __forceinline__ bool planned(const Args& g) { return g.plan.head->T == g.T && g.plan.head->n == g.n; }
+// Tile i of the table; false where the plan has none.  The tile is loaded beside the
+// plan's head: i is below the table's room.
+__device__ __forceinline__ bool tile_of(const Args& g, int i, Tile& t) {
+    const int T = g.plan.head->T, n = g.plan.head->n, tiles = *g.plan.tiles_n;
+    t = g.plan.tiles[i];
+    return T == g.T && n == g.n && i < tiles;
+}
 __device__ __forceinline__ int rank_of(const Args& g, int a) {
     const int r = g.ranks ? g.ranks[a] : g.R;
     return r < 0 ? 0 : r < g.R ? r : g.R;
@@ -66,6 +74,11 @@ inline size_t outer_slots(int T, int size) { return 2 * (size_t(T) / size + 1); 
 int outer_bf16(const OuterArgs (&a)[2], int table, hipStream_t s);
 int shrink_bf16(const ShrinkArgs& a, int table, hipStream_t s);
 int expand_bf16(const ExpandArgs& a, int table, bool ybf, hipStream_t s);
+
+inline Args with_table(Args g, int table) {
+    g.plan = plan_of(g.plan_at, g.T, g.n, table);
+    return g;
+}
 
 inline bool chunks16(const void* p, int64_t ld, int C, int esz) {
     return C % (16 / esz) == 0 && ld * esz % 16 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;

@@ -42,8 +42,8 @@ __device__ __forceinline__ void put(void* p, int64_t i, float v) {
 template <bool BF, int RT>
 __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs a) {
     __shared__ float part[kWaves][RT * 16][17];
-    if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[0]) return;
-    const Tile tile = a.g.plan.tiles[0][blockIdx.x];
+    Tile tile;
+    if (!tile_of(a.g, blockIdx.x, tile)) return;
     if (tile.adapter < 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int rank = rank_of(a.g, tile.adapter);
@@ -89,8 +89,8 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs a) {
 // (c, q) feeds columns 4 c + j of row 4 q + i and gets columns 16 q .. + 15 of token c.
 template <bool BF, bool YBF>
 __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
-    if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[0]) return;
-    const Tile tile = a.g.plan.tiles[0][blockIdx.x];
+    Tile tile;
+    if (!tile_of(a.g, blockIdx.x, tile)) return;
     if (a.v_out && a.parts > 1 && blockIdx.y == 0 && tile.adapter >= 0)
         for (int i = threadIdx.x; i < tile.count * a.g.R; i += kThreads) {
             const int64_t at = int64_t(a.g.plan.order[tile.first + i / a.g.R]) * a.g.R + i % a.g.R;
@@ -319,7 +319,7 @@ extern "C" int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, in
     STMOE_CHECK(reinterpret_cast<uintptr_t>(ws) % 256 == 0 && reinterpret_cast<uintptr_t>(plan) % 256 == 0,
                 "ws and plan must be 256-byte aligned");
     STMOE_CHECK(reinterpret_cast<uintptr_t>(v) % 16 == 0, "v must be 16-byte aligned");
-    const Args g{plan_of(plan, T, n_adapters), T, n_adapters, R, ranks, scales};
+    const Args g{plan_of(plan, T, n_adapters, 0), plan, T, n_adapters, R, ranks, scales};
     const int parts = column_parts(T, n_adapters, Hin);
     float* mine = reinterpret_cast<float*>(ws);
     return shrink_expand(ShrinkArgs{g, x, ldx, Hin, a_ptrs, 0, mine, parts},
@@ -352,7 +352,7 @@ extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int
     STMOE_CHECK(reinterpret_cast<uintptr_t>(ws) % 256 == 0 && reinterpret_cast<uintptr_t>(plan) % 256 == 0,
                 "ws and plan must be 256-byte aligned");
     STMOE_CHECK(reinterpret_cast<uintptr_t>(v) % 16 == 0, "v must be 16-byte aligned");
-    const Args g{plan_of(plan, T, n_adapters), T, n_adapters, R, ranks, scales};
+    const Args g{plan_of(plan, T, n_adapters, 0), plan, T, n_adapters, R, ranks, scales};
     float* u = reinterpret_cast<float*>(ws);
     hipStream_t s = as_stream(stream);
     const bool bf = dtype == STMOE_BF16;

@@ -56,26 +56,41 @@ __device__ __forceinline__ bf16x8 column(const u32x4 (&rows)[8], int j) {
     return operand(q);
 }
 
-// Eight values of a row of R from r on, 0 beyond it; the sum of its parts.
+// The chunk of eight columns, of 16, that lane c feeds so that the results i of the lanes
+// q (rows 4 q + i) stand side by side: four lanes store 64 bytes of a row.
+__device__ __forceinline__ int chunk(int c) { return (c >> 2) | (c & 3) << 2; }
+
+// Eight values of a row of R from r on, 0 beyond it; the sum of its parts (one or an even
+// number), two at a time.
 __device__ __forceinline__ void load8(const float* row, int64_t part, int parts, int r, int R, float (&v)[8]) {
+    if (R % 8 == 0) {
+        const float* at = row + (r < R ? r : 0);
+        f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 4);
+        if (parts > 1) {
+            lo += *reinterpret_cast<const f32x4*>(at + part);
+            hi += *reinterpret_cast<const f32x4*>(at + part + 4);
+            for (int p = 2; p < parts; p += 2) {
+                const float* a0 = at + p * part;
+                const float* a1 = a0 + part;
+                const f32x4 l0 = *reinterpret_cast<const f32x4*>(a0), h0 = *reinterpret_cast<const f32x4*>(a0 + 4);
+                const f32x4 l1 = *reinterpret_cast<const f32x4*>(a1), h1 = *reinterpret_cast<const f32x4*>(a1 + 4);
+                lo += l0 + l1;
+                hi += h0 + h1;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = r < R ? lo[i] : 0.f;
+            v[4 + i] = r < R ? hi[i] : 0.f;
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    for (int p = 0; p < parts; ++p, row += part) {
-        if (R % 8 == 0) {
-            if (r < R) {
-                const f32x4 lo = *reinterpret_cast<const f32x4*>(row + r), hi = *reinterpret_cast<const f32x4*>(row + r + 4);
+    for (int p = 0; p < parts; ++p, row += part)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[i] += lo[i];
-                    v[4 + i] += hi[i];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r + i < R) v[i] += row[r + i];
-        }
-    }
+        for (int i = 0; i < 8; ++i)
+            if (r + i < R) v[i] += row[r + i];
 }
 
 // v = x A^T.  16 NT tokens a workgroup (a tile, or a part of one) and, with several
@@ -83,14 +98,13 @@ __device__ __forceinline__ void load8(const float* row, int64_t part, int parts,
 // feeds columns 16 q .. + 15 of token c and of rank c: 32 bytes of a row, 128 a quarter
 // wave.
 template <int RT, int NT>
-__global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a, int table) {
+__global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a) {
     constexpr int TOK = 16 * NT, LD = 16 * RT + 4;
     __shared__ __attribute__((aligned(16))) float red[2][TOK][LD];
-    if (!planned(a.g)) return;
-    const int sub = tile_tokens(table) / TOK, ti = blockIdx.x / sub, k0 = (blockIdx.x % sub) * TOK;
-    if (ti >= a.g.plan.head->tiles[table]) return;
-    const Tile tile = a.g.plan.tiles[table][ti];
-    if (tile.adapter < 0 || k0 >= tile.count) return;
+    __shared__ int64_t token[TOK];
+    const int sub = a.g.plan.size / TOK, k0 = (blockIdx.x % sub) * TOK;
+    Tile tile;
+    if (!tile_of(a.g, blockIdx.x / sub, tile) || tile.adapter < 0 || k0 >= tile.count) return;
     const int count = tile.count - k0 < TOK ? tile.count - k0 : TOK, first = tile.first + k0;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int rank = rank_of(a.g, tile.adapter);
@@ -101,7 +115,9 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
         const int k = 16 * i + c;
-        xr[i] = reinterpret_cast<const char*>(a.x) + 2 * (a.g.plan.order[first + (k < count ? k : 0)] * a.ld);
+        const int64_t t = a.g.plan.order[first + (k < count ? k : 0)];
+        xr[i] = reinterpret_cast<const char*>(a.x) + 2 * (t * a.ld);
+        if (wave == 0 && q == 0) token[k] = t;
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
@@ -119,15 +135,20 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
         u32x4 x[NT][2], m[RT][2];
     };
     auto load = [&](int h0, Chunk& v) __attribute__((always_inline)) {
+        // whole chunks without a branch around each load
+        const auto go = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int h = h0 + 16 * q + 8 * u;
-            const bool in = h < a.C;       // C is a multiple of 8
+            for (int u = 0; u < 2; ++u) {
+                const int h = h0 + 32 * u + 8 * q;
+                const bool in = whole() || h < a.C;        // C is a multiple of 8
 #pragma unroll
-            for (int i = 0; i < NT; ++i) v.x[i][u] = in ? *reinterpret_cast<const u32x4*>(xr[i] + 2 * int64_t(h)) : zero;
+                for (int i = 0; i < NT; ++i) v.x[i][u] = in ? *reinterpret_cast<const u32x4*>(xr[i] + 2 * int64_t(h)) : zero;
 #pragma unroll
-            for (int i = 0; i < RT; ++i) v.m[i][u] = in ? *reinterpret_cast<const u32x4*>(mr[i] + 2 * int64_t(h)) : zero;
-        }
+                for (int i = 0; i < RT; ++i) v.m[i][u] = in ? *reinterpret_cast<const u32x4*>(mr[i] + 2 * int64_t(h)) : zero;
+            }
+        };
+        if (h0 + 64 <= a.C) go(std::true_type());
+        else go(std::false_type());
     };
     auto use = [&](const Chunk& v) __attribute__((always_inline)) {
 #pragma unroll
@@ -138,17 +159,23 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
                 for (int i = 0; i < NT; ++i) acc[i][j] = mfma(operand(v.m[j][u]), operand(v.x[i][u]), acc[i][j]);
     };
     // the next columns are on their way while these are used
-    int h0 = 64 * (blockIdx.y * kWaves + wave);
-    if (rank > 0 && h0 < a.C) {
+    const int lo = 64 * (blockIdx.y * kWaves + wave), rounds = lo < a.C ? (a.C - lo + step - 1) / step : 0;
+    if (rank > 0 && rounds > 0) {
         Chunk v0, v1;
-        load(h0, v0);
-        for (;;) {
-            load(h0 + step, v1);
+        int at = int(blockIdx.x) % rounds;
+        auto next = [&]() __attribute__((always_inline)) {
+            const int h = lo + at * step;
+            at = at + 1 < rounds ? at + 1 : 0;
+            return h;
+        };
+        load(next(), v0);
+        for (int n = rounds;;) {
+            load(next(), v1);
             use(v0);
-            if ((h0 += step) >= a.C) break;
-            load(h0 + step, v0);
+            if (--n == 0) break;
+            load(next(), v0);
             use(v1);
-            if ((h0 += step) >= a.C) break;
+            if (--n == 0) break;
         }
     }
     // the waves' sums, two and two
@@ -168,28 +195,48 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
     const float s = a.scaled && a.g.scales ? a.g.scales[tile.adapter] : 1.f;
     const int R = a.g.R;
     float* out = a.v + int64_t(blockIdx.y) * a.g.T * R;
-    for (int i = threadIdx.x; i < count * R; i += kThreads) {
-        const int k = i / R, r = i - k * R;
-        out[int64_t(a.g.plan.order[first + k]) * R + r] = r < rank ? s * (red[0][k][r] + red[1][k][r]) : 0.f;
+    // 4 RT threads a token, four ranks each
+#pragma unroll
+    for (int i = threadIdx.x; i < TOK * 4 * RT; i += kThreads) {
+        const int k = i / (4 * RT), r = 4 * (i % (4 * RT));
+        if (k >= count || r >= R) continue;
+        float* to = out + token[k] * R + r;
+        const f32x4 p = *reinterpret_cast<const f32x4*>(&red[0][k][r]), o = *reinterpret_cast<const f32x4*>(&red[1][k][r]);
+        f32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = r + j < rank ? s * (p[j] + o[j]) : 0.f;
+        if (R % 4 == 0) {
+            *reinterpret_cast<f32x4*>(to) = v;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (r + j < R) to[j] = v[j];
+        }
     }
 }
 
 // y = base + s v B.  A tile of up to 16 NS tokens and 512 columns a workgroup, 128 a
-// wave, whose lane (c, q) holds columns 8 c .. + 7 of ranks 8 q .. + 7 (of every 32) as
-// the row operand, rows (columns of B) being 8 c + j for instruction j: it gets columns
-// 32 q .. + 31 of token c.  v's pieces are made once for the workgroup, in LDS.  With a
+// wave, whose lane (c, q) holds columns 8 chunk(c) .. + 7 of ranks 8 q .. + 7 (of every
+// 32) as the row operand, rows (columns of B) being 8 chunk(c) + j for instruction j: it
+// gets columns 32 i + 8 q + j of token c.  v's pieces are made once for the workgroup, in LDS.  With a
 // rank of 16 at most the lanes q = 2, 3 hold the same ranks as q = 0, 1, against the
 // second piece of v.
 template <int KS, bool PACK, bool YBF, int NS>
-__global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a, int table) {
+__global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a) {
     constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P, W = YBF ? 1 : 2;
     __shared__ u32x4 vf[NS][NM][64];
-    if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[table]) return;
-    const Tile tile = a.g.plan.tiles[table][blockIdx.x];
+    Tile tile;
+    const int sub = a.g.plan.size / (16 * NS);
+    if (!tile_of(a.g, blockIdx.y / sub, tile)) return;
+    // the workgroup's part of the tile
+    const int skip = (blockIdx.y % sub) * 16 * NS;
+    if (skip >= tile.count) return;
+    tile.first += skip;
+    tile.count = tile.count - skip < 16 * NS ? tile.count - skip : 16 * NS;
     const int R = a.g.R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int64_t part = int64_t(a.g.T) * R;
     const int32_t* order = a.g.plan.order + tile.first;
-    if (a.v_out && a.parts > 1 && blockIdx.y == 0 && tile.adapter >= 0)
+    if (a.v_out && a.parts > 1 && blockIdx.x == 0 && tile.adapter >= 0)
         for (int i = threadIdx.x; i < tile.count * R; i += kThreads) {
             const int64_t at = int64_t(order[i / R]) * R + i % R;
             float sum = 0.f;
@@ -197,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
             a.v_out[at] = sum;
         }
     if (tile.adapter < 0 && a.base == a.y) return;
-    const int o0 = (blockIdx.y * kWaves + wave) * 128;
+    const int o0 = (blockIdx.x * kWaves + wave) * 128;
     const u32x4 zero = {0u, 0u, 0u, 0u};
     int32_t t[NS];
 #pragma unroll
@@ -206,13 +253,13 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
     auto load_base = [&](int k, u32x4 (&b)[4][W]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int o = o0 + 32 * q + 8 * i;
-            const bool in = a.base && 16 * k + c < tile.count && o < a.C;
+            // tokens and columns beyond the last ones load others and are not stored
+            const int o = o0 + 32 * i + 8 * q < a.C ? o0 + 32 * i + 8 * q : 0;
 #pragma unroll
             for (int w = 0; w < W; ++w)
-                b[i][w] = in ? reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.base) +
-                                                              (YBF ? 2 : 4) * (t[k] * a.ld_base + o))[w]
-                             : zero;
+                b[i][w] = a.base ? reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.base) +
+                                                                  (YBF ? 2 : 4) * (t[k] * a.ld_base + o))[w]
+                                 : zero;
         }
     };
     bf16x8 mf[KS][8];
@@ -227,8 +274,10 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int r = 32 * k + 8 * (PACK ? q & 1 : q) + i, o = o0 + 8 * c;
-                rows[k][i] = r < rank && o < a.C ? *reinterpret_cast<const u32x4*>(m + 2 * (int64_t(r) * a.C + o)) : zero;
+                // ranks beyond the last one count as zeros, columns are not stored
+                const int r = 32 * k + 8 * (PACK ? q & 1 : q) + i, o = o0 + 8 * chunk(c);
+                const int64_t at = int64_t(r < rank ? r : 0) * a.C + (o < a.C ? o : 0);
+                rows[k][i] = rank > 0 ? *reinterpret_cast<const u32x4*>(m + 2 * at) : zero;
             }
         load_base(0, b0);
 #pragma unroll
@@ -248,9 +297,14 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
             }
         }
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < KS; ++k) {
+            if (rank < (PACK ? 16 : 32 * (k + 1)))
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (32 * k + 8 * (PACK ? q & 1 : q) + i >= rank) rows[k][i] = zero;
 #pragma unroll
             for (int j = 0; j < 8; ++j) mf[k][j] = column(rows[k], j);
+        }
     } else {
         load_base(0, b0);
     }
@@ -270,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
         if (16 * k + c >= tile.count) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int o = o0 + 32 * q + 8 * i;
+            const int o = o0 + 32 * i + 8 * q;
             if (o >= a.C) continue;
             float y[8];
 #pragma unroll
@@ -308,27 +362,44 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
 
 // d = u^T x of a tile of tokens (a gradient, or its sum of an adapter with several
 // tiles).  512 columns and up to 64 ranks a workgroup, 128 columns a wave, 32 tokens at
-// a time: the lane (c, q) loads columns 8 c .. + 7 of tokens 8 q .. + 7, the row operand
-// of instruction j being columns 8 c + j.  u's three pieces are made once for the
+// a time: the lane (c, q) loads columns 8 chunk(c) .. + 7 of tokens 8 q .. + 7, the row
+// operand of instruction j being columns 8 chunk(c) + j.  u's three pieces are made once for the
 // workgroup, in LDS, 128 tokens at a time.
 constexpr int kStage = 4;          // times 32 tokens
+
+// One of two calls' arguments, field by field: a reference to either would put both into
+// scratch memory (lora_outer_bf16_kernel 31 us for it, not 21, lora_join_kernel 13.4, not 4.9).
+__device__ __forceinline__ OuterArgs one_of(bool second, const OuterArgs& p, const OuterArgs& o) {
+    OuterArgs a = p;
+    a.x = second ? o.x : p.x;
+    a.ld = second ? o.ld : p.ld;
+    a.C = second ? o.C : p.C;
+    a.u = second ? o.u : p.u;
+    a.scaled = second ? o.scaled : p.scaled;
+    a.d = second ? o.d : p.d;
+    a.part = second ? o.part : p.part;
+    return a;
+}
+
 template <int RT>
-__global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox, OuterArgs oy, int table) {
+__global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox, OuterArgs oy) {
     constexpr int P = 3;
     __shared__ u32x4 uf[kStage][RT][P][64];
-    __shared__ int32_t order[tile_tokens(kTables - 1)];
-    const OuterArgs& a = blockIdx.z & 1 ? oy : ox;
+    __shared__ __attribute__((aligned(16))) int32_t order[tile_tokens(kTables - 1) + 64 * kStage];
+    const OuterArgs a = one_of(blockIdx.z & 1, ox, oy);
     const int rt0 = (blockIdx.z >> 1) * 64;
-    if (!planned(a.g) || int(blockIdx.x) >= a.g.plan.head->tiles[table]) return;
-    const Tile tile = a.g.plan.tiles[table][blockIdx.x];
-    if (tile.adapter < 0 || int(blockIdx.y) * 128 * kWaves >= a.C) return;
+    Tile tile;
+    if (!tile_of(a.g, blockIdx.y, tile)) return;
+    if (tile.adapter < 0 || int(blockIdx.x) * 128 * kWaves >= a.C) return;
     const int R = a.g.R, rank = rank_of(a.g, tile.adapter);
     if (rt0 >= rank) return;
-    for (int i = threadIdx.x; i < tile.count; i += kThreads) order[i] = a.g.plan.order[tile.first + i];
+    // tokens beyond the last one (loads go up to two stages past a stage's first, which is
+    // below the count): the first, whose values are not used
+    for (int i = threadIdx.x; i < tile.count + 64 * kStage; i += kThreads)
+        order[i] = a.g.plan.order[tile.first + (i < tile.count ? i : 0)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
-    const int h0 = (blockIdx.y * kWaves + wave) * 128, h = h0 + 8 * c;
-    const bool cols = h < a.C;
-    const char* x = reinterpret_cast<const char*>(a.x) + 2 * int64_t(h);
+    const int h0 = (blockIdx.x * kWaves + wave) * 128, h = h0 + 8 * chunk(c);
+    const char* x = reinterpret_cast<const char*>(a.x) + 2 * int64_t(h < a.C ? h : 0);   // columns beyond the last: not stored
     const u32x4 zero = {0u, 0u, 0u, 0u};
     f32x4 acc[RT][8];
 #pragma unroll
@@ -338,20 +409,24 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
     // thread: rank c of tile i, tokens 8 q .. + 7 of the wave's 32
     float u[RT][8];
     auto load_u = [&](int k0) __attribute__((always_inline)) {
+        const int p0 = k0 + 32 * wave + 8 * q;
+        const int4 t0 = *reinterpret_cast<const int4*>(order + p0), t1 = *reinterpret_cast<const int4*>(order + p0 + 4);
+        const int t[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+        for (int i = 0; i < RT; ++i) {
+            const int r = rt0 + 16 * i + c;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int p = k0 + 32 * wave + 8 * q + k, r = rt0 + 16 * i + c;
-                u[i][k] = p < tile.count && r < rank ? a.u[int64_t(order[p]) * R + r] : 0.f;
-            }
+            for (int k = 0; k < 8; ++k) u[i][k] = a.u[int64_t(t[k]) * R + (r < R ? r : 0)];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[i][k] = p0 + k < tile.count && r < rank ? u[i][k] : 0.f;
+        }
     };
     auto load_x = [&](int k0, u32x4 (&rows)[8]) __attribute__((always_inline)) {
+        const int p0 = k0 + 8 * q;
+        const int4 t0 = *reinterpret_cast<const int4*>(order + p0), t1 = *reinterpret_cast<const int4*>(order + p0 + 4);
+        const int t[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int p = k0 + 8 * q + k;
-            rows[k] = cols && p < tile.count ? *reinterpret_cast<const u32x4*>(x + 2 * (order[p] * a.ld)) : zero;
-        }
+        for (int k = 0; k < 8; ++k) rows[k] = *reinterpret_cast<const u32x4*>(x + 2 * (t[k] * a.ld));
     };
     u32x4 rows[2][8];
     __syncthreads();
@@ -373,6 +448,10 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
         for (int n = 0; n < kStage; ++n) {
             if (k0 + 32 * n >= tile.count) break;
             bf16x8 xf[8];
+            if (k0 + 32 * (n + 1) > tile.count)
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k0 + 32 * n + 8 * q + k >= tile.count) rows[n & 1][k] = zero;
 #pragma unroll
             for (int j = 0; j < 8; ++j) xf[j] = column(rows[n & 1], j);
             // two loads of 32 tokens are on their way while these are used
@@ -387,17 +466,17 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
                 }
         }
     }
-    const int tiles = a.g.plan.base[table][tile.adapter + 1] - a.g.plan.base[table][tile.adapter];
+    const int tiles = a.g.plan.base[tile.adapter + 1] - a.g.plan.base[tile.adapter];
     const float s = a.scaled && a.g.scales ? a.g.scales[tile.adapter] : 1.f;
     float* d = tiles == 1 ? a.d[tile.adapter]
-                          : a.part + int64_t(outer_slot(tile.first, tile_tokens(table), tile.piece == tiles - 1)) * R * a.C;
+                          : a.part + int64_t(outer_slot(tile.first, a.g.plan.size, tile.piece == tiles - 1)) * R * a.C;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         const int r = rt0 + 16 * i + c;
         if (r >= rank) continue;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int o = h0 + 32 * q + 8 * k;
+            const int o = h0 + 32 * k + 8 * q;
             if (o >= a.C) continue;
             f32x4* out = reinterpret_cast<f32x4*>(d + int64_t(r) * a.C + o);
             out[0] = f32x4{s * acc[i][0][k], s * acc[i][1][k], s * acc[i][2][k], s * acc[i][3][k]};
@@ -408,31 +487,42 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
 
 // The gradients of adapters with several tiles, their sums in order, and of those
 // without a token: zeros.
-__global__ __launch_bounds__(kThreads) void lora_join_kernel(OuterArgs ox, OuterArgs oy, int table) {
-    const OuterArgs& a = blockIdx.z ? oy : ox;
-    const int ad = blockIdx.x, size = tile_tokens(table);
+__global__ __launch_bounds__(kThreads) void lora_join_kernel(OuterArgs ox, OuterArgs oy) {
+    const OuterArgs a = one_of(blockIdx.z, ox, oy);
+    const int ad = blockIdx.x, size = a.g.plan.size;
     // side by side
-    const int tiles = a.g.plan.base[table][ad + 1] - a.g.plan.base[table][ad], first = a.g.plan.seg[ad];
+    const int tiles = a.g.plan.base[ad + 1] - a.g.plan.base[ad], first = a.g.plan.seg[ad];
     const int64_t all = int64_t(rank_of(a.g, ad)) * a.C, part = int64_t(a.g.R) * a.C;
     float* d = a.d[ad];
     if (!planned(a.g) || tiles == 1) return;
     for (int64_t i = 4 * (int64_t(blockIdx.y) * kThreads + threadIdx.x); i < all; i += 4 * int64_t(gridDim.y) * kThreads) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-        for (int k = 0; k < tiles; ++k)
-            sum += *reinterpret_cast<const f32x4*>(a.part + outer_slot(first + k * size, size, k == tiles - 1) * part + i);
+        for (int k0 = 0; k0 < tiles; k0 += 8) {    // eight loads at once
+            f32x4 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = k0 + j;
+                v[j] = k < tiles ? *reinterpret_cast<const f32x4*>(
+                                       a.part + outer_slot(first + k * size, size, k == tiles - 1) * part + i)
+                                 : f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += v[j];
+        }
         *reinterpret_cast<f32x4*>(d + i) = sum;
     }
 }
 
 }  // namespace
 
-int outer_bf16(const OuterArgs (&a)[2], int table, hipStream_t s) {
+int outer_bf16(const OuterArgs (&o)[2], int table, hipStream_t s) {
+    OuterArgs a[2] = {o[0], o[1]};
+    for (OuterArgs& g : a) g.g = with_table(g.g, table);
     const int R = a[0].g.R, C = a[0].C > a[1].C ? a[0].C : a[1].C, n = a[0].g.n;
-    const dim3 grid(unsigned(plan_layout(a[0].g.T, n).max_tiles[table]), unsigned((C + 128 * kWaves - 1) / (128 * kWaves)),
+    const dim3 grid(unsigned((C + 128 * kWaves - 1) / (128 * kWaves)), unsigned(plan_layout(a[0].g.T, n).max_tiles[table]),
                     R > 64 ? 4 : 2);
     const auto go = [&](auto rt) {
-        hipLaunchKernelGGL((lora_outer_bf16_kernel<rt()>), grid, dim3(kThreads), 0, s, a[0], a[1], table);
+        hipLaunchKernelGGL((lora_outer_bf16_kernel<rt()>), grid, dim3(kThreads), 0, s, a[0], a[1]);
     };
     if (R <= 16) go(std::integral_constant<int, 1>());
     else if (R <= 32) go(std::integral_constant<int, 2>());
@@ -440,16 +530,18 @@ int outer_bf16(const OuterArgs (&a)[2], int table, hipStream_t s) {
     STMOE_LAUNCHED();
     const int64_t chunks = (int64_t(R) * C / 4 + kThreads - 1) / kThreads, most = n < 64 ? 512 / n : 8;
     hipLaunchKernelGGL(lora_join_kernel, dim3(unsigned(n), unsigned(chunks < most ? chunks : most), 2), dim3(kThreads), 0, s,
-                       a[0], a[1], table);
+                       a[0], a[1]);
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
 
-int shrink_bf16(const ShrinkArgs& a, int table, hipStream_t s) {
+int shrink_bf16(const ShrinkArgs& o, int table, hipStream_t s) {
+    ShrinkArgs a = o;
+    a.g = with_table(o.g, table);
     const int tiles = plan_layout(a.g.T, a.g.n).max_tiles[table];
     const auto go = [&](auto rt, auto nt) {
         const dim3 grid(unsigned(tiles * (tile_tokens(table) / (16 * nt()))), unsigned(a.parts));
-        hipLaunchKernelGGL((lora_shrink_bf16_kernel<rt(), nt()>), grid, dim3(kThreads), 0, s, a, table);
+        hipLaunchKernelGGL((lora_shrink_bf16_kernel<rt(), nt()>), grid, dim3(kThreads), 0, s, a);
     };
     const auto with = [&](auto rt) {
         if (table == 0) go(rt, std::integral_constant<int, 1>());
@@ -464,17 +556,25 @@ int shrink_bf16(const ShrinkArgs& a, int table, hipStream_t s) {
     return STMOE_OK;
 }
 
-int expand_bf16(const ExpandArgs& a, int table, bool ybf, hipStream_t s) {
-    const dim3 grid(unsigned(plan_layout(a.g.T, a.g.n).max_tiles[table]), unsigned((a.C + 128 * kWaves - 1) / (128 * kWaves)));
-    const auto with = [&](auto ks, auto pack, auto ns) {
-        if (ybf) hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), true, ns()>), grid, dim3(kThreads), 0, s, a, table);
-        else hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), false, ns()>), grid, dim3(kThreads), 0, s, a, table);
+int expand_bf16(const ExpandArgs& o, int table, bool ybf, hipStream_t s) {
+    ExpandArgs a = o;
+    const unsigned cols = unsigned((a.C + 128 * kWaves - 1) / (128 * kWaves));
+    const PlanLayout y = plan_layout(a.g.T, a.g.n);
+    const int R = a.g.R;
+    // 128 tokens a workgroup where that leaves two workgroups for most CUs: B is loaded
+    // and v split half as often
+    const bool wide = table == 1 && R <= 64 && int64_t(cols) * (a.g.T / 128) >= 400;
+    const auto with = [&](auto ks, auto pack, auto ns, int tab) {
+        a.g = with_table(o.g, tab);
+        const dim3 grid(cols, unsigned(y.max_tiles[tab] * (tile_tokens(tab) / (16 * ns()))));
+        if (ybf) hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), true, ns()>), grid, dim3(kThreads), 0, s, a);
+        else hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), false, ns()>), grid, dim3(kThreads), 0, s, a);
     };
     const auto go = [&](auto ks, auto pack) {
-        if (table == 0) with(ks, pack, std::integral_constant<int, 1>());
-        else with(ks, pack, std::integral_constant<int, 4>());
+        if (table == 0) with(ks, pack, std::integral_constant<int, 1>(), 0);
+        else if (wide) with(ks, pack, std::integral_constant<int, ks() == 4 ? 4 : 8>(), ks() == 4 ? 1 : 2);
+        else with(ks, pack, std::integral_constant<int, 4>(), 1);
     };
-    const int R = a.g.R;
     if (R <= 16) go(std::integral_constant<int, 1>(), std::true_type());
     else if (R <= 32) go(std::integral_constant<int, 1>(), std::false_type());
     else if (R <= 64) go(std::integral_constant<int, 2>(), std::false_type());

@@ -53,26 +53,28 @@ __host__ __device__ inline PlanLayout plan_layout(int T, int n) {
     return y;
 }
 
-// What the kernels read of a plan.
+// What the kernels read of a plan: one of its tables.
 struct Plan {
     const PlanHead* head;
+    const int32_t* tiles_n;        // [1] tiles of the table
     const int32_t* seg;            // [n + 2] first position of every adapter; T
     const int32_t* order;          // [T] token at every position
-    const int32_t* base[kTables];  // [n + 2] first tile of every adapter
-    const Tile* tiles[kTables];
+    const int32_t* base;           // [n + 2] first tile of every adapter
+    const Tile* tiles;
+    int size;                      // tokens per tile
 };
 
-inline Plan plan_of(const void* plan, int T, int n) {
+inline Plan plan_of(const void* plan, int T, int n, int table) {
     const PlanLayout y = plan_layout(T, n);
     const char* p = reinterpret_cast<const char*>(plan);
     Plan o{};
     o.head = reinterpret_cast<const PlanHead*>(p);
+    o.tiles_n = o.head->tiles + table;
     o.seg = reinterpret_cast<const int32_t*>(p + y.seg);
     o.order = reinterpret_cast<const int32_t*>(p + y.order);
-    for (int s = 0; s < kTables; ++s) {
-        o.base[s] = reinterpret_cast<const int32_t*>(p + y.base[s]);
-        o.tiles[s] = reinterpret_cast<const Tile*>(p + y.tiles[s]);
-    }
+    o.base = reinterpret_cast<const int32_t*>(p + y.base[table]);
+    o.tiles = reinterpret_cast<const Tile*>(p + y.tiles[table]);
+    o.size = tile_tokens(table);
     return o;
 }
 
