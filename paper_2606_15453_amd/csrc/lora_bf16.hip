@@ -56,10 +56,6 @@ __device__ __forceinline__ bf16x8 column(const u32x4 (&rows)[8], int j) {
     return operand(q);
 }
 
-// The chunk of eight columns, of 16, that lane c feeds so that the results i of the lanes
-// q (rows 4 q + i) stand side by side: four lanes store 64 bytes of a row.
-__device__ __forceinline__ int chunk(int c) { return (c >> 2) | (c & 3) << 2; }
-
 // Eight values of a row of R from r on, 0 beyond it; the sum of its parts (one or an even
 // number), two at a time.
 __device__ __forceinline__ void load8(const float* row, int64_t part, int parts, int r, int R, float (&v)[8]) {
@@ -94,35 +90,40 @@ __device__ __forceinline__ void load8(const float* row, int64_t part, int parts,
 }
 
 // v = x A^T.  16 NT tokens a workgroup (a tile, or a part of one) and, with several
-// parts, some of the columns; a wave takes every fourth 64 columns.  The lane (c, q)
-// feeds columns 16 q .. + 15 of token c and of rank c: 32 bytes of a row, 128 a quarter
-// wave.
+// parts, some of the columns; a wave takes every fourth 64 columns.  Rows go through
+// LDS, each wave's own: eight consecutive lanes load 128 bytes of one, where the matrix
+// instruction's operand has a row a lane, and loads in that order get 16 bytes a cycle
+// and CU out of the cache (8192 tokens x 4096, rank 64: XX us so, 30 without LDS).
 template <int RT, int NT>
 __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a) {
-    constexpr int TOK = 16 * NT, LD = 16 * RT + 4;
-    __shared__ __attribute__((aligned(16))) float red[2][TOK][LD];
+    constexpr int TOK = 16 * NT, LD = 16 * RT + 4, ROWS = 16 * (NT + RT);
+    union Lds {
+        char rows[kWaves][ROWS][128];
+        float red[2][TOK][LD];
+    };
+    __shared__ __attribute__((aligned(16))) Lds lds;
     __shared__ int64_t token[TOK];
-    const int sub = a.g.plan.size / TOK, k0 = (blockIdx.x % sub) * TOK;
     Tile tile;
+    const int sub = a.g.plan.size / TOK, k0 = (blockIdx.x % sub) * TOK;
     if (!tile_of(a.g, blockIdx.x / sub, tile) || tile.adapter < 0 || k0 >= tile.count) return;
     const int count = tile.count - k0 < TOK ? tile.count - k0 : TOK, first = tile.first + k0;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int rank = rank_of(a.g, tile.adapter);
-    const char* m = reinterpret_cast<const char*>(a.m[tile.adapter]);
-    // tokens and ranks beyond the last ones take another's values: their sums are their own
-    const char* xr[NT];
-    const char* mr[RT];
+    // lane: chunk lane & 7 of row 8 i + lane / 8.  Tokens and ranks beyond the last ones
+    // take another's values: their sums are their own
+    const char* row[2 * (NT + RT)];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        const int k = 16 * i + c;
+    for (int i = 0; i < 2 * NT; ++i) {
+        const int k = 8 * i + (lane >> 3);
         const int64_t t = a.g.plan.order[first + (k < count ? k : 0)];
-        xr[i] = reinterpret_cast<const char*>(a.x) + 2 * (t * a.ld);
-        if (wave == 0 && q == 0) token[k] = t;
+        row[i] = reinterpret_cast<const char*>(a.x) + 2 * (t * a.ld);
+        if (wave == 0 && (lane & 7) == 0) token[k] = t;
     }
+    const char* m = reinterpret_cast<const char*>(a.m[tile.adapter]);
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int r = 16 * i + c;
-        mr[i] = m + 2 * (int64_t(r < rank ? r : 0) * a.C);
+    for (int i = 0; i < 2 * RT; ++i) {
+        const int r = 8 * i + (lane >> 3);
+        row[2 * NT + i] = m + 2 * (int64_t(r < rank ? r : 0) * a.C);
     }
     f32x4 acc[NT][RT];
 #pragma unroll
@@ -130,56 +131,65 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 #pragma unroll
         for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const u32x4 zero = {0u, 0u, 0u, 0u};
-    const int step = 64 * kWaves * int(gridDim.y);
     struct Chunk {
-        u32x4 x[NT][2], m[RT][2];
+        u32x4 v[2 * (NT + RT)];
     };
     auto load = [&](int h0, Chunk& v) __attribute__((always_inline)) {
-        // whole chunks without a branch around each load
-        const auto go = [&](auto whole) __attribute__((always_inline)) {
+        const int h = h0 + 8 * (lane & 7);
+        if (h0 + 64 <= a.C) {              // whole chunks without a branch around each load
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int h = h0 + 32 * u + 8 * q;
-                const bool in = whole() || h < a.C;        // C is a multiple of 8
+            for (int i = 0; i < 2 * (NT + RT); ++i) v.v[i] = *reinterpret_cast<const u32x4*>(row[i] + 2 * int64_t(h));
+        } else {
 #pragma unroll
-                for (int i = 0; i < NT; ++i) v.x[i][u] = in ? *reinterpret_cast<const u32x4*>(xr[i] + 2 * int64_t(h)) : zero;
-#pragma unroll
-                for (int i = 0; i < RT; ++i) v.m[i][u] = in ? *reinterpret_cast<const u32x4*>(mr[i] + 2 * int64_t(h)) : zero;
-            }
-        };
-        if (h0 + 64 <= a.C) go(std::true_type());
-        else go(std::false_type());
+            for (int i = 0; i < 2 * (NT + RT); ++i)
+                v.v[i] = h < a.C ? *reinterpret_cast<const u32x4*>(row[i] + 2 * int64_t(h)) : zero;   // C is a multiple of 8
+        }
     };
+    // chunk k of row r is at place k ^ r / 2 % 8: 16 lanes read 16 rows without a conflict
+    char* const mine = lds.rows[wave][0];
+    const int wr = (lane >> 3) * 128 + ((lane & 7) ^ (lane >> 4)) * 16;
+    const int rd = c * 128 + (q ^ (c >> 1)) * 16;
     auto use = [&](const Chunk& v) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int i = 0; i < 2 * (NT + RT); ++i) *reinterpret_cast<u32x4*>(mine + 1024 * i + (i % 2 ? wr ^ 64 : wr)) = v.v[i];
+        // a wave's LDS accesses complete in order
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            bf16x8 x[NT], w[RT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) x[i] = operand(*reinterpret_cast<const u32x4*>(mine + 2048 * i + (rd ^ 64 * u)));
+#pragma unroll
+            for (int i = 0; i < RT; ++i) w[i] = operand(*reinterpret_cast<const u32x4*>(mine + 2048 * (NT + i) + (rd ^ 64 * u)));
 #pragma unroll
             for (int j = 0; j < RT; ++j)
 #pragma unroll
-                for (int i = 0; i < NT; ++i) acc[i][j] = mfma(operand(v.m[j][u]), operand(v.x[i][u]), acc[i][j]);
+                for (int i = 0; i < NT; ++i) acc[i][j] = mfma(w[j], x[i], acc[i][j]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     };
     // the next columns are on their way while these are used
-    const int lo = 64 * (blockIdx.y * kWaves + wave), rounds = lo < a.C ? (a.C - lo + step - 1) / step : 0;
-    if (rank > 0 && rounds > 0) {
+    const int step = 64 * kWaves * int(gridDim.y);
+    int h0 = 64 * (blockIdx.y * kWaves + wave);
+    if (rank > 0 && h0 < a.C) {
         Chunk v0, v1;
-        int at = int(blockIdx.x) % rounds;
-        auto next = [&]() __attribute__((always_inline)) {
-            const int h = lo + at * step;
-            at = at + 1 < rounds ? at + 1 : 0;
-            return h;
-        };
-        load(next(), v0);
-        for (int n = rounds;;) {
-            load(next(), v1);
+        load(h0, v0);
+        for (;;) {
+            h0 += step;
+            if (h0 < a.C) load(h0, v1);
             use(v0);
-            if (--n == 0) break;
-            load(next(), v0);
+            if (h0 >= a.C) break;
+            h0 += step;
+            if (h0 < a.C) load(h0, v0);
             use(v1);
-            if (--n == 0) break;
+            if (h0 >= a.C) break;
         }
     }
     // the waves' sums, two and two
-    auto at = [&](int b, int i, int j) { return reinterpret_cast<f32x4*>(&red[b][16 * i + c][16 * j + 4 * q]); };
+    __syncthreads();
+    auto at = [&](int b, int i, int j) { return reinterpret_cast<f32x4*>(&lds.red[b][16 * i + c][16 * j + 4 * q]); };
     if (wave >= 2)
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -201,7 +211,7 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
         const int k = i / (4 * RT), r = 4 * (i % (4 * RT));
         if (k >= count || r >= R) continue;
         float* to = out + token[k] * R + r;
-        const f32x4 p = *reinterpret_cast<const f32x4*>(&red[0][k][r]), o = *reinterpret_cast<const f32x4*>(&red[1][k][r]);
+        const f32x4 p = *reinterpret_cast<const f32x4*>(&lds.red[0][k][r]), o = *reinterpret_cast<const f32x4*>(&lds.red[1][k][r]);
         f32x4 v;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = r + j < rank ? s * (p[j] + o[j]) : 0.f;
@@ -216,15 +226,16 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 }
 
 // y = base + s v B.  A tile of up to 16 NS tokens and 512 columns a workgroup, 128 a
-// wave, whose lane (c, q) holds columns 8 chunk(c) .. + 7 of ranks 8 q .. + 7 (of every
-// 32) as the row operand, rows (columns of B) being 8 chunk(c) + j for instruction j: it
-// gets columns 32 i + 8 q + j of token c.  v's pieces are made once for the workgroup, in LDS.  With a
-// rank of 16 at most the lanes q = 2, 3 hold the same ranks as q = 0, 1, against the
-// second piece of v.
+// wave, whose lane (c, q) holds columns 8 c .. + 7 of ranks 8 q .. + 7 (of every 32) as
+// the column operand, that of instruction j being columns 8 c + j: it gets columns 8 c
+// .. + 7 of tokens 4 q .. + 3, so that 16 lanes load and store 256 bytes of a row.  v's
+// pieces are made once for the workgroup, in LDS.  With a rank of 16 at most the lanes q =
+// 2, 3 hold the same ranks as q = 0, 1, against the second piece of v.
 template <int KS, bool PACK, bool YBF, int NS>
 __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a) {
     constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P, W = YBF ? 1 : 2;
     __shared__ u32x4 vf[NS][NM][64];
+    __shared__ __attribute__((aligned(16))) int32_t token[16 * NS];
     Tile tile;
     const int sub = a.g.plan.size / (16 * NS);
     if (!tile_of(a.g, blockIdx.y / sub, tile)) return;
@@ -244,24 +255,21 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
             a.v_out[at] = sum;
         }
     if (tile.adapter < 0 && a.base == a.y) return;
-    const int o0 = (blockIdx.x * kWaves + wave) * 128;
+    // tokens beyond the last one: the first, whose row is not stored again
+    if (threadIdx.x < 16 * NS) token[threadIdx.x] = order[int(threadIdx.x) < tile.count ? threadIdx.x : 0];
+    const int o = (blockIdx.x * kWaves + wave) * 128 + 8 * c, oc = o < a.C ? o : 0;    // columns beyond the last: not stored
     const u32x4 zero = {0u, 0u, 0u, 0u};
-    int32_t t[NS];
+    auto load_base = [&](const int4& t, u32x4 (&b)[4][W]) __attribute__((always_inline)) {
+        const int ts[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
-    for (int k = 0; k < NS; ++k) t[k] = order[16 * k + c < tile.count ? 16 * k + c : 0];
-    // base: four chunks of eight columns
-    auto load_base = [&](int k, u32x4 (&b)[4][W]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            // tokens and columns beyond the last ones load others and are not stored
-            const int o = o0 + 32 * i + 8 * q < a.C ? o0 + 32 * i + 8 * q : 0;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int w = 0; w < W; ++w)
                 b[i][w] = a.base ? reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.base) +
-                                                                  (YBF ? 2 : 4) * (t[k] * a.ld_base + o))[w]
+                                                                  (YBF ? 2 : 4) * (ts[i] * a.ld_base + oc))[w]
                                  : zero;
-        }
     };
+    auto tokens = [&](int k) __attribute__((always_inline)) { return *reinterpret_cast<const int4*>(token + 16 * k + 4 * q); };
     bf16x8 mf[KS][8];
     u32x4 b0[4][W], b1[4][W];
     float s = 0.f;
@@ -275,11 +283,10 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 // ranks beyond the last one count as zeros, columns are not stored
-                const int r = 32 * k + 8 * (PACK ? q & 1 : q) + i, o = o0 + 8 * chunk(c);
-                const int64_t at = int64_t(r < rank ? r : 0) * a.C + (o < a.C ? o : 0);
+                const int r = 32 * k + 8 * (PACK ? q & 1 : q) + i;
+                const int64_t at = int64_t(r < rank ? r : 0) * a.C + oc;
                 rows[k][i] = rank > 0 ? *reinterpret_cast<const u32x4*>(m + 2 * at) : zero;
             }
-        load_base(0, b0);
 #pragma unroll
         for (int i = threadIdx.x; i < 64 * NS * KS; i += kThreads) {
             const int l = i & 63, k = (i >> 6) % KS, n = (i >> 6) / KS, lq = l >> 4, lt = 16 * n + (l & 15);
@@ -305,11 +312,11 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
 #pragma unroll
             for (int j = 0; j < 8; ++j) mf[k][j] = column(rows[k], j);
         }
-    } else {
-        load_base(0, b0);
     }
     __syncthreads();
-    auto finish = [&](int k, const u32x4 (&b)[4][W]) __attribute__((always_inline)) {
+    int4 t0 = tokens(0), t1;
+    load_base(t0, b0);
+    auto finish = [&](int k, const int4& t, const u32x4 (&b)[4][W]) __attribute__((always_inline)) {
         f32x4 acc[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -318,14 +325,13 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
             for (int i = NM - 1; i >= 0; --i) {
                 const bf16x8 v = operand(vf[k][i][lane]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] = mfma(mf[PACK ? 0 : i / P][j], v, acc[j]);
+                for (int j = 0; j < 8; ++j) acc[j] = mfma(v, mf[PACK ? 0 : i / P][j], acc[j]);
             }
         }
-        if (16 * k + c >= tile.count) return;
+        const int ts[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int o = o0 + 32 * i + 8 * q;
-            if (o >= a.C) continue;
+            if (16 * k + 4 * q + i >= tile.count || o >= a.C) continue;
             float y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -333,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
                                     : __uint_as_float(b[i][W == 2 ? j / 4 : 0][j % 4]);
                 y[j] = tile.adapter >= 0 ? f + s * acc[j][i] : f;
             }
-            char* out = reinterpret_cast<char*>(a.y) + (YBF ? 2 : 4) * (t[k] * a.ld + o);
+            char* out = reinterpret_cast<char*>(a.y) + (YBF ? 2 : 4) * (ts[i] * a.ld + o);
             if constexpr (YBF) {
                 union {
                     __bf16 h[8];
@@ -352,18 +358,18 @@ __global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a
 #pragma unroll
     for (int k = 0; k < NS; k += 2) {
         if (16 * k >= tile.count) break;
-        if (k + 1 < NS) load_base(k + 1, b1);
-        finish(k, b0);
+        if (k + 1 < NS) load_base(t1 = tokens(k + 1), b1);
+        finish(k, t0, b0);
         if (k + 1 >= NS || 16 * (k + 1) >= tile.count) break;
-        if (k + 2 < NS) load_base(k + 2, b0);
-        finish(k + 1, b1);
+        if (k + 2 < NS) load_base(t0 = tokens(k + 2), b0);
+        finish(k + 1, t1, b1);
     }
 }
 
 // d = u^T x of a tile of tokens (a gradient, or its sum of an adapter with several
 // tiles).  512 columns and up to 64 ranks a workgroup, 128 columns a wave, 32 tokens at
-// a time: the lane (c, q) loads columns 8 chunk(c) .. + 7 of tokens 8 q .. + 7, the row
-// operand of instruction j being columns 8 chunk(c) + j.  u's three pieces are made once for the
+// a time: the lane (c, q) loads columns 8 c .. + 7 of tokens 8 q .. + 7, the column
+// operand of instruction j being columns 8 c + j, and gets them of ranks 4 q .. + 3.  u's three pieces are made once for the
 // workgroup, in LDS, 128 tokens at a time.
 constexpr int kStage = 4;          // times 32 tokens
 
@@ -398,7 +404,7 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
     for (int i = threadIdx.x; i < tile.count + 64 * kStage; i += kThreads)
         order[i] = a.g.plan.order[tile.first + (i < tile.count ? i : 0)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
-    const int h0 = (blockIdx.x * kWaves + wave) * 128, h = h0 + 8 * chunk(c);
+    const int h0 = (blockIdx.x * kWaves + wave) * 128, h = h0 + 8 * c;
     const char* x = reinterpret_cast<const char*>(a.x) + 2 * int64_t(h < a.C ? h : 0);   // columns beyond the last: not stored
     const u32x4 zero = {0u, 0u, 0u, 0u};
     f32x4 acc[RT][8];
@@ -462,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
                 for (int p = P - 1; p >= 0; --p) {
                     const bf16x8 b = operand(uf[n][i][p][lane]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[i][j] = mfma(xf[j], b, acc[i][j]);
+                    for (int j = 0; j < 8; ++j) acc[i][j] = mfma(b, xf[j], acc[i][j]);
                 }
         }
     }
@@ -470,19 +476,17 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
     const float s = a.scaled && a.g.scales ? a.g.scales[tile.adapter] : 1.f;
     float* d = tiles == 1 ? a.d[tile.adapter]
                           : a.part + int64_t(outer_slot(tile.first, a.g.plan.size, tile.piece == tiles - 1)) * R * a.C;
+    if (h >= a.C) return;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int r = rt0 + 16 * i + c;
-        if (r >= rank) continue;
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int o = h0 + 32 * k + 8 * q;
-            if (o >= a.C) continue;
-            f32x4* out = reinterpret_cast<f32x4*>(d + int64_t(r) * a.C + o);
+            const int r = rt0 + 16 * i + 4 * q + k;
+            if (r >= rank) continue;
+            f32x4* out = reinterpret_cast<f32x4*>(d + int64_t(r) * a.C + h);
             out[0] = f32x4{s * acc[i][0][k], s * acc[i][1][k], s * acc[i][2][k], s * acc[i][3][k]};
             out[1] = f32x4{s * acc[i][4][k], s * acc[i][5][k], s * acc[i][6][k], s * acc[i][7][k]};
         }
-    }
 }
 
 // The gradients of adapters with several tiles, their sums in order, and of those
