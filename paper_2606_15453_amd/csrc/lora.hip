@@ -190,17 +190,20 @@ __global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs a) {
 // Tiles of 64 tokens where adapters have that many on average.
 bool large_tiles(int T, int n) { return T >= 64 * n && T > 64; }
 
-// Parts of a token's columns, a workgroup each, where there are few tiles.
+// Rows of all parts of T tokens at most; never falls as T grows.
+int part_rows(int T) { return T < 4096 ? 8 * T : T < 32768 ? 32768 : T; }
+
+// Parts of a token's columns, a workgroup each, where there are few of them.  The launch
+// over the rank adds them up, which costs it more with every part.  us of the two
+// launches with 1, 2, 4 and 8 parts (4096 columns each way): 64 tokens of 32 adapters,
+// rank 64: 22.6, 17.0, 14.5, 15.1; 4096 tokens, rank 16: 35.6, 32.6, 35.5; 8192 tokens,
+// rank 64: 65.3, 70.8, 81.3.
 int column_parts(int T, int n, int C) {
-    const int tiles = large_tiles(T, n) ? T / 64 + n : T / 16 + (T < n ? T : n);
+    const int groups = large_tiles(T, n) ? 2 * (T / 64 + n) : T / 16 + (T < n ? T : n);
     int p = 1;
-    while (p < 8 && tiles * p < 256 && C / (2 * p) >= 512) p *= 2;
+    while (p < 8 && groups * p < 144 && C / (2 * p) >= 512 && 2 * p * T <= part_rows(T)) p *= 2;
     return p;
 }
-
-// Rows of all parts of T tokens at most (parts times tokens, by column_parts), which
-// never falls as T grows.
-int part_rows(int T) { return T < 4096 ? 8 * T : T < 32768 ? 32768 : T; }
 
 // Tokens per tile of the sums over tokens: 256, and 1024 for ranks above 16, whose sums
 // (R x C fp32 a tile) would be as many bytes as the rows.

@@ -93,7 +93,7 @@ __device__ __forceinline__ void load8(const float* row, int64_t part, int parts,
 // parts, some of the columns; a wave takes every fourth 64 columns.  Rows go through
 // LDS, each wave's own: eight consecutive lanes load 128 bytes of one, where the matrix
 // instruction's operand has a row a lane, and loads in that order get 16 bytes a cycle
-// and CU out of the cache (8192 tokens x 4096, rank 64: XX us so, 30 without LDS).
+// and CU out of the cache (4096 tokens x 4096, rank 16: 12.4 us so, 18.1 without LDS).
 template <int RT, int NT>
 __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a) {
     constexpr int TOK = 16 * NT, LD = 16 * RT + 4, ROWS = 16 * (NT + RT);
@@ -232,18 +232,12 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 // pieces are made once for the workgroup, in LDS.  With a rank of 16 at most the lanes q =
 // 2, 3 hold the same ranks as q = 0, 1, against the second piece of v.
 template <int KS, bool PACK, bool YBF, int NS>
-__global__ __launch_bounds__(kThreads) void lora_expand_bf16_kernel(ExpandArgs a) {
+__global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_bf16_kernel(ExpandArgs a) {
     constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P, W = YBF ? 1 : 2;
     __shared__ u32x4 vf[NS][NM][64];
     __shared__ __attribute__((aligned(16))) int32_t token[16 * NS];
     Tile tile;
-    const int sub = a.g.plan.size / (16 * NS);
-    if (!tile_of(a.g, blockIdx.y / sub, tile)) return;
-    // the workgroup's part of the tile
-    const int skip = (blockIdx.y % sub) * 16 * NS;
-    if (skip >= tile.count) return;
-    tile.first += skip;
-    tile.count = tile.count - skip < 16 * NS ? tile.count - skip : 16 * NS;
+    if (!tile_of(a.g, blockIdx.y, tile)) return;
     const int R = a.g.R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int64_t part = int64_t(a.g.T) * R;
     const int32_t* order = a.g.plan.order + tile.first;
@@ -549,7 +543,7 @@ int shrink_bf16(const ShrinkArgs& o, int table, hipStream_t s) {
     };
     const auto with = [&](auto rt) {
         if (table == 0) go(rt, std::integral_constant<int, 1>());
-        else go(rt, std::integral_constant<int, rt() == 8 ? 2 : 4>());
+        else go(rt, std::integral_constant<int, 2>());
     };
     const int R = a.g.R;
     if (R <= 16) with(std::integral_constant<int, 1>());
@@ -562,22 +556,17 @@ int shrink_bf16(const ShrinkArgs& o, int table, hipStream_t s) {
 
 int expand_bf16(const ExpandArgs& o, int table, bool ybf, hipStream_t s) {
     ExpandArgs a = o;
+    a.g = with_table(o.g, table);
     const unsigned cols = unsigned((a.C + 128 * kWaves - 1) / (128 * kWaves));
-    const PlanLayout y = plan_layout(a.g.T, a.g.n);
     const int R = a.g.R;
-    // 128 tokens a workgroup where that leaves two workgroups for most CUs: B is loaded
-    // and v split half as often
-    const bool wide = table == 1 && R <= 64 && int64_t(cols) * (a.g.T / 128) >= 400;
-    const auto with = [&](auto ks, auto pack, auto ns, int tab) {
-        a.g = with_table(o.g, tab);
-        const dim3 grid(cols, unsigned(y.max_tiles[tab] * (tile_tokens(tab) / (16 * ns()))));
+    const auto with = [&](auto ks, auto pack, auto ns) {
+        const dim3 grid(cols, unsigned(plan_layout(a.g.T, a.g.n).max_tiles[table]));
         if (ybf) hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), true, ns()>), grid, dim3(kThreads), 0, s, a);
         else hipLaunchKernelGGL((lora_expand_bf16_kernel<ks(), pack(), false, ns()>), grid, dim3(kThreads), 0, s, a);
     };
     const auto go = [&](auto ks, auto pack) {
-        if (table == 0) with(ks, pack, std::integral_constant<int, 1>(), 0);
-        else if (wide) with(ks, pack, std::integral_constant<int, ks() == 4 ? 4 : 8>(), ks() == 4 ? 1 : 2);
-        else with(ks, pack, std::integral_constant<int, 4>(), 1);
+        if (table == 0) with(ks, pack, std::integral_constant<int, 1>());
+        else with(ks, pack, std::integral_constant<int, 4>());
     };
     if (R <= 16) go(std::integral_constant<int, 1>(), std::true_type());
     else if (R <= 32) go(std::integral_constant<int, 1>(), std::false_type());
