@@ -679,6 +679,14 @@ int moe_ctx_set_prefetch(moe_ctx* ctx, int min_score, int max_per_layer);
  * default) or frozen after profiling (0; HT rows are still overwritten with
  * each selection).  An ablation switch. */
 int moe_ctx_set_online_update(moe_ctx* ctx, int on);
+/* Routing by scores in place of the softmax top-K (arguments as moe_route_scored;
+ * renorm is the description's): bias device [L][E] fp32, or NULL, read by every
+ * layer's router, so it may be moved between tokens (moe_route_bias_step).  A row
+ * with fewer than K candidates (logits or biases of minus infinity) gets the
+ * lowest other experts with weight 0, so K distinct experts always reach the
+ * predictor and the cache.  STMOE_SOFTMAX, NULL, 1, 1, 1, 1.0f is the default. */
+int moe_ctx_set_routing(moe_ctx* ctx, int score, const float* bias, int n_groups, int top_groups, int group_top,
+                        float scale);
 /* All L layers of one token: xs device [L][B][H], ys device out [L][B][H].
  * With graph replay on (moe_ctx_set_graph), every call after the first whose
  * token is not event-timed replays one HIP graph of the whole token: xs is
@@ -686,7 +694,7 @@ int moe_ctx_set_online_update(moe_ctx* ctx, int on);
  * output staging buffer is copied to ys (a copy is skipped when the pointer
  * is the staging buffer itself).  The graph is captured at the first such
  * call and again when `mode`, a setting of the context (moe_ctx_set_prefetch,
- * moe_ctx_set_online_update) or the cache's configuration (warm start,
+ * moe_ctx_set_online_update, moe_ctx_set_routing) or the cache's configuration (warm start,
  * decision site, staged prefetch, prefetch order, replacement rule) has
  * changed since; results equal the eager calls. */
 int moe_decode_token(moe_ctx* ctx, int token, const void* xs, float* ys, int mode);

@@ -33,6 +33,10 @@ int ffn_route_plan(const float* z, int renorm, int32_t* idx, float* w, int B, in
                    const void* const* eptr, const void* const* sptr, int n_shared, void* ws, const void* ebase,
                    size_t estride, hipStream_t st);
 int route_logits(const void* x, const void* w_gate, int B, int H, int E, int dtype, float* z, hipStream_t s);
+// route_scored.hip
+int route_scored_rows(const float* z, int B, int E, int K, int score, const float* bias, int n_groups, int top_groups,
+                      int group_top, int renorm, float scale, int32_t* idx, float* w, hipStream_t s);
+const char* bad_groups(int E, int K, int n_groups, int top_groups, int group_top);
 size_t update_predict_seq_bytes(int L);
 int update_predict_seq_args(stmoe_predictor* p, const int32_t* idx_all, void* dev_args);
 int update_predict_seq(stmoe_predictor* p, const void* dev_args, int use, int online, hipStream_t s);
@@ -114,6 +118,12 @@ struct moe_ctx {
     bool capturing = false;                // a token's layers are being captured into a graph
     int pf_min_score = 2, pf_max = 1 << 30;
     bool want_ranked = false;              // a report asks for the side path's ranked prediction
+    struct {
+        bool on = false;                   // routing by scores instead of the softmax top-K
+        int score = 0, n_groups = 1, top_groups = 1, group_top = 1;
+        const float* bias = nullptr;       // device [L][E] or null
+        float scale = 1.f;
+    } scored;
     int online = 1;                        // Algorithm 3's CCT update on (1) or frozen CCTs (0)
     hipEvent_t rec_ev = nullptr;
     std::vector<const void*> host_table;   // [E] scratch for the cache's answers
@@ -407,6 +417,18 @@ int side_update_predict(moe_ctx* c, int layer, const int32_t* prev, const int32_
     return update_predict(c->pred, layer, prev, idx_l, use, c->online, nullptr, nullptr, nullptr, c->side);
 }
 
+// The layer's router: logits, then the softmax top-K or the selection by scores.
+int route(moe_ctx* c, int layer, const void* x, int32_t* idx, float* w) {
+    if (!c->scored.on)
+        return moe_route_topk(x, c->router[layer], c->B, c->H, c->E, c->K, c->dtype, c->renorm, idx, w, nullptr, c->route_ws,
+                              c->route_ws_bytes, c->s);
+    float* z = reinterpret_cast<float*>(c->route_ws);
+    if (int rc = route_logits(x, c->router[layer], c->B, c->H, c->E, c->dtype, z, c->s)) return rc;
+    const auto& q = c->scored;
+    return route_scored_rows(z, c->B, c->E, c->K, q.score, q.bias ? q.bias + size_t(layer) * c->E : nullptr, q.n_groups,
+                             q.top_groups, q.group_top, c->renorm, q.scale, idx, w, c->s);
+}
+
 // One layer; `timing` permits the FFN events of timed tokens (off while a
 // graph is captured).  Arguments are checked by the callers.
 int decode_layer(moe_ctx* c, int token, int layer, const void* x, float* y, int mode, bool timing,
@@ -460,7 +482,7 @@ int decode_layer(moe_ctx* c, int token, int layer, const void* x, float* y, int 
         STMOE_HIP(hipStreamWaitEvent(c->s, c->ev_side, 0));
         c->side_pending = false;
     }
-    const int place = c->cache || c->mx ? kRouteTail : ffn_route_place(B, K, c->H, c->I, E, c->n_shared, c->dtype);
+    const int place = c->cache || c->mx || c->scored.on ? kRouteTail : ffn_route_place(B, K, c->H, c->I, E, c->n_shared, c->dtype);
     const bool plan = place == kRouteTailPlan, route_in_ffn = place == kRouteInFfn;
     const void* ebase = c->rbase.empty() ? nullptr : c->rbase[size_t(layer)];
     const void* const* sptr = c->n_shared ? c->shared + size_t(layer) * c->n_shared : nullptr;
@@ -493,8 +515,7 @@ int decode_layer(moe_ctx* c, int token, int layer, const void* x, float* y, int 
                                         c->tables + size_t(layer) * E, sptr, c->n_shared, c->ffn_ws, ebase, c->rstride,
                                         c->s))
                 return rc;
-        } else if (int rc = moe_route_topk(x, c->router[layer], B, c->H, E, K, c->dtype, c->renorm, idx_l, w_l,
-                                           nullptr, c->route_ws, c->route_ws_bytes, c->s)) {
+        } else if (int rc = route(c, layer, x, idx_l, w_l)) {
             return rc;
         }
         if (use && c->side && !defer_side) {
@@ -511,14 +532,17 @@ int decode_layer(moe_ctx* c, int token, int layer, const void* x, float* y, int 
     } else if (use) {
         // with a cache the host reads the prediction: one fused launch pair
         const int32_t* prev = layer > 0 ? c->idx + pbase + size_t(layer - 1) * B * K : nullptr;
-        if (int rc = fused_route_predict(x, c->router[layer], c->H, c->dtype, c->renorm, idx_l, w_l,
+        if (c->scored.on) {
+            if (int rc = route(c, layer, x, idx_l, w_l)) return rc;
+            if (int rc = update_predict(c->pred, layer, prev, idx_l, use, c->online, c->ranked, c->ranked + E,
+                                        max_scores(c->ranked, E), c->s))
+                return rc;
+        } else if (int rc = fused_route_predict(x, c->router[layer], c->H, c->dtype, c->renorm, idx_l, w_l,
                                          c->route_ws, c->pred, layer, prev, use, c->online, c->ranked,
                                          c->ranked + E, max_scores(c->ranked, E), c->s))
             return rc;
     } else {
-        if (int rc = moe_route_topk(x, c->router[layer], B, c->H, E, K, c->dtype, c->renorm, idx_l, w_l,
-                                    nullptr, c->route_ws, c->route_ws_bytes, c->s))
-            return rc;
+        if (int rc = route(c, layer, x, idx_l, w_l)) return rc;
     }
     // with a cache the routing record wait and the missed loads come next;
     // without one the FFN follows directly and its first event ends routing
@@ -871,6 +895,26 @@ extern "C" int moe_ctx_set_prefetch(moe_ctx* c, int min_score, int max_per_layer
     STMOE_CHECK(min_score >= 0 && max_per_layer >= 0, "knobs must be >= 0");
     c->pf_min_score = min_score;
     c->pf_max = max_per_layer;
+    ++c->settings;
+    return STMOE_OK;
+}
+
+extern "C" int moe_ctx_set_routing(moe_ctx* c, int score, const float* bias, int n_groups, int top_groups, int group_top,
+                                   float scale) {
+    clear_error();
+    STMOE_CHECK(c, "null ctx");
+    STMOE_CHECK(score == STMOE_SOFTMAX || score == STMOE_SIGMOID, "score must be STMOE_SOFTMAX or STMOE_SIGMOID");
+    STMOE_CHECK(scale > -INFINITY && scale < INFINITY, "scale must be finite");
+    if (const char* bad = bad_groups(c->E, c->K, n_groups, top_groups, group_top)) STMOE_CHECK(false, bad);
+    auto& q = c->scored;
+    // the plain router keeps its own launches
+    q.on = score != STMOE_SOFTMAX || bias || top_groups < n_groups || scale != 1.f;
+    q.score = score;
+    q.bias = bias;
+    q.n_groups = n_groups;
+    q.top_groups = top_groups;
+    q.group_top = group_top;
+    q.scale = scale;
     ++c->settings;
     return STMOE_OK;
 }

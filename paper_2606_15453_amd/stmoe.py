@@ -141,6 +141,7 @@ _SIGS = {
     "moe_decode_token": (i32, [vp, i32, vp, vp, i32]),
     "moe_ctx_set_prefetch": (i32, [vp, i32, i32]),
     "moe_ctx_set_online_update": (i32, [vp, i32]),
+    "moe_ctx_set_routing": (i32, [vp, i32, vp, i32, i32, i32, C.c_float]),
     "moe_ctx_set_predictor_batch": (i32, [vp, i32]),
     "moe_ctx_last_routing": (i32, [vp, vp, vp]),
     "moe_ctx_set_timing": (i32, [vp, i32]),
@@ -854,6 +855,14 @@ class DecodeContext:
     def set_online_update(self, on=True):
         """Algorithm 3's CCT update during decode on, or the CCTs frozen after profiling."""
         _call("moe_ctx_set_online_update", self.h, int(bool(on)))
+
+    def set_routing(self, score="softmax", bias=None, n_groups=1, top_groups=None, group_top=2, scale=1.0):
+        """Routing by scores as route_scored (bias [L][E], which must stay allocated); no arguments: the softmax top-K."""
+        if bias is not None:
+            _dense("bias", bias, (self.L, self.E), _F32, _device("bias", bias))
+        _call("moe_ctx_set_routing", self.h, _score(score), _p(bias), n_groups, n_groups if top_groups is None else top_groups,
+              group_top, scale)
+        self._bias = bias
 
     def token(self, token, xs, ys, mode=MODE_STMOE):
         _call("moe_decode_token", self.h, token, _p(xs), _p(ys), mode)

@@ -259,6 +259,28 @@ def test_large_batch_and_repeat():
     assert int(first[2].sum()) - 128 * 1000 == 20011 * 8
 
 
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("T,E,groups,top", [(7001, 64, 8, 3), (6600, 128, 1, 1), (6200, 64, 32, 9)])
+def test_large_batches_with_rows_of_every_kind(score, T, E, groups, top):
+    """Beyond the batches of one launch: rows of equal logits (more candidates than the selection in 32 bits takes), near
+    ones, NaN, infinities, masked ones, between ordinary ones; their counts are counted once."""
+    import torch
+    z = _logits(T, E, 50, "float32")
+    b = _bias(E, 50, 1e-3 if score == "sigmoid" else 1e-4)
+    z[5::97] = 0.25
+    z[6::101] = z[6::101].round()
+    z[7::103] = z[8] + 1e-6 * z[7::103]
+    z[9::211] = -float("inf")
+    z[10::223, 3:] = -float("inf")
+    z[12::499, 7] = -float("inf")
+    z[13::1009, 11] = float("nan") if score == "sigmoid" else 80.0
+    z[-1] = z[-2]
+    mask = torch.ones(T, dtype=torch.uint8, device=DEV)
+    mask[::41] = 0
+    for bias in (b, None, torch.zeros(E, device=DEV)):
+        _check(z, 6, score, bias, groups, top, 2, renorm=True, scale=1.5, mask=mask)
+
+
 def test_streams_and_graphs():
     """On another stream; captured and replayed over new logits between eager work."""
     import torch
