@@ -7,9 +7,11 @@
 // y, dx), and over the tokens of an adapter (outer: dA, dB).  A and B are both held
 // by ranks, [r][columns], so each product serves both.  v and u are fp32 throughout.
 //
-// The plan's tiles hold tokens of one adapter.  These kernels run on the fp32 matrix
-// instruction (16 x 16 x 4): bf16 values are exact in it, and a lane takes one value
-// of each operand at a time, so any layout of rows and columns does.
+// The plan's tiles hold tokens of one adapter.  These kernels take fp32 rows and bf16
+// ones of any length, stride and alignment (lora_bf16.hip takes bf16 ones in whole 16-byte
+// chunks).  They run on the fp32 matrix instruction (16 x 16 x 4): bf16 values are exact
+// in it, and a lane takes one value of each operand at a time, so any layout of rows and
+// columns does.  Rows that allow it are loaded four values at once (VEC).
 #include <type_traits>
 
 #include "lora.h"
@@ -32,14 +34,38 @@ __device__ __forceinline__ float at(const void* p, int64_t i) {
     return BF ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(p)[i]) << 16)
               : reinterpret_cast<const float*>(p)[i];
 }
+// Values i to i + 3 of a row of C; 0 beyond it and where `in` is false.  VEC: C and i are
+// multiples of 4, the row is aligned to four values.
+template <bool BF, bool VEC>
+__device__ __forceinline__ void at4(const void* p, int64_t row, int i, int C, bool in, float (&v)[4]) {
+    if constexpr (VEC) {
+        in = in && i < C;
+        const int64_t k = in ? row + i : 0;        // row 0 of the matrix is there for all
+        if constexpr (BF) {
+            const uint2 q = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(p) + k);
+            v[0] = in ? bf16_lo(q.x) : 0.f;
+            v[1] = in ? bf16_hi(q.x) : 0.f;
+            v[2] = in ? bf16_lo(q.y) : 0.f;
+            v[3] = in ? bf16_hi(q.y) : 0.f;
+        } else {
+            const f32x4 q = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(p) + k);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = in ? q[j] : 0.f;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = in && i + j < C ? at<BF>(p, row + i + j) : 0.f;
+    }
+}
 template <bool BF>
 __device__ __forceinline__ void put(void* p, int64_t i, float v) {
     if (BF) reinterpret_cast<__bf16*>(p)[i] = __bf16(v);
     else reinterpret_cast<float*>(p)[i] = v;
 }
 
-// One tile of 16 tokens a workgroup, its waves a part of the columns each.
-template <bool BF, int RT>
+// One tile of 16 tokens a workgroup and, with several parts, some of the columns; its
+// waves every fourth 16 of them.
+template <bool BF, int RT, bool VEC>
 __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs a) {
     __shared__ float part[kWaves][RT * 16][17];
     Tile tile;
@@ -48,28 +74,26 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int rank = rank_of(a.g, tile.adapter);
     const void* m = a.m[tile.adapter];
-    const bool in = c < tile.count;
-    const int t = a.g.plan.order[tile.first + (in ? c : 0)];
+    // tokens beyond the last one: the first, whose sums are not stored again
+    const int64_t t = a.g.plan.order[tile.first + (c < tile.count ? c : 0)];
     f32x4 acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int h0 = 16 * wave; h0 < a.C; h0 += 16 * kWaves) {
-        float xv[4];
+    if (rank > 0)
+#pragma unroll(RT <= 2 ? 4 : 1)
+        for (int h0 = 16 * (wave + kWaves * int(blockIdx.y)); h0 < a.C; h0 += 16 * kWaves * int(gridDim.y)) {
+            float xv[4], mv[RT][4];
+            at4<BF, VEC>(a.x, t * a.ld, h0 + 4 * q, a.C, true, xv);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int h = h0 + 4 * q + j;
-            xv[j] = in && h < a.C ? at<BF>(a.x, t * a.ld + h) : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int r = 16 * i + c;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int h = h0 + 4 * q + j;
-                acc[i] = mfma(r < rank && h < a.C ? at<BF>(m, int64_t(r) * a.C + h) : 0.f, xv[j], acc[i]);
+            for (int i = 0; i < RT; ++i) {
+                const int r = 16 * i + c;          // ranks beyond the last one: the first's, not stored
+                at4<BF, VEC>(m, int64_t(r < rank ? r : 0) * a.C, h0 + 4 * q, a.C, true, mv[i]);
             }
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i] = mfma(mv[i][j], xv[j], acc[i]);
         }
-    }
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -81,13 +105,13 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs a) {
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) sum += part[w][r][k];
-        a.v[int64_t(a.g.plan.order[tile.first + k]) * a.g.R + r] = r < rank ? s * sum : 0.f;
+        a.v[(int64_t(blockIdx.y) * a.g.T + a.g.plan.order[tile.first + k]) * a.g.R + r] = r < rank ? s * sum : 0.f;
     }
 }
 
 // One tile of 16 tokens and 256 columns a workgroup, 64 columns a wave: the lane
 // (c, q) feeds columns 4 c + j of row 4 q + i and gets columns 16 q .. + 15 of token c.
-template <bool BF, bool YBF>
+template <bool BF, bool YBF, bool VEC>
 __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
     Tile tile;
     if (!tile_of(a.g, blockIdx.x, tile)) return;
@@ -111,16 +135,15 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
         const int rank = rank_of(a.g, tile.adapter);
         const void* m = a.m[tile.adapter];
         if (a.scaled && a.g.scales) s = a.g.scales[tile.adapter];
+#pragma unroll 4
         for (int r0 = 0; r0 < rank; r0 += 4) {
             const int r = r0 + q;
-            float vv = 0.f;
+            float vv = 0.f, mv[4];
             if (in && r < rank)
                 for (int p = 0; p < a.parts; ++p) vv += a.v[(int64_t(p) * a.g.T + t) * a.g.R + r];
+            at4<BF, VEC>(m, int64_t(r) * a.C, o0 + 4 * c, a.C, r < rank, mv);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int o = o0 + 4 * c + j;
-                acc[j] = mfma(r < rank && o < a.C ? at<BF>(m, int64_t(r) * a.C + o) : 0.f, vv, acc[j]);
-            }
+            for (int j = 0; j < 4; ++j) acc[j] = mfma(mv[j], vv, acc[j]);
         }
     }
     if (!in) return;
@@ -136,38 +159,40 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
         }
 }
 
-// One adapter and 64 columns a workgroup, its waves a part of the tokens each.
-template <bool BF, int RT>
-__global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs a) {
+// A tile of tokens and 64 columns a workgroup, its waves every fourth four of the tokens.
+template <bool BF, int RT, bool VEC>
+__global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs ox, OuterArgs oy) {
     __shared__ float part[kWaves][16][65];
-    if (!planned(a.g)) return;
+    const OuterArgs a = one_of(blockIdx.z, ox, oy);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
-    const int ad = blockIdx.x, h0 = blockIdx.y * 64;
-    const int rank = rank_of(a.g, ad), t0 = a.g.plan.seg[ad], t1 = a.g.plan.seg[ad + 1];
+    const int h0 = blockIdx.x * 64;
+    Tile tile;
+    if (!tile_of(a.g, blockIdx.y, tile) || tile.adapter < 0 || h0 >= a.C) return;
+    const int rank = rank_of(a.g, tile.adapter), tiles = a.g.plan.base[tile.adapter + 1] - a.g.plan.base[tile.adapter];
     f32x4 acc[RT][4];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int p0 = t0 + 4 * wave; p0 < t1; p0 += 4 * kWaves) {
-        const bool in = p0 + q < t1;
-        const int64_t t = a.g.plan.order[in ? p0 + q : t0];
-        float xv[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int h = h0 + 4 * c + j;
-            xv[j] = in && h < a.C ? at<BF>(a.x, t * a.ld + h) : 0.f;
-        }
+#pragma unroll(RT <= 2 ? 4 : 1)
+    for (int p0 = 4 * wave; p0 < tile.count; p0 += 4 * kWaves) {
+        const bool in = p0 + q < tile.count;
+        const int64_t t = a.g.plan.order[tile.first + (in ? p0 + q : 0)];
+        float xv[4], uv[RT];
+        at4<BF, VEC>(a.x, t * a.ld, h0 + 4 * c, a.C, in, xv);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int r = 16 * i + c;
-            const float uv = in && r < rank ? a.u[t * a.g.R + r] : 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = mfma(xv[j], uv, acc[i][j]);
+            uv[i] = in && r < rank ? a.u[t * a.g.R + r] : 0.f;
         }
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = mfma(xv[j], uv[i], acc[i][j]);
     }
-    const float s = a.scaled && a.g.scales ? a.g.scales[ad] : 1.f;
-    float* d = a.d[ad];
+    const float s = a.scaled && a.g.scales ? a.g.scales[tile.adapter] : 1.f;
+    float* d = tiles == 1 ? a.d[tile.adapter]
+                          : a.part + int64_t(outer_slot(tile.first, a.g.plan.size, tile.piece == tiles - 1)) * a.g.R * a.C;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         __syncthreads();
@@ -205,6 +230,36 @@ int column_parts(int T, int n, int C) {
     return p;
 }
 
+// The gradients of adapters with several tiles, their sums in order, and of those
+// without a token: zeros.  W values at once: C is a multiple of W.
+template <int W>
+__global__ __launch_bounds__(kThreads) void lora_join_kernel(OuterArgs ox, OuterArgs oy) {
+    typedef float vec __attribute__((ext_vector_type(W)));
+    const OuterArgs a = one_of(blockIdx.z, ox, oy);
+    const int ad = blockIdx.x, size = a.g.plan.size;
+    // side by side
+    const int tiles = a.g.plan.base[ad + 1] - a.g.plan.base[ad], first = a.g.plan.seg[ad];
+    const int64_t all = int64_t(rank_of(a.g, ad)) * a.C, part = int64_t(a.g.R) * a.C;
+    float* d = a.d[ad];
+    if (!planned(a.g) || tiles == 1) return;
+    for (int64_t i = W * (int64_t(blockIdx.y) * kThreads + threadIdx.x); i < all; i += W * int64_t(gridDim.y) * kThreads) {
+        vec sum = 0.f;
+        for (int k0 = 0; k0 < tiles; k0 += 8) {    // eight loads at once
+            vec v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = k0 + j;
+                v[j] = 0.f;
+                if (k < tiles)
+                    v[j] = *reinterpret_cast<const vec*>(a.part + outer_slot(first + k * size, size, k == tiles - 1) * part + i);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += v[j];
+        }
+        *reinterpret_cast<vec*>(d + i) = sum;
+    }
+}
+
 // Tokens per tile of the sums over tokens: 256, and 1024 for ranks above 16, whose sums
 // (R x C fp32 a tile) would be as many bytes as the rows.
 int outer_table(int, int, int R) { return R <= 16 ? 2 : 3; }
@@ -221,10 +276,26 @@ void with_rank(int R, F f) {
     else f(std::integral_constant<int, 8>());
 }
 
+// Rows of C values that are loaded four at once.
+bool fours(const void* p, int64_t ld, int C, int esz) {
+    return C % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * esz) == 0;
+}
+
+// Calls f(bf16, VEC).
+template <class F>
+void with_rows(bool bf, bool vec, F f) {
+    if (bf && vec) f(std::true_type(), std::true_type());
+    else if (bf) f(std::true_type(), std::false_type());
+    else if (vec) f(std::false_type(), std::true_type());
+    else f(std::false_type(), std::false_type());
+}
+
 int shrink(const ShrinkArgs& a, int tiles, bool bf, hipStream_t s) {
-    with_rank(a.g.R, [&](auto rt) {
-        if (bf) hipLaunchKernelGGL((lora_shrink_kernel<true, rt()>), dim3(unsigned(tiles)), dim3(kThreads), 0, s, a);
-        else hipLaunchKernelGGL((lora_shrink_kernel<false, rt()>), dim3(unsigned(tiles)), dim3(kThreads), 0, s, a);
+    const dim3 grid(unsigned(tiles), unsigned(a.parts));
+    with_rows(bf, fours(a.x, a.ld, a.C, bf ? 2 : 4), [&](auto b, auto vec) {
+        with_rank(a.g.R, [&](auto rt) {
+            hipLaunchKernelGGL((lora_shrink_kernel<b(), rt(), vec()>), grid, dim3(kThreads), 0, s, a);
+        });
     });
     STMOE_LAUNCHED();
     return STMOE_OK;
@@ -232,20 +303,34 @@ int shrink(const ShrinkArgs& a, int tiles, bool bf, hipStream_t s) {
 
 int expand(const ExpandArgs& a, int tiles, bool bf, bool ybf, hipStream_t s) {
     const dim3 grid(unsigned(tiles), unsigned((a.C + 64 * kWaves - 1) / (64 * kWaves)));
-    if (bf && ybf) hipLaunchKernelGGL((lora_expand_kernel<true, true>), grid, dim3(kThreads), 0, s, a);
-    else if (bf) hipLaunchKernelGGL((lora_expand_kernel<true, false>), grid, dim3(kThreads), 0, s, a);
-    else if (ybf) hipLaunchKernelGGL((lora_expand_kernel<false, true>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((lora_expand_kernel<false, false>), grid, dim3(kThreads), 0, s, a);
+    with_rows(bf, a.C % 4 == 0, [&](auto b, auto vec) {
+        if (ybf) hipLaunchKernelGGL((lora_expand_kernel<b(), true, vec()>), grid, dim3(kThreads), 0, s, a);
+        else hipLaunchKernelGGL((lora_expand_kernel<b(), false, vec()>), grid, dim3(kThreads), 0, s, a);
+    });
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
 
-int outer(const OuterArgs& a, bool bf, hipStream_t s) {
-    const dim3 grid(unsigned(a.g.n), unsigned((a.C + 63) / 64));
-    with_rank(a.g.R, [&](auto rt) {
-        if (bf) hipLaunchKernelGGL((lora_outer_kernel<true, rt()>), grid, dim3(kThreads), 0, s, a);
-        else hipLaunchKernelGGL((lora_outer_kernel<false, rt()>), grid, dim3(kThreads), 0, s, a);
+int outer(const OuterArgs (&a)[2], int table, bool bf, hipStream_t s) {
+    const int C = a[0].C > a[1].C ? a[0].C : a[1].C;
+    const dim3 grid(unsigned((C + 63) / 64), unsigned(plan_layout(a[0].g.T, a[0].g.n).max_tiles[table]), 2);
+    const int esz = bf ? 2 : 4;
+    with_rows(bf, fours(a[0].x, a[0].ld, a[0].C, esz) && fours(a[1].x, a[1].ld, a[1].C, esz), [&](auto b, auto vec) {
+        with_rank(a[0].g.R, [&](auto rt) {
+            hipLaunchKernelGGL((lora_outer_kernel<b(), rt(), vec()>), grid, dim3(kThreads), 0, s, a[0], a[1]);
+        });
     });
+    STMOE_LAUNCHED();
+    return STMOE_OK;
+}
+
+int join(const OuterArgs (&a)[2], hipStream_t s) {
+    const int C = a[0].C > a[1].C ? a[0].C : a[1].C, n = a[0].g.n;
+    const bool vec = a[0].C % 4 == 0 && a[1].C % 4 == 0;
+    const int64_t chunks = (int64_t(a[0].g.R) * C / (vec ? 4 : 1) + kThreads - 1) / kThreads, most = n < 64 ? 512 / n : 8;
+    const dim3 grid(unsigned(n), unsigned(chunks < most ? chunks : most), 2);
+    if (vec) hipLaunchKernelGGL(lora_join_kernel<4>, grid, dim3(kThreads), 0, s, a[0], a[1]);
+    else hipLaunchKernelGGL(lora_join_kernel<1>, grid, dim3(kThreads), 0, s, a[0], a[1]);
     STMOE_LAUNCHED();
     return STMOE_OK;
 }
@@ -260,9 +345,8 @@ int shrink_expand(ShrinkArgs sh, ExpandArgs ex, int dtype, int ydtype, hipStream
     const bool fast_expand = bf && ex.C % 8 == 0 && chunks16(ex.y, ex.ld, ex.C, ysz) &&
                              (!ex.base || chunks16(ex.base, ex.ld_base, ex.C, ysz));
     const int table = large_tiles(sh.g.T, sh.g.n) ? 1 : 0;
-    if (!fast_shrink || sh.parts == 1) {
+    if (sh.parts == 1) {
         // one part: where the caller wants it
-        sh.parts = ex.parts = 1;
         if (ex.v_out) sh.v = ex.v_out;
         ex.v = sh.v;
     }
@@ -367,9 +451,10 @@ extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int
         return rc;
     const int table = outer_table(T, n_adapters, R);
     float* sums = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + rows_bytes(T, R) + rows_bytes(part_rows(T), R));
-    const OuterArgs o[2] = {{g, x, ldx, Hin, u, 0, da_ptrs, sums},
-                            {g, dy, ld_dy, Hout, v, 1, db_ptrs, sums + outer_slots(T, tile_tokens(table)) * R * Hin}};
-    if (bf && chunks16(x, ldx, Hin, 2) && chunks16(dy, ld_dy, Hout, 2)) return outer_bf16(o, table, s);
-    if (int rc = outer(o[1], bf, s)) return rc;
-    return outer(o[0], bf, s);
+    const Args gt = with_table(g, table);
+    const OuterArgs o[2] = {{gt, x, ldx, Hin, u, 0, da_ptrs, sums},
+                            {gt, dy, ld_dy, Hout, v, 1, db_ptrs, sums + outer_slots(T, tile_tokens(table)) * R * Hin}};
+    const bool fast = bf && chunks16(x, ldx, Hin, 2) && chunks16(dy, ld_dy, Hout, 2);
+    if (int rc = fast ? outer_bf16(o, table, s) : outer(o, table, bf, s)) return rc;
+    return join(o, s);
 }

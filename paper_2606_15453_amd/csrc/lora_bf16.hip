@@ -367,20 +367,6 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_
 // workgroup, in LDS, 128 tokens at a time.
 constexpr int kStage = 4;          // times 32 tokens
 
-// One of two calls' arguments, field by field: a reference to either would put both into
-// scratch memory (lora_outer_bf16_kernel 31 us for it, not 21, lora_join_kernel 13.4, not 4.9).
-__device__ __forceinline__ OuterArgs one_of(bool second, const OuterArgs& p, const OuterArgs& o) {
-    OuterArgs a = p;
-    a.x = second ? o.x : p.x;
-    a.ld = second ? o.ld : p.ld;
-    a.C = second ? o.C : p.C;
-    a.u = second ? o.u : p.u;
-    a.scaled = second ? o.scaled : p.scaled;
-    a.d = second ? o.d : p.d;
-    a.part = second ? o.part : p.part;
-    return a;
-}
-
 template <int RT>
 __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox, OuterArgs oy) {
     constexpr int P = 3;
@@ -483,39 +469,9 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
         }
 }
 
-// The gradients of adapters with several tiles, their sums in order, and of those
-// without a token: zeros.
-__global__ __launch_bounds__(kThreads) void lora_join_kernel(OuterArgs ox, OuterArgs oy) {
-    const OuterArgs a = one_of(blockIdx.z, ox, oy);
-    const int ad = blockIdx.x, size = a.g.plan.size;
-    // side by side
-    const int tiles = a.g.plan.base[ad + 1] - a.g.plan.base[ad], first = a.g.plan.seg[ad];
-    const int64_t all = int64_t(rank_of(a.g, ad)) * a.C, part = int64_t(a.g.R) * a.C;
-    float* d = a.d[ad];
-    if (!planned(a.g) || tiles == 1) return;
-    for (int64_t i = 4 * (int64_t(blockIdx.y) * kThreads + threadIdx.x); i < all; i += 4 * int64_t(gridDim.y) * kThreads) {
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        for (int k0 = 0; k0 < tiles; k0 += 8) {    // eight loads at once
-            f32x4 v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int k = k0 + j;
-                v[j] = k < tiles ? *reinterpret_cast<const f32x4*>(
-                                       a.part + outer_slot(first + k * size, size, k == tiles - 1) * part + i)
-                                 : f32x4{0.f, 0.f, 0.f, 0.f};
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += v[j];
-        }
-        *reinterpret_cast<f32x4*>(d + i) = sum;
-    }
-}
-
 }  // namespace
 
-int outer_bf16(const OuterArgs (&o)[2], int table, hipStream_t s) {
-    OuterArgs a[2] = {o[0], o[1]};
-    for (OuterArgs& g : a) g.g = with_table(g.g, table);
+int outer_bf16(const OuterArgs (&a)[2], int table, hipStream_t s) {
     const int R = a[0].g.R, C = a[0].C > a[1].C ? a[0].C : a[1].C, n = a[0].g.n;
     const dim3 grid(unsigned((C + 128 * kWaves - 1) / (128 * kWaves)), unsigned(plan_layout(a[0].g.T, n).max_tiles[table]),
                     R > 64 ? 4 : 2);
@@ -525,10 +481,6 @@ int outer_bf16(const OuterArgs (&o)[2], int table, hipStream_t s) {
     if (R <= 16) go(std::integral_constant<int, 1>());
     else if (R <= 32) go(std::integral_constant<int, 2>());
     else go(std::integral_constant<int, 4>());
-    STMOE_LAUNCHED();
-    const int64_t chunks = (int64_t(R) * C / 4 + kThreads - 1) / kThreads, most = n < 64 ? 512 / n : 8;
-    hipLaunchKernelGGL(lora_join_kernel, dim3(unsigned(n), unsigned(chunks < most ? chunks : most), 2), dim3(kThreads), 0, s,
-                       a[0], a[1]);
     STMOE_LAUNCHED();
     return STMOE_OK;
 }

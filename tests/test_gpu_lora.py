@@ -130,7 +130,7 @@ class Batch:
 SHAPES = [(1, 64, 64, 1, 16), (1, 2048, 2048, 8, 16), (2, 8, 8, 3, 1), (16, 256, 128, 16, 8), (17, 512, 256, 3, 64),
           (37, 1000, 61, 5, 12), (64, 1024, 768, 32, 64), (130, 72, 1032, 2, 33), (300, 520, 1000, 3, 12),
           (33, 264, 24, 40, 128), (600, 384, 640, 2, 100), (5, 1, 1, 2, 3), (50, 31, 257, 4, 20), (2500, 136, 72, 2, 40), (1300, 520, 264, 1, 16),
-          (2300, 64, 88, 1, 70)]
+          (2300, 64, 88, 1, 70), (700, 61, 33, 1, 5)]
 
 
 @pytest.mark.parametrize("dtype,ydtype", [("bfloat16", "bfloat16"), ("bfloat16", "float32"), ("float32", "float32"),
