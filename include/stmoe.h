@@ -443,7 +443,8 @@ int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapter
  *           NULL: not computed; base may be dx when ld_base = ld_dx)
  *   dA_a  = scale_a * sum over a's tokens of (dy[t] B_a^T)^T x[t]
  *   dB_a  = scale_a * sum over a's tokens of v[t]^T dy[t]
- *   base, dx   device [T] rows of Hin values, dtype
+ *   base, dx   device [T] rows of Hin values, dtype; dx does not overlap x,
+ *              dy or v, which are read after it is written
  *   da_ptrs    device array [n_adapters] of device pointers to fp32 [r][Hin],
  *              16-byte aligned; db_ptrs so to fp32 [r][Hout].  Overwritten,
  *              with zeros for an adapter without tokens; no two may overlap

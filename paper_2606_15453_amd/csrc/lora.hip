@@ -434,6 +434,7 @@ extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int
         if (const char* bad = bad_rows(dx, ld_dx, Hin, dtype)) STMOE_CHECK(false, bad);
     if (dx && base)
         if (const char* bad = bad_rows(base, ld_base, Hin, dtype)) STMOE_CHECK(false, bad);
+    STMOE_CHECK(!dx || (dx != x && dx != dy), "dx must not be x or dy");
     STMOE_CHECK(!dx || base != dx || ld_base == ld_dx, "base in the place of dx must have its row stride");
     STMOE_CHECK(ws_bytes >= moe_lora_backward_workspace_bytes(T, Hin, Hout, n_adapters, R, dtype), "workspace too small");
     STMOE_CHECK(reinterpret_cast<uintptr_t>(ws) % 256 == 0 && reinterpret_cast<uintptr_t>(plan) % 256 == 0,

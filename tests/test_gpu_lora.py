@@ -130,7 +130,8 @@ class Batch:
 SHAPES = [(1, 64, 64, 1, 16), (1, 2048, 2048, 8, 16), (2, 8, 8, 3, 1), (16, 256, 128, 16, 8), (17, 512, 256, 3, 64),
           (37, 1000, 61, 5, 12), (64, 1024, 768, 32, 64), (130, 72, 1032, 2, 33), (300, 520, 1000, 3, 12),
           (33, 264, 24, 40, 128), (600, 384, 640, 2, 100), (5, 1, 1, 2, 3), (50, 31, 257, 4, 20), (2500, 136, 72, 2, 40), (1300, 520, 264, 1, 16),
-          (2300, 64, 88, 1, 70), (700, 61, 33, 1, 5)]
+          (2300, 64, 88, 1, 70), (700, 61, 33, 1, 5),
+          (20, 2048, 61, 3, 12), (20, 1027, 64, 3, 8), (20, 61, 2048, 2, 8), (3, 8192, 4096, 2, 16)]
 
 
 @pytest.mark.parametrize("dtype,ydtype", [("bfloat16", "bfloat16"), ("bfloat16", "float32"), ("float32", "float32"),
@@ -286,6 +287,16 @@ def test_a_plan_of_another_batch_writes_nothing():
     assert (y == 2).all()
     _, dA, dB = b.backward(torch.zeros((40, 8), device=DEV))
     assert all(torch.isnan(m).all() for m in dA + dB)
+
+
+def test_the_gradient_of_x_does_not_take_its_place():
+    from paper_2606_15453_amd import stmoe as S
+    import torch
+    b = Batch(8, 64, 64, 2, 8, seed=19)
+    v = torch.zeros((8, 8), device=DEV)
+    for bad in (b.x, b.dy):
+        with pytest.raises(S.StmoeError):
+            b.backward(v, dx=bad)
 
 
 def test_streams_and_graphs():

@@ -52,7 +52,8 @@ def test_backward_refusals():
     for bad in [dict(x=None), dict(dy=None), dict(v=None), dict(plan=None), dict(ap=None), dict(bp=None), dict(da=None),
                 dict(db=None), dict(ws=None), dict(T=0), dict(T=65537), dict(Hin=0), dict(Hout=65537, ldy=65537), dict(n=0),
                 dict(R=129), dict(dt=2), dict(ldx=63), dict(ldy=31), dict(ldd=63), dict(ldb=63), dict(x=257), dict(dy=257),
-                dict(dx=257), dict(base=257), dict(v=264), dict(plan=264), dict(ws=264), dict(nb=16), dict(base=512, ldb=72)]:
+                dict(dx=257), dict(base=257), dict(v=264), dict(plan=264), dict(ws=264), dict(nb=16), dict(base=512, ldb=72),
+                dict(dx=256), dict(x=512)]:
         a = dict(ok, **bad)
         rc = L.moe_lora_backward(a["x"], a["ldx"], a["dy"], a["ldy"], a["v"], a["T"], a["Hin"], a["Hout"], a["n"], a["R"],
                                  a["dt"], a["plan"], a["ap"], a["bp"], None, None, a["da"], a["db"], a["base"], a["ldb"],
