@@ -11,7 +11,10 @@
 // ones of any length, stride and alignment (lora_bf16.hip takes bf16 ones in whole 16-byte
 // chunks).  They run on the fp32 matrix instruction (16 x 16 x 4): bf16 values are exact
 // in it, and a lane takes one value of each operand at a time, so any layout of rows and
-// columns does.  Rows that allow it are loaded four values at once (VEC).
+// columns does.  Rows that allow it are loaded four values at once (VEC).  Small calls
+// are bound by the latency of tile, order and rows, one load after the other (37 x 1000 x
+// 61 fp32: 6.6 and 6.3 us); large ones by the instruction and by loads of a row a lane:
+// 4096 x 2048 x 2048 fp32, rank 64, 171 us for 100 MB and 2.1 GFLOP.
 #include <type_traits>
 
 #include "lora.h"

@@ -94,6 +94,9 @@ __device__ __forceinline__ void load8(const float* row, int64_t part, int parts,
 // LDS, each wave's own: eight consecutive lanes load 128 bytes of one, where the matrix
 // instruction's operand has a row a lane, and loads in that order get 16 bytes a cycle
 // and CU out of the cache (4096 tokens x 4096, rank 16: 12.4 us so, 18.1 without LDS).
+// Bound by the rows from HBM and, at larger ranks, as much again of A out of the L2s for
+// every 32 tokens: 8192 x 4096, rank 64, 28.6 us, 2.3 TB/s of rows (64 tokens a workgroup
+// 27.8 in two parts, which cost the next launch more; 16 tokens 32.7).
 template <int RT, int NT>
 __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a) {
     constexpr int TOK = 16 * NT, LD = 16 * RT + 4, ROWS = 16 * (NT + RT);
@@ -230,7 +233,10 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 // the column operand, that of instruction j being columns 8 c + j: it gets columns 8 c
 // .. + 7 of tokens 4 q .. + 3, so that 16 lanes load and store 256 bytes of a row.  v's
 // pieces are made once for the workgroup, in LDS.  With a rank of 16 at most the lanes q =
-// 2, 3 hold the same ranks as q = 0, 1, against the second piece of v.
+// 2, 3 hold the same ranks as q = 0, 1, against the second piece of v.  Bound by base and
+// y: 8192 x 4096 bf16, rank 64, 37.1 us, 3.6 TB/s of them (128 tokens a workgroup 39; with
+// columns as the row operand, 16 bytes of each of 64 rows a store, 49); 4096 x 4096, rank
+// 16, 19.3 us, 3.5 TB/s.
 template <int KS, bool PACK, bool YBF, int NS>
 __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_bf16_kernel(ExpandArgs a) {
     constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P, W = YBF ? 1 : 2;
@@ -364,7 +370,8 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_
 // tiles).  512 columns and up to 64 ranks a workgroup, 128 columns a wave, 32 tokens at
 // a time: the lane (c, q) loads columns 8 c .. + 7 of tokens 8 q .. + 7, the column
 // operand of instruction j being columns 8 c + j, and gets them of ranks 4 q .. + 3.  u's three pieces are made once for the
-// workgroup, in LDS, 128 tokens at a time.
+// workgroup, in LDS, 128 tokens at a time.  Bound by the rows: both gradients of 4096 x
+// 4096 each way, rank 16, in 19.7 us, 3.4 TB/s and 8 MB of sums of tiles on top.
 constexpr int kStage = 4;          // times 32 tokens
 
 template <int RT>
