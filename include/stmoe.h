@@ -408,7 +408,8 @@ int moe_expert_ffn_mx(const void* x, const int32_t* topk_idx, const float* topk_
  * moe_lora_plan sorts a batch's tokens by adapter, once for every projection
  * of every layer that the batch passes.  plan: device, 256-byte aligned,
  * moe_lora_plan_bytes(T, n_adapters) bytes, read by the calls that take it
- * with the same T and n_adapters (with others they write nothing).
+ * with the same T and n_adapters (where it is the plan of others, in a buffer
+ * large enough, they write nothing).
  *   adapter  device [T] int32
  *   0 <= T <= 65536, 1 <= n_adapters <= 4096
  * ---------------------------------------------------------------------- */
@@ -434,8 +435,8 @@ int moe_lora_plan(const int32_t* adapter, int T, int n_adapters, void* plan, siz
  * is held in 32 bits.  The same inputs give the same bits. */
 size_t moe_lora_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype);
 int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapters, int R, int dtype, int ydtype,
-             const void* plan, const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks,
-             const float* scales, const void* base, int64_t ld_base, void* y, int64_t ldy, float* v, void* ws,
+             const void* plan, size_t plan_bytes, const void* const* a_ptrs, const void* const* b_ptrs,
+             const int32_t* ranks, const float* scales, const void* base, int64_t ld_base, void* y, int64_t ldy, float* v, void* ws,
              size_t ws_bytes, void* stream);
 /* Its gradient, for T >= 1: from dy (device [T] rows of Hout values, row stride
  * ld_dy, dtype), x and v as moe_lora took and gave them,
@@ -451,8 +452,8 @@ int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapter
  *   ws         moe_lora_backward_workspace_bytes(...) bytes, as above */
 size_t moe_lora_backward_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype);
 int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int64_t ld_dy, const float* v, int T, int Hin,
-                      int Hout, int n_adapters, int R, int dtype, const void* plan, const void* const* a_ptrs,
-                      const void* const* b_ptrs, const int32_t* ranks, const float* scales, float* const* da_ptrs,
+                      int Hout, int n_adapters, int R, int dtype, const void* plan, size_t plan_bytes,
+                      const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks, const float* scales, float* const* da_ptrs,
                       float* const* db_ptrs, const void* base, int64_t ld_base, void* dx, int64_t ld_dx, void* ws,
                       size_t ws_bytes, void* stream);
 

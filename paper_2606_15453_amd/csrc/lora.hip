@@ -393,8 +393,8 @@ extern "C" size_t moe_lora_workspace_bytes(int T, int Hin, int Hout, int n_adapt
 }
 
 extern "C" int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapters, int R, int dtype, int ydtype,
-                        const void* plan, const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks,
-                        const float* scales, const void* base, int64_t ld_base, void* y, int64_t ldy, float* v, void* ws,
+                        const void* plan, size_t plan_bytes, const void* const* a_ptrs, const void* const* b_ptrs,
+                        const int32_t* ranks, const float* scales, const void* base, int64_t ld_base, void* y, int64_t ldy, float* v, void* ws,
                         size_t ws_bytes, void* stream) {
     clear_error();
     if (const char* bad = bad_call(T, Hin, Hout, n_adapters, R, dtype, ydtype)) STMOE_CHECK(false, bad);
@@ -405,6 +405,7 @@ extern "C" int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, in
     if (base)
         if (const char* bad = bad_rows(base, ld_base, Hout, ydtype)) STMOE_CHECK(false, bad);
     STMOE_CHECK(base != y || ld_base == ldy, "base in the place of y must have its row stride");
+    STMOE_CHECK(plan_bytes >= moe_lora_plan_bytes(T, n_adapters), "plan too small");
     STMOE_CHECK(ws_bytes >= moe_lora_workspace_bytes(T, Hin, Hout, n_adapters, R, dtype), "workspace too small");
     STMOE_CHECK(reinterpret_cast<uintptr_t>(ws) % 256 == 0 && reinterpret_cast<uintptr_t>(plan) % 256 == 0,
                 "ws and plan must be 256-byte aligned");
@@ -423,8 +424,8 @@ extern "C" size_t moe_lora_backward_workspace_bytes(int T, int Hin, int Hout, in
 }
 
 extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int64_t ld_dy, const float* v, int T, int Hin,
-                                 int Hout, int n_adapters, int R, int dtype, const void* plan, const void* const* a_ptrs,
-                                 const void* const* b_ptrs, const int32_t* ranks, const float* scales, float* const* da_ptrs,
+                                 int Hout, int n_adapters, int R, int dtype, const void* plan, size_t plan_bytes,
+                                 const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks, const float* scales, float* const* da_ptrs,
                                  float* const* db_ptrs, const void* base, int64_t ld_base, void* dx, int64_t ld_dx, void* ws,
                                  size_t ws_bytes, void* stream) {
     clear_error();
@@ -439,6 +440,7 @@ extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int
         if (const char* bad = bad_rows(base, ld_base, Hin, dtype)) STMOE_CHECK(false, bad);
     STMOE_CHECK(!dx || (dx != x && dx != dy), "dx must not be x or dy");
     STMOE_CHECK(!dx || base != dx || ld_base == ld_dx, "base in the place of dx must have its row stride");
+    STMOE_CHECK(plan_bytes >= moe_lora_plan_bytes(T, n_adapters), "plan too small");
     STMOE_CHECK(ws_bytes >= moe_lora_backward_workspace_bytes(T, Hin, Hout, n_adapters, R, dtype), "workspace too small");
     STMOE_CHECK(reinterpret_cast<uintptr_t>(ws) % 256 == 0 && reinterpret_cast<uintptr_t>(plan) % 256 == 0,
                 "ws and plan must be 256-byte aligned");

@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 // .. + 7 of tokens 4 q .. + 3, so that 16 lanes load and store 256 bytes of a row.  v's
 // pieces are made once for the workgroup, in LDS.  With a rank of 16 at most the lanes q =
 // 2, 3 hold the same ranks as q = 0, 1, against the second piece of v.  Bound by base and
-// y: 8192 x 4096 bf16, rank 64, 37.1 us, 3.6 TB/s of them (128 tokens a workgroup 39; with
+// y: 8192 x 4096 bf16, rank 64, 35.2 us, 3.8 TB/s of them (128 tokens a workgroup 39; with
 // columns as the row operand, 16 bytes of each of 64 rows a store, 49); 4096 x 4096, rank
 // 16, 19.3 us, 3.5 TB/s.
 template <int KS, bool PACK, bool YBF, int NS>
@@ -272,6 +272,14 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_
     auto tokens = [&](int k) __attribute__((always_inline)) { return *reinterpret_cast<const int4*>(token + 16 * k + 4 * q); };
     bf16x8 mf[KS][8];
     u32x4 b0[4][W], b1[4][W];
+    // the first tokens' base, beside what the product waits for
+    int4 t0, t1;
+    {
+        int ts[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ts[i] = order[4 * q + i < tile.count ? 4 * q + i : 0];
+        t0 = make_int4(ts[0], ts[1], ts[2], ts[3]);
+    }
     float s = 0.f;
     if (tile.adapter >= 0) {
         const int rank = rank_of(a.g, tile.adapter);
@@ -287,6 +295,7 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_
                 const int64_t at = int64_t(r < rank ? r : 0) * a.C + oc;
                 rows[k][i] = rank > 0 ? *reinterpret_cast<const u32x4*>(m + 2 * at) : zero;
             }
+        load_base(t0, b0);
 #pragma unroll
         for (int i = threadIdx.x; i < 64 * NS * KS; i += kThreads) {
             const int l = i & 63, k = (i >> 6) % KS, n = (i >> 6) / KS, lq = l >> 4, lt = 16 * n + (l & 15);
@@ -312,10 +321,10 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_
 #pragma unroll
             for (int j = 0; j < 8; ++j) mf[k][j] = column(rows[k], j);
         }
+    } else {
+        load_base(t0, b0);
     }
     __syncthreads();
-    int4 t0 = tokens(0), t1;
-    load_base(t0, b0);
     auto finish = [&](int k, const int4& t, const u32x4 (&b)[4][W]) __attribute__((always_inline)) {
         f32x4 acc[8];
 #pragma unroll

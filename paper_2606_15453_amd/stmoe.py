@@ -103,9 +103,9 @@ _SIGS = {
     "moe_lora_plan_bytes": (sz, [i32, i32]),
     "moe_lora_plan": (i32, [vp, i32, i32, vp, sz, vp]),
     "moe_lora_workspace_bytes": (sz, [i32] * 6),
-    "moe_lora": (i32, [vp, i64, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, sz, vp]),
+    "moe_lora": (i32, [vp, i64, i32, i32, i32, i32, i32, i32, i32, vp, sz, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, sz, vp]),
     "moe_lora_backward_workspace_bytes": (sz, [i32] * 6),
-    "moe_lora_backward": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64,
+    "moe_lora_backward": (i32, [vp, i64, vp, i64, vp, i32, i32, i32, i32, i32, i32, vp, sz, vp, vp, vp, vp, vp, vp, vp, i64,
                                 vp, i64, vp, sz, vp]),
     "moe_mx_quantize": (i32, [vp, i64, i32, i64, i32, vp, vp, vp]),
     "moe_mx_dequantize": (i32, [vp, vp, i64, i32, vp, i64, i32, vp]),
@@ -585,11 +585,9 @@ def _plan(plan, dev):
 
 
 def _adapters(T, plan, a_ptrs, b_ptrs, ranks, scales, dev):
-    """(number of adapters, plan pointer) after the checks that lora and lora_backward share."""
+    """(number of adapters, plan pointer and bytes) after the checks that lora and lora_backward share."""
     n = a_ptrs.numel()
-    at, nbytes = _plan(plan, dev)
-    if nbytes < lora_plan_bytes(T, n):
-        raise ValueError(f"plan is not that of {T} tokens and {n} adapters")
+    at = _plan(plan, dev)
     for name, t in (("a_ptrs", a_ptrs), ("b_ptrs", b_ptrs)):
         _dense(name, t, (n,), (torch.int64,), dev)
     if ranks is not None:
@@ -636,7 +634,7 @@ def lora(x, plan, a_ptrs, b_ptrs, R, y, ws, base=None, ranks=None, scales=None, 
     n, at = _adapters(T, plan, a_ptrs, b_ptrs, ranks, scales, dev)
     if v is not None:
         _dense("v", v, (T, R), _F32, dev)
-    _call("moe_lora", x.data_ptr(), ldx, T, Hin, Hout, n, R, dt, _DTYPES[y.dtype], at, a_ptrs.data_ptr(),
+    _call("moe_lora", x.data_ptr(), ldx, T, Hin, Hout, n, R, dt, _DTYPES[y.dtype], *at, a_ptrs.data_ptr(),
           b_ptrs.data_ptr(), _p(ranks), _p(scales), _p(base), ld_base, y.data_ptr(), ldy, _p(v), *_workspace(ws, dev),
           _s(stream))
 
@@ -666,7 +664,7 @@ def lora_backward(x, dy, v, plan, a_ptrs, b_ptrs, R, da_ptrs, db_ptrs, ws, dx=No
     for name, t in (("da_ptrs", da_ptrs), ("db_ptrs", db_ptrs)):
         _dense(name, t, (n,), (torch.int64,), dev)
     _dense("v", v, (T, R), _F32, dev)
-    _call("moe_lora_backward", x.data_ptr(), ldx, dy.data_ptr(), ld_dy, v.data_ptr(), T, Hin, Hout, n, R, dt, at,
+    _call("moe_lora_backward", x.data_ptr(), ldx, dy.data_ptr(), ld_dy, v.data_ptr(), T, Hin, Hout, n, R, dt, *at,
           a_ptrs.data_ptr(), b_ptrs.data_ptr(), _p(ranks), _p(scales), da_ptrs.data_ptr(), db_ptrs.data_ptr(), _p(base),
           ld_base, _p(dx), ld_dx, *_workspace(ws, dev), _s(stream))
 

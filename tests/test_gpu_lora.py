@@ -287,6 +287,11 @@ def test_a_plan_of_another_batch_writes_nothing():
     assert (y == 2).all()
     _, dA, dB = b.backward(torch.zeros((40, 8), device=DEV))
     assert all(torch.isnan(m).all() for m in dA + dB)
+    b.plan = b.plan[:1024].clone()
+    with pytest.raises(S.StmoeError, match="plan too small"):
+        b.forward(y=y)
+    with pytest.raises(S.StmoeError, match="plan too small"):
+        b.backward(torch.zeros((40, 8), device=DEV))
 
 
 def test_the_gradient_of_x_does_not_take_its_place():

@@ -30,33 +30,33 @@ def test_workspace_sizes():
 
 
 def test_lora_refusals():
-    ok = dict(x=256, ldx=64, T=4, Hin=64, Hout=32, n=2, R=8, dt=S.BF16, yt=S.F32, plan=256, ap=256, bp=256, ranks=None,
+    ok = dict(x=256, ldx=64, T=4, Hin=64, Hout=32, n=2, R=8, dt=S.BF16, yt=S.F32, plan=256, pb=1 << 20, ap=256, bp=256, ranks=None,
               sc=None, base=256, ldb=32, y=512, ldy=32, v=None, ws=256, nb=1 << 30)
     for bad in [dict(x=None), dict(plan=None), dict(ap=None), dict(bp=None), dict(y=None), dict(ws=None), dict(T=-1),
                 dict(T=65537), dict(Hin=0), dict(Hout=0), dict(Hin=65537, ldx=65537), dict(n=0), dict(n=4097), dict(R=0),
                 dict(R=129), dict(dt=S.MXFP4), dict(yt=3), dict(ldx=63), dict(ldy=31), dict(ldb=31), dict(ldx=2 ** 31 + 1),
                 dict(x=257), dict(y=514), dict(base=257), dict(v=260), dict(plan=264), dict(ws=264), dict(nb=16),
-                dict(base=512, ldb=40)]:
+                dict(base=512, ldb=40), dict(pb=300)]:
         a = dict(ok, **bad)
-        rc = L.moe_lora(a["x"], a["ldx"], a["T"], a["Hin"], a["Hout"], a["n"], a["R"], a["dt"], a["yt"], a["plan"], a["ap"],
-                        a["bp"], a["ranks"], a["sc"], a["base"], a["ldb"], a["y"], a["ldy"], a["v"], a["ws"], a["nb"], None)
+        rc = L.moe_lora(a["x"], a["ldx"], a["T"], a["Hin"], a["Hout"], a["n"], a["R"], a["dt"], a["yt"], a["plan"],
+                        a["pb"], a["ap"], a["bp"], a["ranks"], a["sc"], a["base"], a["ldb"], a["y"], a["ldy"], a["v"], a["ws"], a["nb"], None)
         assert rc == S.EINVAL, bad
         assert L.stmoe_last_error().decode().startswith("moe_lora:")
-    assert L.moe_lora(None, 64, 0, 64, 32, 2, 8, 1, 0, None, None, None, None, None, None, 0, None, 32, None, None, 0,
+    assert L.moe_lora(None, 64, 0, 64, 32, 2, 8, 1, 0, None, 0, None, None, None, None, None, 0, None, 32, None, None, 0,
                       None) == S.OK
 
 
 def test_backward_refusals():
-    ok = dict(x=256, ldx=64, dy=256, ldy=32, v=256, T=4, Hin=64, Hout=32, n=2, R=8, dt=S.BF16, plan=256, ap=256, bp=256,
+    ok = dict(x=256, ldx=64, dy=256, ldy=32, v=256, T=4, Hin=64, Hout=32, n=2, R=8, dt=S.BF16, plan=256, pb=1 << 20, ap=256, bp=256,
               da=256, db=256, base=256, ldb=64, dx=512, ldd=64, ws=256, nb=1 << 30)
     for bad in [dict(x=None), dict(dy=None), dict(v=None), dict(plan=None), dict(ap=None), dict(bp=None), dict(da=None),
                 dict(db=None), dict(ws=None), dict(T=0), dict(T=65537), dict(Hin=0), dict(Hout=65537, ldy=65537), dict(n=0),
                 dict(R=129), dict(dt=2), dict(ldx=63), dict(ldy=31), dict(ldd=63), dict(ldb=63), dict(x=257), dict(dy=257),
                 dict(dx=257), dict(base=257), dict(v=264), dict(plan=264), dict(ws=264), dict(nb=16), dict(base=512, ldb=72),
-                dict(dx=256), dict(x=512)]:
+                dict(dx=256), dict(x=512), dict(pb=300)]:
         a = dict(ok, **bad)
         rc = L.moe_lora_backward(a["x"], a["ldx"], a["dy"], a["ldy"], a["v"], a["T"], a["Hin"], a["Hout"], a["n"], a["R"],
-                                 a["dt"], a["plan"], a["ap"], a["bp"], None, None, a["da"], a["db"], a["base"], a["ldb"],
+                                 a["dt"], a["plan"], a["pb"], a["ap"], a["bp"], None, None, a["da"], a["db"], a["base"], a["ldb"],
                                  a["dx"], a["ldd"], a["ws"], a["nb"], None)
         assert rc == S.EINVAL, bad
         assert L.stmoe_last_error().decode().startswith("moe_lora_backward:")
