@@ -516,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void route_scored_kernel(ScoredArgs a) {
         }
         if (a.renorm) total = row16::sum(w);
         w = mine >= 0 ? a.scale * (w / total) : 0.f;
-        if (a.fill && __any(l < a.K && mine < 0))
+        if (a.fill && __any(in && l < a.K && mine < 0))
             for (int e = 0; e < a.E; ++e) {
                 // the row's first free place takes the lowest expert it has not
                 const uint32_t has = uint32_t(__ballot(mine == e) >> (kLanes * r)) & 0xffffu;
