@@ -112,8 +112,9 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs a) {
     }
 }
 
-// One tile of 16 tokens and 256 columns a workgroup, 64 columns a wave: the lane
-// (c, q) feeds columns 4 c + j of row 4 q + i and gets columns 16 q .. + 15 of token c.
+// One tile of 16 tokens and 256 columns a workgroup, 64 columns a wave: the lane (c, q)
+// feeds columns 4 c .. + 3 of rank q (of every four) as the column operands and gets them
+// of tokens 4 q .. + 3.  VEC: of the adapter's rows and of base and y.
 template <bool BF, bool YBF, bool VEC>
 __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
     Tile tile;
@@ -146,20 +147,38 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
                 for (int p = 0; p < a.parts; ++p) vv += a.v[(int64_t(p) * a.g.T + t) * a.g.R + r];
             at4<BF, VEC>(m, int64_t(r) * a.C, o0 + 4 * c, a.C, r < rank, mv);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = mfma(mv[j], vv, acc[j]);
+            for (int j = 0; j < 4; ++j) acc[j] = mfma(vv, mv[j], acc[j]);
         }
     }
-    if (!in) return;
+    const int o = o0 + 4 * c;
+    if (o >= a.C) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+        if (4 * q + i >= tile.count) continue;
+        const int64_t t = a.g.plan.order[tile.first + 4 * q + i];
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.base) at4<YBF, VEC>(a.base, t * a.ld_base, o, a.C, true, y);
+        if (tile.adapter >= 0)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int o = o0 + 16 * q + 4 * i + j;
-            if (o < a.C) {
-                const float b = a.base ? at<YBF>(a.base, t * a.ld_base + o) : 0.f;
-                put<YBF>(a.y, t * a.ld + o, tile.adapter >= 0 ? b + s * acc[j][i] : b);
+            for (int j = 0; j < 4; ++j) y[j] += s * acc[j][i];
+        if constexpr (VEC) {
+            if constexpr (YBF) {
+                union {
+                    __bf16 h[4];
+                    uint2 q;
+                } u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u.h[j] = __bf16(y[j]);
+                *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.y) + t * a.ld + o) = u.q;
+            } else {
+                *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.y) + t * a.ld + o) = f32x4{y[0], y[1], y[2], y[3]};
             }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (o + j < a.C) put<YBF>(a.y, t * a.ld + o + j, y[j]);
         }
+    }
 }
 
 // A tile of tokens and 64 columns a workgroup, its waves every fourth four of the tokens.
@@ -306,7 +325,9 @@ int shrink(const ShrinkArgs& a, int tiles, bool bf, hipStream_t s) {
 
 int expand(const ExpandArgs& a, int tiles, bool bf, bool ybf, hipStream_t s) {
     const dim3 grid(unsigned(tiles), unsigned((a.C + 64 * kWaves - 1) / (64 * kWaves)));
-    with_rows(bf, a.C % 4 == 0, [&](auto b, auto vec) {
+    const int ysz = ybf ? 2 : 4;
+    const bool vec4 = fours(a.y, a.ld, a.C, ysz) && (!a.base || fours(a.base, a.ld_base, a.C, ysz));
+    with_rows(bf, vec4, [&](auto b, auto vec) {
         if (ybf) hipLaunchKernelGGL((lora_expand_kernel<b(), true, vec()>), grid, dim3(kThreads), 0, s, a);
         else hipLaunchKernelGGL((lora_expand_kernel<b(), false, vec()>), grid, dim3(kThreads), 0, s, a);
     });
