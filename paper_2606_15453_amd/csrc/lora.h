@@ -54,6 +54,24 @@ struct ExpandArgs {
     int64_t ld;
 };
 
+// The sum of v's parts (an even number) for a tile's tokens, shared among the `of`
+// workgroups that hold the tile's columns: one for all was the launch's last by far
+// (4096 x 4096, rank 64, two parts: 33.7 us, 23.7 so).
+__device__ __forceinline__ void sum_parts(const ExpandArgs& a, const int32_t* order, int count, int nth, int of) {
+    const int64_t part = int64_t(a.g.T) * a.g.R;
+    for (int i = nth * int(blockDim.x) + threadIdx.x; i < count * a.g.R; i += of * int(blockDim.x)) {
+        const int k = i / a.g.R;
+        const int64_t at = int64_t(order[k]) * a.g.R + (i - k * a.g.R);
+        float sum = 0.f;
+        for (int p = 0; p < a.parts; p += 2) {
+            const float v0 = a.v[p * part + at], v1 = a.v[(p + 1) * part + at];
+            sum += v0;
+            sum += v1;
+        }
+        a.v_out[at] = sum;
+    }
+}
+
 struct OuterArgs {
     Args g;
     const void* x;                 // [T] rows of C values, row stride ld

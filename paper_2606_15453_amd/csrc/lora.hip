@@ -13,8 +13,8 @@
 // in it, and a lane takes one value of each operand at a time, so any layout of rows and
 // columns does.  Rows that allow it are loaded four values at once (VEC).  Small calls
 // are bound by the latency of tile, order and rows, one load after the other (37 x 1000 x
-// 61 fp32: 6.6 and 6.3 us); large ones by the instruction and by loads of a row a lane:
-// 4096 x 2048 x 2048 fp32, rank 64, 171 us for 100 MB and 2.1 GFLOP.
+// 61 fp32: 6.7 and 4.6 us); large ones by loads of a row a lane and of the adapter again
+// for every 16 tokens: 4096 x 2048 x 2048 fp32, rank 64, 27 and 48 us for 100 MB.
 #include <type_traits>
 
 #include "lora.h"
@@ -119,13 +119,8 @@ template <bool BF, bool YBF, bool VEC>
 __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs a) {
     Tile tile;
     if (!tile_of(a.g, blockIdx.x, tile)) return;
-    if (a.v_out && a.parts > 1 && blockIdx.y == 0 && tile.adapter >= 0)
-        for (int i = threadIdx.x; i < tile.count * a.g.R; i += kThreads) {
-            const int64_t at = int64_t(a.g.plan.order[tile.first + i / a.g.R]) * a.g.R + i % a.g.R;
-            float sum = 0.f;
-            for (int p = 0; p < a.parts; ++p) sum += a.v[int64_t(p) * a.g.T * a.g.R + at];
-            a.v_out[at] = sum;
-        }
+    if (a.v_out && a.parts > 1 && tile.adapter >= 0)
+        sum_parts(a, a.g.plan.order + tile.first, tile.count, blockIdx.y, gridDim.y);
     if (tile.adapter < 0 && a.base == a.y) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int o0 = (blockIdx.y * kWaves + wave) * 64;
@@ -282,11 +277,18 @@ __global__ __launch_bounds__(kThreads) void lora_join_kernel(OuterArgs ox, Outer
     }
 }
 
-// Tokens per tile of the sums over tokens: 256, and 1024 for ranks above 16, whose sums
-// (R x C fp32 a tile) would be as many bytes as the rows.
-int outer_table(int, int, int R) { return R <= 16 ? 2 : 3; }
+// Tokens per tile of the sums over tokens: 256, and for ranks above 16, whose sums (R x C
+// fp32 a tile) would be as many bytes as the rows, 1024 from as many tokens on as give
+// the CUs a workgroup each (4096 x 4096 each way, one adapter of rank 64: the gradient 88
+// us with 256, 108 with 1024).
+int outer_limit(int Hin, int Hout) { return 131072 / (((Hin > Hout ? Hin : Hout) + 511) / 512); }
+int outer_table(int T, int Hin, int Hout, int R) { return R <= 16 || T < outer_limit(Hin, Hout) ? 2 : 3; }
+// Never falls as T grows.
 size_t outer_bytes(int T, int Hin, int Hout, int R) {
-    return outer_slots(T, tile_tokens(outer_table(T, 1, R))) * R * (size_t(Hin) + Hout) * sizeof(float);
+    const int most = outer_limit(Hin, Hout);
+    size_t slots = outer_slots(R <= 16 || T < most ? T : most, tile_tokens(2));
+    if (outer_table(T, Hin, Hout, R) == 3 && outer_slots(T, tile_tokens(3)) > slots) slots = outer_slots(T, tile_tokens(3));
+    return slots * R * (size_t(Hin) + Hout) * sizeof(float);
 }
 
 // Calls f(16-row tiles of the rank).
@@ -476,7 +478,7 @@ extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int
     if (int rc = shrink_expand(ShrinkArgs{g, dy, ld_dy, Hout, b_ptrs, 1, mine, parts},
                                ExpandArgs{g, mine, parts, u, a_ptrs, Hin, 0, base, ld_base, dx, ld_dx}, dtype, dtype, s))
         return rc;
-    const int table = outer_table(T, n_adapters, R);
+    const int table = outer_table(T, Hin, Hout, R);
     float* sums = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + rows_bytes(T, R) + rows_bytes(part_rows(T), R));
     const Args gt = with_table(g, table);
     const OuterArgs o[2] = {{gt, x, ldx, Hin, u, 0, da_ptrs, sums},

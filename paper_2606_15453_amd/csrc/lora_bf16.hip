@@ -247,13 +247,7 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_
     const int R = a.g.R, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
     const int64_t part = int64_t(a.g.T) * R;
     const int32_t* order = a.g.plan.order + tile.first;
-    if (a.v_out && a.parts > 1 && blockIdx.x == 0 && tile.adapter >= 0)
-        for (int i = threadIdx.x; i < tile.count * R; i += kThreads) {
-            const int64_t at = int64_t(order[i / R]) * R + i % R;
-            float sum = 0.f;
-            for (int p = 0; p < a.parts; ++p) sum += a.v[p * part + at];
-            a.v_out[at] = sum;
-        }
+    if (a.v_out && a.parts > 1 && tile.adapter >= 0) sum_parts(a, order, tile.count, blockIdx.x, gridDim.x);
     if (tile.adapter < 0 && a.base == a.y) return;
     // tokens beyond the last one: the first, whose row is not stored again
     if (threadIdx.x < 16 * NS) token[threadIdx.x] = order[int(threadIdx.x) < tile.count ? threadIdx.x : 0];
