@@ -436,8 +436,8 @@ int moe_lora_plan(const int32_t* adapter, int T, int n_adapters, void* plan, siz
 size_t moe_lora_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype);
 int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapters, int R, int dtype, int ydtype,
              const void* plan, size_t plan_bytes, const void* const* a_ptrs, const void* const* b_ptrs,
-             const int32_t* ranks, const float* scales, const void* base, int64_t ld_base, void* y, int64_t ldy, float* v, void* ws,
-             size_t ws_bytes, void* stream);
+             const int32_t* ranks, const float* scales, const void* base, int64_t ld_base, void* y,
+             int64_t ldy, float* v, void* ws, size_t ws_bytes, void* stream);
 /* Its gradient, for T >= 1: from dy (device [T] rows of Hout values, row stride
  * ld_dy, dtype), x and v as moe_lora took and gave them,
  *   dx[t] = base[t] + scale_a * (dy[t] B_a^T) A_a      (base NULL: zeros; dx
@@ -453,9 +453,9 @@ int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapter
 size_t moe_lora_backward_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype);
 int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int64_t ld_dy, const float* v, int T, int Hin,
                       int Hout, int n_adapters, int R, int dtype, const void* plan, size_t plan_bytes,
-                      const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks, const float* scales, float* const* da_ptrs,
-                      float* const* db_ptrs, const void* base, int64_t ld_base, void* dx, int64_t ld_dx, void* ws,
-                      size_t ws_bytes, void* stream);
+                      const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks,
+                      const float* scales, float* const* da_ptrs, float* const* db_ptrs, const void* base,
+                      int64_t ld_base, void* dx, int64_t ld_dx, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Expert cache policy (host only, no HIP calls): per-layer partition of C

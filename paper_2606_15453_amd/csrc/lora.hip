@@ -417,8 +417,8 @@ extern "C" size_t moe_lora_workspace_bytes(int T, int Hin, int Hout, int n_adapt
 
 extern "C" int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapters, int R, int dtype, int ydtype,
                         const void* plan, size_t plan_bytes, const void* const* a_ptrs, const void* const* b_ptrs,
-                        const int32_t* ranks, const float* scales, const void* base, int64_t ld_base, void* y, int64_t ldy, float* v, void* ws,
-                        size_t ws_bytes, void* stream) {
+                        const int32_t* ranks, const float* scales, const void* base, int64_t ld_base, void* y,
+                        int64_t ldy, float* v, void* ws, size_t ws_bytes, void* stream) {
     clear_error();
     if (const char* bad = bad_call(T, Hin, Hout, n_adapters, R, dtype, ydtype)) STMOE_CHECK(false, bad);
     if (T == 0) return STMOE_OK;
@@ -448,9 +448,10 @@ extern "C" size_t moe_lora_backward_workspace_bytes(int T, int Hin, int Hout, in
 
 extern "C" int moe_lora_backward(const void* x, int64_t ldx, const void* dy, int64_t ld_dy, const float* v, int T, int Hin,
                                  int Hout, int n_adapters, int R, int dtype, const void* plan, size_t plan_bytes,
-                                 const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks, const float* scales, float* const* da_ptrs,
-                                 float* const* db_ptrs, const void* base, int64_t ld_base, void* dx, int64_t ld_dx, void* ws,
-                                 size_t ws_bytes, void* stream) {
+                                 const void* const* a_ptrs, const void* const* b_ptrs, const int32_t* ranks,
+                                 const float* scales, float* const* da_ptrs, float* const* db_ptrs,
+                                 const void* base, int64_t ld_base, void* dx, int64_t ld_dx, void* ws, size_t ws_bytes,
+                                 void* stream) {
     clear_error();
     if (const char* bad = bad_call(T, Hin, Hout, n_adapters, R, dtype, dtype)) STMOE_CHECK(false, bad);
     STMOE_CHECK(T >= 1, "T must be in [1, 65536]");
