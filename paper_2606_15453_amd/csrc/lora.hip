@@ -13,7 +13,7 @@
 // in it, and a lane takes one value of each operand at a time, so any layout of rows and
 // columns does.  Rows that allow it are loaded four values at once (VEC).  Small calls
 // are bound by the latency of tile, order and rows, one load after the other (37 x 1000 x
-// 61 fp32: 6.7 and 4.6 us); large ones by loads of a row a lane and of the adapter again
+// 61 fp32: 6.6 and 5.3 us); large ones by loads of a row a lane and of the adapter again
 // for every 16 tokens: 4096 x 2048 x 2048 fp32, rank 64, 27 and 48 us for 100 MB.
 #include <type_traits>
 
