@@ -514,7 +514,8 @@ __global__ __launch_bounds__(kThreads) void route_scored_kernel(ScoredArgs a) {
         } else {
             w = mine >= 0 ? expf(zk - top) : 0.f;
         }
-        if (a.renorm) total = row16::sum(w);
+        // a softmax's sum that is NaN makes its row NaN, also where what is selected has none
+        if (a.renorm) total = total != total ? total : row16::sum(w);
         w = mine >= 0 ? a.scale * (w / total) : 0.f;
         if (a.fill && __any(in && l < a.K && mine < 0))
             for (int e = 0; e < a.E; ++e) {
