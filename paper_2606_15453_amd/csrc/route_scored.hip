@@ -512,6 +512,8 @@ __global__ __launch_bounds__(kThreads) void route_scored_kernel(ScoredArgs a) {
             w = sigmoid_of_row(zk, a.renorm);
             if (mine < 0) w = 0.f;
         } else {
+            // renormalised: from the selected ones' largest; the row's may be any distance above
+            if (a.renorm) top = largest(zk);
             w = mine >= 0 ? expf(zk - top) : 0.f;
         }
         // a softmax's sum that is NaN makes its row NaN, also where what is selected has none

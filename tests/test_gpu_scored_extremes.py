@@ -31,3 +31,53 @@ def test_nan_stays_in_renormalised_softmax_weights(T, bad):
             ri, rw, _ = scoredref.route(_f64(z[clean]), 4, "softmax", None if bias is None else _f64(bias), groups, top, 2, True)
             assert np.array_equal(idx.cpu().numpy()[clean], ri)
             np.testing.assert_allclose(_f64(w)[clean], rw, rtol=2.5e-6, atol=1e-30)
+
+
+@pytest.mark.parametrize("T", [40, 6400])
+def test_selected_logits_far_below_the_largest(T):
+    """The expert of the largest logit is ruled out by its bias or its group: the quotients are the selected ones' own."""
+    import torch
+    z = _logits(T, 16, 61, "float32")
+    for t, gap in enumerate((80, 90, 100, 104, 120, 200, 700)):
+        z[t, t] += gap
+    b = torch.zeros(16, device=DEV)
+    b[:8] = -INF
+    for bias, groups, top in ((b, 1, 1), (b, 4, 2), (b + torch.arange(16, device=DEV) * 1e-3, 1, 1)):
+        for K in (1, 4, 8):
+            _check(z, K, "softmax", bias, groups, top, 2, renorm=True, scale=1.5)
+            _check(z, K, "softmax", bias, groups, top, 1, renorm=True)
+
+
+@pytest.mark.parametrize("capped,graph", [(0, 0), (0, 1), (1, 0)])
+def test_selected_logits_far_below_the_largest_in_a_decode_context(capped, graph):
+    """Expert 0 has a logit of some 150 on every layer and is ruled out by its bias."""
+    import torch
+    from test_gpu_decode import Stack
+    from test_gpu_scored_decode import _context
+    from paper_2606_15453_amd import stmoe as S
+    from paper_2606_15453_amd import workload as W
+    st = Stack(W.CONFIGS["tiny"].scaled(P=8, B=1, T=1))
+    cfg = st.cfg
+    for l in range(cfg.L):
+        x = st.x_dev[0][l][0].float()
+        st.wg_dev[l][0] = (x * (150 / (x * x).sum())).to(st.wg_dev[l].dtype)
+    bias = torch.zeros((cfg.L, cfg.E), device=DEV)
+    bias[:, 0] = -INF
+    ctx, pred, keep = _context(st, capped, 0, graph, True)
+    ctx.set_routing("softmax", bias)
+    y = torch.full((cfg.L, cfg.B, cfg.H), float("nan"), device=DEV)
+    ws = torch.empty(S.route_workspace_bytes(cfg.B, cfg.E), dtype=torch.uint8, device=DEV)
+    i, w, z = (torch.empty((cfg.B, n), dtype=d, device=DEV) for n, d in
+               ((cfg.K, torch.int32), (cfg.K, torch.float32), (cfg.E, torch.float32)))
+    ctx.token(0, st.x_dev[0], y, mode=S.MODE_STMOE)
+    torch.cuda.synchronize()
+    idx, got = ctx.last_routing()
+    for l in range(cfg.L):
+        S.route_topk(st.x_dev[0][l], st.wg_dev[l], cfg.K, i, w, ws, logits=z)
+        assert z[0, 0] > 120
+        ri, rw, _ = scoredref.route(_f64(z), cfg.K, "softmax", _f64(bias[l]), renorm=True)
+        assert np.array_equal(idx[l], ri)
+        np.testing.assert_allclose(got[l], rw, rtol=2.5e-6, atol=1e-30)
+    assert torch.isfinite(y).all()
+    ctx.close()
+    pred.close()
