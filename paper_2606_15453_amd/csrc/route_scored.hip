@@ -373,7 +373,10 @@ __device__ __forceinline__ bool select(const ScoredArgs& a, RowRoom<V>& room, co
             second = fmax(fmax(second, o2), fmin(first, o1));
             first = fmax(first, o1);
         }
-        const F sum = a.group_top == 2 && second != F(-INFINITY) ? first + second : first;
+        const bool both = a.group_top == 2 && second != F(-INFINITY);
+        const F sum = both ? first + second : first;
+        // two numbers whose sum is none in 32 bits
+        if constexpr (F32) again |= both && !(fabsf(sum) < INFINITY);
         // both terms' slack, and that of the sum; none for a group without candidates
         const float off = sum == F(-INFINITY) ? -1.f : 4.f * slack(a.sigmoid, a.sigmoid ? 0.f : 1.f / total, float(sum));
         int before = 0;

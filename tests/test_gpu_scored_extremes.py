@@ -81,3 +81,20 @@ def test_selected_logits_far_below_the_largest_in_a_decode_context(capped, graph
     assert torch.isfinite(y).all()
     ctx.close()
     pred.close()
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("T", [500, 6500])
+def test_groups_by_sums_that_overflow(score, T):
+    """Two biases of the type's lowest or largest values: the group's score is beyond 32 bits and still has its place,
+    above that of a group without candidates."""
+    import torch
+    z = _logits(T, 8, 62, "float32")
+    low = torch.finfo(torch.float32).min
+    for bias, top, K in (([-INF, -INF, low, low, 0, 0, 0, 0], 3, 6), ([low, low, 0.9 * low, low, 0, 0, low, 0.8 * low], 2, 4),
+                         ([-INF, low, low, low, -INF, -INF, low, 0], 3, 6), ([-low, -0.9 * low, -low, -low, 0, 0, 0, 0], 1, 2),
+                         ([0, 0, -0.7 * low, -0.7 * low, -0.7 * low, -0.8 * low, 1, 1], 2, 3), ([low] * 8, 2, 4)):
+        b = torch.tensor(bias, device=DEV)
+        for renorm in (False, True):
+            _check(z, K, score, b, 4, top, 2, renorm)
+        _check(z, K, score, b, 4, top, 1)
