@@ -377,15 +377,21 @@ __device__ __forceinline__ bool select(const ScoredArgs& a, RowRoom<V>& room, co
         const F sum = both ? first + second : first;
         // two numbers whose sum is none in 32 bits
         if constexpr (F32) again |= both && !(fabsf(sum) < INFINITY);
-        // both terms' slack, and that of the sum; none for a group without candidates
-        const float off = sum == F(-INFINITY) ? -1.f : 4.f * slack(a.sigmoid, a.sigmoid ? 0.f : 1.f / total, float(sum));
+        // the terms' slack, each by its own size: terms of opposite sign leave a small sum of two
+        // large errors.  What slack has of |c| holds the sum's rounding too
+        float off = 0.f;
+        if constexpr (F32) {
+            const float p = a.sigmoid ? 0.f : 1.f / total;
+            if (first != F(-INFINITY)) off = 1.03125f * slack(a.sigmoid, p, first);
+            if (both) off += 1.03125f * slack(a.sigmoid, p, second);
+        }
         int before = 0;
         bool near = false;
         const auto against = [&](auto n) {
             const F other = rotate<n()>(sum);
             const int at = rotate<n()>(g);
             before += other > sum || (other == sum && at < g);
-            if constexpr (F32) near |= fabsf(other - sum) <= off;
+            if constexpr (F32) near |= fabsf(other - sum) <= off + rotate<n()>(off);
         };
         if (pairs) rotations<7>(against);
         else rotations<15>(against);
@@ -394,7 +400,8 @@ __device__ __forceinline__ bool select(const ScoredArgs& a, RowRoom<V>& room, co
             rotations<15>([&](auto n) {
                 const F other = rotate<n()>(sum);
                 const int there = rotate<n()>(before);
-                again |= fabsf(float(other - sum)) <= off && (there < a.top_groups) != (before < a.top_groups);
+                const float offs = off + rotate<n()>(off);
+                again |= fabsf(float(other - sum)) <= offs && (there < a.top_groups) != (before < a.top_groups);
             });
         }
         const uint32_t kept = uint32_t(__ballot(before < a.top_groups) >> (kLanes * r));

@@ -98,3 +98,20 @@ def test_groups_by_sums_that_overflow(score, T):
         for renorm in (False, True):
             _check(z, K, score, b, 4, top, 2, renorm)
         _check(z, K, score, b, 4, top, 1)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("size", [4.0, 64.0, 1000.0, 3e5])
+@pytest.mark.parametrize("T", [300, 6500])
+def test_groups_by_sums_that_cancel(score, size, T):
+    """A group's two choices near +size and -size: rounded to 2^-24 of those in 32 bits, while the sums of different groups
+    are nearer than that; seven blocks of eight rows have groups of nearly one score, a part of a rounding to 32 of them
+    apart."""
+    import torch
+    z = _logits(T, 16, 63, "float32")
+    k = torch.arange(T, device=DEV)[:, None] // 8 % 8
+    z = torch.where(k == 0, z, z * 2.0 ** (k - 22) * size)
+    sign = torch.tensor([1.0, -1.0], device=DEV).repeat(8)
+    for bias in (size * sign, size * sign + _bias(16, 63, 2.0 ** -10)):
+        for top, K in ((4, 8), (3, 2)):
+            _check(z, K, score, bias, 8, top, 2)
