@@ -155,11 +155,12 @@ __device__ __forceinline__ int select64(const ScoredArgs& a, int64_t row, bool l
     return mine;
 }
 
-// Scores whose quotients are the selected sigmoids', which may all be below the
-// smallest number: from -64 down 1 + e^z is 1, and e^(z - top) has their ratios.
+// Scores whose quotients are the selected sigmoids', which may be below the smallest number:
+// with a largest logit m below 0, of which they may be any fraction, e^-m times those.
 __device__ __forceinline__ float sigmoid_of_row(float z, bool renorm) {
-    const float top = largest(z);
-    return renorm && top < -64.f ? expf(z - top) : 1.f / (1.f + expf(-z));
+    const float m = renorm ? fminf(largest(z), 0.f) : 0.f;
+    const float e = expf(-fabsf(z));
+    return (z >= 0.f ? 1.f : m == 0.f ? e : expf(z - m)) / (1.f + e);
 }
 
 // A row's room: its choices in 64 bits, the group stage's values, or the candidates of

@@ -115,3 +115,30 @@ def test_groups_by_sums_that_cancel(score, size, T):
     for bias in (size * sign, size * sign + _bias(16, 63, 2.0 ** -10)):
         for top, K in ((4, 8), (3, 2)):
             _check(z, K, score, bias, 8, top, 2)
+
+
+@pytest.mark.parametrize("T", [9, 6200])
+def test_renormalised_sigmoids_of_very_negative_logits(T):
+    """Quotients of sigmoids of which some, or all, are below what 32 bits hold."""
+    import torch
+    from paper_2606_15453_amd import stmoe as S
+    z = -20 - 10 * torch.rand((T, 8), generator=torch.Generator(device=DEV).manual_seed(64), device=DEV)
+    for t, row in enumerate([[-60, -95], [-60, -88, -89, -105], [-30, -91], [-63.9, -100], [-64.1, -100, -110], [-1, -60],
+                             [0, -88, -80], [-200, -210, -260], [5, -70, 90]]):
+        z[t] = -INF
+        z[t, :len(row)] = torch.tensor(row, device=DEV)
+    b = torch.zeros(8, device=DEV)
+    for bias in (None, b):
+        _check(z, 4, "sigmoid", bias, renorm=True, scale=2.0)
+    idx, _, _ = _run(z, 4, score="sigmoid", renorm=True)
+    d_w = torch.randn((T, 4), generator=torch.Generator(device=DEV).manual_seed(65), device=DEV)
+    out = torch.empty_like(z)
+    S.route_scored_backward(z, idx, d_w, out, score="sigmoid", renorm=True)
+    ref = scoredref.route_grad(_f64(z), idx.cpu().numpy(), _f64(d_w), "sigmoid", True, 1.0)
+    # of an expert's own quotient times a difference of at most twice the largest d_w
+    p = scoredref.route(_f64(z), 4, "sigmoid", renorm=True)[1]
+    tol = np.zeros_like(ref)
+    for t in range(T):
+        k = idx[t].cpu().numpy() >= 0
+        tol[t, idx[t].cpu().numpy()[k]] = 1e-5 * p[t][k] * np.abs(_f64(d_w[t])).max() + 1e-30
+    assert (np.abs(_f64(out) - ref) <= tol).all()
