@@ -47,6 +47,24 @@ __device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&p)[N]) {
     }
 }
 
+// The numbers of an operand, zeros in the place of infinities and NaN: what pieces after the
+// first are multiplied with where a product came out as NaN.  An infinity against a piece of 0
+// or of the other sign than the value would be NaN or take the infinity back.
+__device__ __forceinline__ bf16x8 numbers(bf16x8 m) {
+    union {
+        bf16x8 v;
+        uint32_t w[4];
+    } u;
+    u.v = m;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        uint32_t w = u.w[d];
+        asm volatile("" : "+v"(w));        // made where it is used: kept beside m it costs registers
+        u.w[d] = ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+    }
+    return u.v;
+}
+
 // Columns of eight rows as operands: fragment j has column j of rows 0 to 7.
 __device__ __forceinline__ bf16x8 column(const u32x4 (&rows)[8], int j) {
     u32x4 q;
@@ -238,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 // columns as the row operand, 16 bytes of each of 64 rows a store, 49); 4096 x 4096, rank
 // 16, 19.3 us, 3.5 TB/s.
 template <int KS, bool PACK, bool YBF, int NS>
-__global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_bf16_kernel(ExpandArgs a) {
+__global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : NS == 1 ? 2 : 1) void lora_expand_bf16_kernel(ExpandArgs a) {
     constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P, W = YBF ? 1 : 2;
     __shared__ u32x4 vf[NS][NM][64];
     __shared__ __attribute__((aligned(16))) int32_t token[16 * NS];
@@ -330,6 +348,21 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : 1) void lora_expand_
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[j] = mfma(v, mf[PACK ? 0 : i / P][j], acc[j]);
             }
+            bool nan = false;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                nan |= __builtin_isunordered(acc[j][0], acc[j][1]) || __builtin_isunordered(acc[j][2], acc[j][3]);
+            if (__any(nan))
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = NM - 1; i >= 0; --i) {
+                        const bf16x8 m = mf[PACK ? 0 : i / P][j];
+                        const bool whole = PACK ? i == 0 && q < 2 : i % P == 0;
+                        acc[j] = mfma(operand(vf[k][i][lane]), whole ? m : numbers(m), acc[j]);
+                    }
+                }
         }
         const int ts[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
@@ -467,16 +500,49 @@ __global__ __launch_bounds__(kThreads) void lora_outer_bf16_kernel(OuterArgs ox,
     float* d = tiles == 1 ? a.d[tile.adapter]
                           : a.part + int64_t(outer_slot(tile.first, a.g.plan.size, tile.piece == tiles - 1)) * R * a.C;
     if (h >= a.C) return;
+    bool nan = false;
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int r = rt0 + 16 * i + 4 * q + k;
             if (r >= rank) continue;
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) nan |= __builtin_isunordered(acc[i][j][k], acc[i][j + 1][k]);
             f32x4* out = reinterpret_cast<f32x4*>(d + int64_t(r) * a.C + h);
             out[0] = f32x4{s * acc[i][0][k], s * acc[i][1][k], s * acc[i][2][k], s * acc[i][3][k]};
             out[1] = f32x4{s * acc[i][4][k], s * acc[i][5][k], s * acc[i][6][k], s * acc[i][7][k]};
         }
+    // sums that are NaN, perhaps of an infinite x against a piece of u (numbers()): again in fp32
+    if (!__any(nan)) return;
+#pragma unroll 1
+    for (int i = 0; i < RT; ++i) {
+        float sum[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[k][j] = 0.f;
+        const int r0 = rt0 + 16 * i + 4 * q;
+#pragma unroll 1
+        for (int p = 0; p < tile.count; ++p) {
+            const int64_t t = order[p];
+            const u32x4 row = *reinterpret_cast<const u32x4*>(x + 2 * (t * a.ld));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float v = r0 + k < rank ? a.u[t * R + r0 + k] : 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[k][j] += v * (j % 2 ? bf16_hi(row[j / 2]) : bf16_lo(row[j / 2]));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (r0 + k >= rank) continue;
+            float* out = d + int64_t(r0 + k) * a.C + h;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (out[j] != out[j]) out[j] = s * sum[k][j];
+        }
+    }
 }
 
 }  // namespace
