@@ -30,19 +30,22 @@ __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// N pieces of eight values.  What is left of a value that rounds to an infinity is
-// nothing, not NaN.
+// N pieces of eight values.  A number that rounds to an infinity has the largest bf16 number
+// for its first piece; of an infinity or NaN nothing is left.
 template <int N>
 __device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&p)[N]) {
+    constexpr float most = 3.38953138925153547590470800371487866880e38f;     // 2^128 (1 - 2^-8)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float left = x[i];
+        const bool number = fabsf(x[i]) < INFINITY;
+        float left = number ? fminf(fmaxf(x[i], -most), most) : x[i];
+        const float beyond = number ? x[i] - left : 0.f;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const __bf16 b = __bf16(left);
             p[k][i] = b;
-            const float f = float(b);
-            left = fabsf(f) < INFINITY ? left - f : 0.f;
+            left = number ? left - float(b) : 0.f;
+            if (k == 0) left += beyond;
         }
     }
 }

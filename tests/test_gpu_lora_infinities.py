@@ -1,5 +1,5 @@
-"""GPU: infinities in low-rank adapters' rows and matrices against the plain forms in 64 bits: an infinity where the
-formula has one, NaN where it has NaN, the same numbers elsewhere.
+"""GPU: infinities and values at the end of the range in low-rank adapters' rows and matrices against the plain forms in 64
+bits: an infinity where the formula has one, NaN where it has NaN, the same numbers elsewhere.
 
 An operand of bf16 is exact in the matrix instruction, the fp32 one (v, u) goes in as pieces: an infinity against a piece
 that is 0, or of the other sign than the value, must not show."""
@@ -97,3 +97,32 @@ def test_infinite_rows_and_adapters_of_the_gradient(dtype, T, Hin, Hout, n, R):
         rows = np.flatnonzero(b.ids == a)
         with np.errstate(invalid="ignore"):
             _same(dB[a], _f64(v)[rows].T @ _f64(b.dy)[rows], "dB of infinite rows", T)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_sums_at_the_end_of_the_range(dtype):
+    """v and u above the largest bf16 number round to an infinity in their first piece and are numbers all the same."""
+    import torch
+    T, big = 20, 3.395e38
+    b = Batch(T, 64, 64, 1, 16, dtype, "float32", ids=np.zeros(T), seed=72)
+    b.A[0].zero_()
+    b.A[0][:, 0], b.A[0][:, 1] = 2.0 ** 64, 2.0 ** 64
+    b.B[0].zero_()
+    b.B[0][3, 6] = 0.5
+    b.B[0][4, 7] = 2.0 ** -100
+    b.x.zero_()
+    b.x[:, 0], b.x[:, 1] = 255 * 2.0 ** 56, 127 * 2.0 ** 49     # 2^128 (1 - 2^-8 + 127 2^-15), which rounds up in bf16
+    b.scales.fill_(1.0)
+    b.base.zero_()
+    v = torch.empty((T, 16), device=DEV)
+    y = b.forward(v=v)
+    assert torch.isfinite(v).all() and (v > big).all()
+    want = _f64(v)[0, 0] * np.array([0.5, 2.0 ** -100])
+    np.testing.assert_allclose(_f64(y)[:, 6:8], np.tile(want, (T, 1)), rtol=2.0 ** -20)
+    assert not y[:, :6].any() and not y[:, 8:].any()
+    # dB = v^T dy, one token's own
+    b.dy.zero_()
+    b.dy[2, 11] = 2.0 ** -100
+    _, _, dB = b.backward(v, dx=None)
+    np.testing.assert_allclose(_f64(dB[0])[:, 11], want[1], rtol=2.0 ** -20)
+    assert not dB[0][:, :11].any() and not dB[0][:, 12:].any()
