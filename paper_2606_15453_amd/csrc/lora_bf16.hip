@@ -1,10 +1,10 @@
 // Low-rank adapters over bf16 rows in whole 16-byte chunks: the products of lora.hip on
 // the bf16 matrix instruction (16 x 16 x 32).
 //
-// One operand of every product is bf16 and exact; the fp32 one (v, u) is split into
-// bf16 pieces, the value's rounding and the roundings of what is left: two hold 16 bits
-// of it (2^-17 of itself off at most, where a bf16 result is rounded by 2^-9), three its
-// 24.
+// One operand of every product is bf16 and exact; the fp32 one (v, u) is split into three
+// bf16 pieces, the value's rounding and the roundings of what is left twice: its 24 bits.
+// (Two hold 16, which a bf16 result shows where its terms cancel; the third costs the product
+// over the rank 1 to 3%: 8192 x 4096, rank 64, 35.0 us with two, 35.7 with three.)
 #include <type_traits>
 
 #include "lora.h"
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_bf16_kernel(ShrinkArgs a
 // 16, 19.3 us, 3.5 TB/s.
 template <int KS, bool PACK, bool YBF, int NS>
 __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : NS == 1 ? 2 : 1) void lora_expand_bf16_kernel(ExpandArgs a) {
-    constexpr int P = YBF ? 2 : 3, NM = PACK ? (P + 1) / 2 : KS * P, W = YBF ? 1 : 2;
+    constexpr int P = 3, NM = PACK ? 2 : KS * P, W = YBF ? 1 : 2;
     __shared__ u32x4 vf[NS][NM][64];
     __shared__ __attribute__((aligned(16))) int32_t token[16 * NS];
     Tile tile;
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kThreads, KS <= 2 && YBF ? 3 : NS == 1 ? 2 : 1) voi
             split(v, p);
             if constexpr (PACK) {
                 *reinterpret_cast<bf16x8*>(&vf[n][0][l]) = lq < 2 ? p[0] : p[1];
-                if constexpr (P == 3) *reinterpret_cast<bf16x8*>(&vf[n][1][l]) = lq < 2 ? p[2] : operand(zero);
+                *reinterpret_cast<bf16x8*>(&vf[n][1][l]) = lq < 2 ? p[2] : operand(zero);
             } else {
 #pragma unroll
                 for (int j = 0; j < P; ++j) *reinterpret_cast<bf16x8*>(&vf[n][P * k + j][l]) = p[j];

@@ -1,4 +1,4 @@
-"""GPU: infinities and values at the end of the range in low-rank adapters' rows and matrices against the plain forms in 64
+"""GPU: infinities, values at the end of the range and terms that cancel in low-rank adapters against the plain forms in 64
 bits: an infinity where the formula has one, NaN where it has NaN, the same numbers elsewhere.
 
 An operand of bf16 is exact in the matrix instruction, the fp32 one (v, u) goes in as pieces: an infinity against a piece
@@ -126,3 +126,26 @@ def test_sums_at_the_end_of_the_range(dtype):
     _, _, dB = b.backward(v, dx=None)
     np.testing.assert_allclose(_f64(dB[0])[:, 11], want[1], rtol=2.0 ** -20)
     assert not dB[0][:, :11].any() and not dB[0][:, 12:].any()
+
+
+@pytest.mark.parametrize("T,R", [(3, 2), (40, 16), (200, 24), (70, 64), (150, 100), (1100, 16)])
+@pytest.mark.parametrize("ydtype", ["bfloat16", "float32"])
+def test_cancelling_terms(ydtype, T, R):
+    """v = 1 + 2^-9 + 2^-18, three bf16 pieces, less 1 + 2^-9: exact in 32 bits, and in either type of result; u so."""
+    import torch
+    b = Batch(T, 64, 64, 1, R, "bfloat16", ydtype, ids=np.zeros(T), seed=73)
+    for m in (b.A[0], b.B[0], b.x, b.dy, b.base, b.dbase):
+        m.zero_()
+    b.scales.fill_(1.0)
+    terms = torch.tensor([1.0, 2.0 ** -9, 2.0 ** -18], device=DEV)
+    b.x[:, :3], b.dy[:, 5:8] = terms, terms
+    b.A[0][0, :3], b.A[0][R - 1, :2] = 1.0, 1.0
+    b.B[0][0, 5:8], b.B[0][R - 1, 5:7] = 1.0, 1.0
+    b.A[0][0, 20], b.A[0][R - 1, 20] = 1.0, -1.0
+    b.B[0][0, 30], b.B[0][R - 1, 30] = 3.0, -3.0
+    v = torch.empty((T, R), device=DEV)
+    y = b.forward(v=v)
+    assert (v[:, 0] == 1 + 2.0 ** -9 + 2.0 ** -18).all()
+    assert (y[:, 30] == 3 * 2.0 ** -18).all()
+    dx, _, _ = b.backward(v)
+    assert (dx[:, 20] == 2.0 ** -18).all()
