@@ -236,7 +236,10 @@ int moe_route_balance_backward(const void* logits, int64_t T, int64_t ld, int E,
  * the logits themselves); equal ones go to the lower index, of experts and of
  * groups.  A logit or a bias of minus infinity is no candidate; the type's
  * lowest value is a number like others.  A choice that is NaN ranks below
- * every number; a softmax over a NaN or plus infinity is NaN throughout.
+ * every number; a softmax over a NaN or plus infinity is NaN throughout, and
+ * so are its weights, renormalised or not.  Weights are quotients of 32-bit
+ * exponentials; renormalised ones go by the selected logits alone, however far
+ * they are below others.
  *
  *   logits   device [T] rows of E values, row stride ld elements, dtype
  *   score    STMOE_SOFTMAX or STMOE_SIGMOID
@@ -249,8 +252,9 @@ int moe_route_balance_backward(const void* logits, int64_t T, int64_t ld, int E,
  *   counts   device [E] int32, or NULL: the number of selections of every
  *            expert is added to it
  *   0 <= T <= 2^26 (0: nothing is done); n_groups divides E; K at most 16 and
- *   the experts of top_groups groups.  One launch, no workspace.  The same
- *   inputs give the same bits.
+ *   the experts of top_groups groups.  One launch, beyond 6144 tokens two,
+ *   between which topk_idx holds marks (-2); no workspace.  The same inputs
+ *   give the same bits.
  * ---------------------------------------------------------------------- */
 enum { STMOE_SOFTMAX = 0, STMOE_SIGMOID = 1 };
 int moe_route_scored(const void* logits, int64_t T, int64_t ld, int E, int K, int dtype, int score,
@@ -259,7 +263,9 @@ int moe_route_scored(const void* logits, int64_t T, int64_t ld, int E, int K, in
                      int32_t* counts, void* stream);
 /* Its gradient: d_logits from the gradients d_w (device [T][K] fp32) of the
  * weights, with the selection topk_idx as a constant; entries outside [0, E)
- * have no part, an expert named twice counts twice.
+ * have no part, an expert named twice counts twice.  With renorm, and for
+ * sigmoids, the selected logits alone are read (a NaN beside them reaches the
+ * gradient by d_w).
  *   d_logits device out [T] rows of E values, row stride ld_d, dtype; may be
  *            logits itself when ld_d = ld */
 int moe_route_scored_backward(const void* logits, int64_t T, int64_t ld, int E, int K, int dtype, int score,
@@ -432,7 +438,8 @@ int moe_lora_plan(const int32_t* adapter, int T, int n_adapters, void* plan, siz
  *            ordered on one stream.  Its size never falls as T grows
  * dtype and ydtype: STMOE_BF16 or STMOE_F32 each; Hin, Hout 1 to 65536 (bf16:
  * multiples of 8 in 16-byte aligned rows are faster).  Sums are fp32, and x A^T
- * is held in 32 bits.  The same inputs give the same bits. */
+ * is held in 32 bits (24 of them enter the bf16 products, in three pieces).  The
+ * same inputs give the same bits. */
 size_t moe_lora_workspace_bytes(int T, int Hin, int Hout, int n_adapters, int R, int dtype);
 int moe_lora(const void* x, int64_t ldx, int T, int Hin, int Hout, int n_adapters, int R, int dtype, int ydtype,
              const void* plan, size_t plan_bytes, const void* const* a_ptrs, const void* const* b_ptrs,
